@@ -254,6 +254,70 @@ epd_status epd_encode_cached(epd_handle h, epd_store_handle s, uint64_t model_sa
                              void* out_visual_tokens, int32_t* hit_out, uint64_t* keys_out,
                              void* stream);
 
+/* ---- operators beside the encoder ---------------------------------------------------------
+ * What a program computes around V_m = E(I_m) with the same building blocks.  They have no handle: every
+ * call names its sizes, buffers and stream, allocates nothing, waits for nothing and may be captured
+ * into a graph.  Calls share nothing, so they may be made from several threads and streams; where a call takes
+ * a workspace, that is its own until its kernels have run.  Buffers and stream belong to the
+ * current device.  Outputs must not overlap inputs unless it is said that they may.  Results are
+ * deterministic.  On an error nothing is launched (EPD_ERR_HIP: nothing further). */
+
+/* Message of the last failure of such a call on this thread.  Never NULL. */
+const char* epd_op_last_error(void);
+
+/* Rotary positions with several axes.  A head has P = sum of pairs[] rotary pairs, pair p belongs to
+ * one axis and turns by positions[axis][token] * f_p, (x, y) -> (x cos - y sin, x sin + y cos);
+ * head elements from 2 P on stay as they are.  The encoder's own embedding (epd_encode_cfg) is
+ * SECTIONS, LADDER_AXIS, HALF with raster positions. */
+typedef enum { EPD_ROPE_SECTIONS = 0, EPD_ROPE_INTERLEAVED = 1 } epd_rope_layout;
+typedef enum { EPD_ROPE_LADDER_AXIS = 0, EPD_ROPE_LADDER_HEAD = 1 } epd_rope_ladder;
+typedef enum { EPD_ROPE_HALF = 0, EPD_ROPE_ADJACENT = 1 } epd_rope_pairing;
+typedef struct {
+  uint32_t struct_size; /* sizeof(epd_rope_cfg)                                                     */
+  int32_t dtype;        /* epd_dtype of the tensors; turned in fp32, rounded once                   */
+  int32_t head_dim;     /* 2 .. 256                                                                 */
+  int32_t axes;         /* 1 .. 4: rows of positions                                                */
+  int32_t pairs[4];     /* rotary pairs of each axis, P = their sum, 1 <= P <= head_dim / 2          */
+  int32_t layout;       /* SECTIONS: the pairs of axis 0, then those of axis 1, ...  INTERLEAVED: one
+                           pair of every axis that still has any, in turn                          */
+  int32_t ladder;       /* AXIS: f_p = base^(-j/n) for the j-th of an axis's n pairs; HEAD:
+                           f_p = base^(-p/P)                                                        */
+  int32_t pairing;      /* HALF: pair p = elements (p, p + P); ADJACENT: (2p, 2p + 1)               */
+  double base;          /* > 0                                                                      */
+} epd_rope_cfg;
+typedef struct {
+  const void* in;       /* device; element e of head h of token t at in[t * in_token + h * in_head + e] */
+  void* out;            /* device; the same with out_*.  May be `in` (then with the same strides)   */
+  int64_t in_token, in_head, out_token, out_head; /* strides in elements, 0 .. 2^40; rows of `out` are
+                           apart, `in` may repeat rows (stride 0)                                   */
+  int32_t heads;        /* 0 .. 256                                                                 */
+} epd_rope_tensor;
+
+/* Turn `tokens` rows of num_tensors (1 .. 4) tensors, say q and k, by the same positions.
+ *   positions  device int32, axis x of token t at positions[x * position_stride + t]; any value
+ *   inverse    1: turn back (by the negated angle): the gradient of the call with inverse = 0
+ * tensors is a HOST array.  tokens = 0 launches nothing.  EPD_ERR_INVALID_ARG, EPD_ERR_UNSUPPORTED
+ * (sizes outside of the ranges above), EPD_ERR_SHAPE (strides). */
+epd_status epd_rope_apply(const epd_rope_cfg* cfg, const epd_rope_tensor* tensors, int32_t num_tensors,
+                          const int32_t* positions, int64_t position_stride, int32_t tokens,
+                          int32_t inverse, void* stream);
+
+/* (t, h, w) positions of sequences of text and visual tokens (V_m || V_t, section 3.1 "Prefill Stage",
+ * Eq. 2; the paper does not say how they are counted).  A sequence starts at p = start[s]; a text of n
+ * tokens takes positions p .. p + n - 1 on all three axes, and p moves on by n; an item of (t, h, w) tokens
+ * (visual tokens: the grid behind the merge), in raster order, takes (p + t_step * ti, p + r, p + c), and p moves
+ * on by max(t_step * (t - 1) + 1, h, w).
+ *   span_thw    HOST int32 [num_spans, 3]: (n, 0, 0) = a text of n >= 0 tokens, else an item's (t, h, w) >= 1
+ *   cu_spans    HOST int32 [num_sequences + 1]: sequence s has the spans [cu[s], cu[s+1])
+ *   start       HOST int32 [num_sequences], or NULL = 0 (a conversation goes on at an earlier next_out)
+ *   positions   device int32 [3, position_stride], position_stride >= tokens; tokens in the order of the spans
+ *   next_out    HOST int32 [num_sequences], or NULL: p behind each sequence, its next token's position
+ * Host arrays are consumed before the call returns.  EPD_ERR_SHAPE where the spans are inconsistent or
+ * tokens or positions pass 2^31 - 1. */
+epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, int32_t num_sequences,
+                              const int32_t* start, int32_t t_step, int32_t* positions,
+                              int64_t position_stride, int32_t* next_out, void* stream);
+
 /* Release host-side state (events, pinned staging).  The workspace stays the caller's. */
 epd_status epd_encode_destroy(epd_handle h);
 

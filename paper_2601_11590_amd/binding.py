@@ -23,6 +23,9 @@ EPD_F32, EPD_BF16 = 0, 1
 EPD_LAYERNORM, EPD_RMSNORM = 0, 1
 EPD_GELU_ERF, EPD_GELU_TANH = 0, 1
 EPD_ROPE_NONE, EPD_ROPE_2D, EPD_ROPE_3D = 0, 2, 3
+EPD_ROPE_SECTIONS, EPD_ROPE_INTERLEAVED = 0, 1
+EPD_ROPE_LADDER_AXIS, EPD_ROPE_LADDER_HEAD = 0, 1
+EPD_ROPE_HALF, EPD_ROPE_ADJACENT = 0, 1
 (EPD_STEP_PLAN, EPD_STEP_PATCH_EMBED, EPD_STEP_NORM, EPD_STEP_QKV, EPD_STEP_ATTN, EPD_STEP_PROJ,
  EPD_STEP_FC1, EPD_STEP_FC2, EPD_STEP_MERGE, EPD_STEP_COUNT) = range(10)
 STEP_NAMES = ["plan", "patch_embed", "norm", "qkv", "attn", "proj", "fc1", "fc2", "merge"]
@@ -55,11 +58,23 @@ class epd_encode_cfg(C.Structure):
                 ("workspace_bytes", C.c_uint64)]
 
 
+class epd_rope_cfg(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("head_dim", C.c_int32), ("axes", C.c_int32),
+                ("pairs", C.c_int32 * 4), ("layout", C.c_int32), ("ladder", C.c_int32), ("pairing", C.c_int32),
+                ("base", C.c_double)]
+
+
+class epd_rope_tensor(C.Structure):
+    _fields_ = [("input", C.c_void_p), ("output", C.c_void_p), ("in_token", C.c_int64), ("in_head", C.c_int64),   # C names: in, out
+                ("out_token", C.c_int64), ("out_head", C.c_int64), ("heads", C.c_int32)]
+
+
 EXPORTS = ["epd_encode_workspace_bytes", "epd_encode_create", "epd_encode", "epd_encode_destroy",
            "epd_encode_last_error", "epd_encode_debug_hidden", "epd_encode_set_timing", "epd_encode_set_tuning", "epd_encode_set_compute_units",
            "epd_encode_get_timing", "epd_preprocess", "epd_encode_cached", "epd_store_create",
            "epd_store_destroy", "epd_store_last_error", "epd_store_hash", "epd_store_hash_noalloc", "epd_store_lookup", "epd_store_insert",
            "epd_store_stats", "epd_probe_stream_read", "epd_probe_mfma_rate", "epd_probe_gemm_plan"]
+OPERATOR_EXPORTS = ["epd_op_last_error", "epd_rope_apply", "epd_rope_positions"]    # the operators beside the encoder
 
 
 def _load() -> C.CDLL:
@@ -115,6 +130,14 @@ def _load() -> C.CDLL:
     lib.epd_encode_get_timing.restype = C.c_int
     lib.epd_encode_get_timing.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int64),
                                           C.POINTER(C.c_double)]
+    lib.epd_op_last_error.restype = C.c_char_p
+    lib.epd_op_last_error.argtypes = []
+    lib.epd_rope_apply.restype = C.c_int
+    lib.epd_rope_apply.argtypes = [C.POINTER(epd_rope_cfg), C.POINTER(epd_rope_tensor), C.c_int32, C.c_void_p, C.c_int64,
+                                   C.c_int32, C.c_int32, C.c_void_p]
+    lib.epd_rope_positions.restype = C.c_int
+    lib.epd_rope_positions.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64,
+                                       C.c_void_p, C.c_void_p]
     return lib
 
 
@@ -516,6 +539,121 @@ class MMStore:
 def to_device_patches(patches_f32: np.ndarray, dtype: str, device: str = "cuda:0") -> torch.Tensor:
     """Host float32 rows (already rounded to ``dtype``) -> device tensor of that dtype."""
     return torch.from_numpy(np.ascontiguousarray(patches_f32)).to(device).to(torch_dtype(dtype)).contiguous()
+
+
+# ---------------------------------------------------------------- operators beside the encoder
+
+def epd_op_last_error() -> str:
+    return lib.epd_op_last_error().decode()
+
+
+def _op_check(status: int) -> None:
+    if status != EPD_OK:
+        raise EpdError(status, epd_op_last_error())
+
+
+def epd_rope_apply(cfg: epd_rope_cfg, tensors, positions: int, position_stride: int, tokens: int, inverse: bool, stream: int) -> None:
+    """tensors: a ctypes array of ``epd_rope_tensor``."""
+    _op_check(lib.epd_rope_apply(C.byref(cfg), tensors, len(tensors), positions, position_stride, tokens, 1 if inverse else 0, stream))
+
+
+def epd_rope_positions(span_thw: np.ndarray, cu_spans: np.ndarray, start: Optional[np.ndarray], t_step: int, positions: int,
+                       position_stride: int, stream: int) -> np.ndarray:
+    """Returns the next position of every sequence, int32 [num_sequences]."""
+    span = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
+    cu = np.ascontiguousarray(cu_spans, dtype=np.int32)
+    if cu.ndim != 1 or len(cu) < 1 or (len(cu) > 1 and int(cu.max()) > len(span)):
+        raise ValueError("cu_spans must be [num_sequences + 1] and end within the spans")
+    n = len(cu) - 1
+    if start is not None:
+        start = np.ascontiguousarray(start, dtype=np.int32)
+        if start.shape != (n,):
+            raise ValueError("start must be [num_sequences]")
+    after = np.empty(n, dtype=np.int32)
+    _op_check(lib.epd_rope_positions(span.ctypes.data, cu.ctypes.data, n, None if start is None else start.ctypes.data, t_step, positions,
+                                     position_stride, after.ctypes.data, stream))
+    return after
+
+
+class _on:
+    """Makes a tensor's device the current one around a call, where it is not."""
+
+    def __init__(self, device: torch.device):
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+        self.device = device
+
+    def __enter__(self) -> int:
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str = "cuda:0", out: Optional[torch.Tensor] = None):
+    """(t, h, w) positions of sequences of texts (n, 0, 0) and items (t, h, w), sequence s being the spans
+    [cu_spans[s], cu_spans[s + 1]) and starting at start[s].  Returns (int32 device tensor [3, tokens], next position of every
+    sequence int32 [sequences])."""
+    span = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
+    cu = np.ascontiguousarray(cu_spans, dtype=np.int32)
+    used = span[:int(cu[-1])].astype(np.int64)
+    tokens = max(0, int(np.where(used[:, 1] == 0, used[:, 0], used.prod(axis=1)).sum()))
+    dev = torch.device(device) if out is None else out.device
+    if dev.index is None:
+        dev = torch.device(dev.type, torch.cuda.current_device())
+    if out is None:
+        out = torch.empty((3, tokens), dtype=torch.int32, device=dev)
+    if not out.is_cuda or out.dtype != torch.int32 or out.dim() != 2 or out.shape[0] != 3 or out.shape[1] < tokens or (out.shape[1] and out.stride(1) != 1):
+        raise ValueError("out must be a device int32 [3, >= tokens] whose rows are contiguous")
+    with _on(dev) as stream:
+        after = epd_rope_positions(span, cu, start, t_step, out.data_ptr() or 256, out.stride(0), stream)      # no tokens: nothing is written
+    return out, after
+
+
+class Rope:
+    """Rotation of q / k rows by positions on several axes (``epd_rope_apply``)."""
+
+    def __init__(self, dtype: str, head_dim: int, pairs: Sequence[int], layout: str = "sections", ladder: str = "axis", pairing: str = "half",
+                 base: float = 10000.0):
+        c = self.cfg = epd_rope_cfg()
+        c.struct_size = C.sizeof(epd_rope_cfg)
+        c.dtype = {"f32": EPD_F32, "bf16": EPD_BF16}[dtype]
+        c.head_dim, c.axes = head_dim, len(pairs)
+        if not 1 <= len(pairs) <= 4:
+            raise ValueError("pairs: one to four axes")
+        c.pairs = (C.c_int32 * 4)(*pairs)
+        c.layout = {"sections": EPD_ROPE_SECTIONS, "interleaved": EPD_ROPE_INTERLEAVED}[layout]
+        c.ladder = {"axis": EPD_ROPE_LADDER_AXIS, "head": EPD_ROPE_LADDER_HEAD}[ladder]
+        c.pairing = {"half": EPD_ROPE_HALF, "adjacent": EPD_ROPE_ADJACENT}[pairing]
+        c.base = base
+        self.dtype, self.head_dim, self.axes = torch_dtype(dtype), head_dim, len(pairs)
+
+    def apply(self, tensors: Sequence[torch.Tensor], positions: torch.Tensor, inverse: bool = False,
+              out: Optional[Sequence[torch.Tensor]] = None):
+        """tensors: one to four of [tokens, heads, head_dim] (views with any strides but the last), positions int32 [axes, tokens].
+        Returns the turned tensors: ``out``, which may be ``tensors`` itself, or new ones.  ``inverse`` turns back: the gradients of
+        the inputs, given those of the outputs."""
+        T = positions.shape[-1]
+        if not positions.is_cuda or positions.dtype != torch.int32 or positions.dim() != 2 or positions.shape[0] != self.axes or (T > 1 and positions.stride(1) != 1):
+            raise ValueError("positions must be a device int32 [%d, tokens] whose rows are contiguous" % self.axes)
+        if out is None:
+            out = [torch.empty(x.shape, dtype=self.dtype, device=x.device) for x in tensors]
+        if len(out) != len(tensors):
+            raise ValueError("as many outputs as tensors")
+        arr = (epd_rope_tensor * len(tensors))()
+        for a, x, y in zip(arr, tensors, out):
+            for v in (x, y):
+                if v.device != positions.device or v.dtype != self.dtype or v.dim() != 3 or v.shape[0] != T or v.shape[2] != self.head_dim or v.shape != x.shape:
+                    raise ValueError("tensors must be [tokens, heads, %d] of %s on the positions' device" % (self.head_dim, self.dtype))
+                if v.stride(2) != 1 and v.numel():
+                    raise ValueError("the elements of a head must be contiguous")
+            si, so = x.stride(), y.stride()
+            a.input, a.output, a.in_token, a.in_head, a.out_token, a.out_head, a.heads = x.data_ptr(), y.data_ptr(), si[0], si[1], so[0], so[1], x.shape[1]
+        with _on(positions.device) as stream:
+            epd_rope_apply(self.cfg, arr, positions.data_ptr() or 256, positions.stride(0), T, inverse, stream)
+        return list(out)
 
 
 EPI_STORE, EPI_GELU, EPI_RESIDUAL, EPI_QKV = 0, 1, 2, 3

@@ -2,8 +2,7 @@
 // 3.1, Eq. 1).  Host-side only: validates, partitions the caller's workspace, builds the
 // per-call plan (segment / item offsets, attention work list), and enqueues the kernels of
 // the ViT forward pass on the caller's stream.  No device memory is allocated here.
-#include "../../include/epd_encode.h"
-#include "epd_internal.h"
+#include "op_error.h"
 
 #include <algorithm>
 #include <cmath>
@@ -18,6 +17,7 @@ using namespace epd;
 namespace {
 
 thread_local std::string g_create_error = "";
+thread_local char g_op_error[512] = "";
 
 constexpr size_t kAlign = 256;
 constexpr int kStagingSlots = 4;
@@ -282,7 +282,17 @@ epd_status copy_weight(epd_encoder* h, size_t dst_off, const void* src, size_t b
 
 }  // namespace
 
+epd_status epd::op_fail(epd_status status, const char* format, ...) {
+  va_list ap;
+  va_start(ap, format);
+  vsnprintf(g_op_error, sizeof(g_op_error), format, ap);
+  va_end(ap);
+  return status;
+}
+
 extern "C" {
+
+const char* epd_op_last_error(void) { return g_op_error; }
 
 uint64_t epd_encode_workspace_bytes(const epd_encode_cfg* cfg) {
   std::string err;

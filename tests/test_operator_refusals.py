@@ -1,0 +1,145 @@
+"""What the operators beside the encoder refuse, all on the host: nothing is launched, no GPU is needed."""
+
+import ctypes as C
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2601_11590_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "epd_encode.h")
+
+
+def test_every_declared_operator_is_exported():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(epd_(?:op|rope|gated)_\w+)\s*\(", text))
+    assert names == set(B.OPERATOR_EXPORTS)
+    for n in names:
+        assert getattr(B.lib, n) is not None
+
+
+def test_structs_and_enums_match_the_header(tmp_path):
+    structs = {"epd_rope_cfg": B.epd_rope_cfg, "epd_rope_tensor": B.epd_rope_tensor}
+    lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "epd_encode.h"', "int main(void) {"]
+    want = []
+    for name, t in structs.items():
+        lines.append('printf("%%zu\\n", sizeof(%s));' % name)
+        want.append(C.sizeof(t))
+        for f, _ in t._fields_:
+            lines.append('printf("%%zu\\n", offsetof(%s, %s));' % (name, {"input": "in", "output": "out"}.get(f, f)))
+            want.append(getattr(t, f).offset)
+    for e in ("EPD_ROPE_SECTIONS", "EPD_ROPE_INTERLEAVED", "EPD_ROPE_LADDER_AXIS", "EPD_ROPE_LADDER_HEAD", "EPD_ROPE_HALF", "EPD_ROPE_ADJACENT"):
+        lines.append('printf("%%d\\n", (int)%s);' % e)
+        want.append(getattr(B, e))
+    src = tmp_path / "probe.c"
+    src.write_text("\n".join(lines + ["return 0; }"]))
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(tmp_path / "probe")], check=True)
+    out = subprocess.run([str(tmp_path / "probe")], check=True, stdout=subprocess.PIPE, text=True).stdout.split()
+    assert [int(v) for v in out] == want
+
+
+# ------------------------------------------------------------------ rotation
+
+def rope(cfg=None, tensors=None, positions=0x1000, stride=64, tokens=10, inverse=0, **change):
+    c = B.Rope("bf16", 64, (8, 12, 12)).cfg
+    for k, v in change.items():
+        if k == "pairs":
+            v = (C.c_int32 * 4)(*v)
+        setattr(c, k, v)
+    if tensors is None:
+        tensors = [dict()]
+    arr = (B.epd_rope_tensor * max(1, len(tensors)))()
+    for a, t in zip(arr, tensors):
+        d = dict(input=0x10000, output=0x20000, in_token=256, in_head=64, out_token=256, out_head=64, heads=4)
+        d.update(t)
+        for k, v in d.items():
+            setattr(a, k, v)
+    st = B.lib.epd_rope_apply(C.byref(c) if cfg is None else cfg, arr, len(tensors), positions, stride, tokens, inverse, None)
+    return st, B.epd_op_last_error()
+
+
+@pytest.mark.parametrize("kw,status,needle", [
+    (dict(struct_size=4), B.EPD_ERR_INVALID_ARG, "struct_size"),
+    (dict(dtype=2), B.EPD_ERR_INVALID_ARG, "dtype"),
+    (dict(layout=2), B.EPD_ERR_INVALID_ARG, "layout"),
+    (dict(ladder=-1), B.EPD_ERR_INVALID_ARG, "ladder"),
+    (dict(pairing=5), B.EPD_ERR_INVALID_ARG, "pairing"),
+    (dict(axes=0), B.EPD_ERR_INVALID_ARG, "axes"),
+    (dict(axes=5), B.EPD_ERR_INVALID_ARG, "axes"),
+    (dict(base=0.0), B.EPD_ERR_INVALID_ARG, "base"),
+    (dict(base=float("nan")), B.EPD_ERR_INVALID_ARG, "base"),
+    (dict(base=float("inf")), B.EPD_ERR_INVALID_ARG, "base"),
+    (dict(head_dim=258), B.EPD_ERR_UNSUPPORTED, "head_dim"),
+    (dict(head_dim=0), B.EPD_ERR_UNSUPPORTED, "head_dim"),
+    (dict(pairs=(-1, 12, 12, 0)), B.EPD_ERR_INVALID_ARG, "pairs"),
+    (dict(pairs=(0, 0, 0, 0)), B.EPD_ERR_UNSUPPORTED, "pairs"),
+    (dict(pairs=(9, 12, 12, 0)), B.EPD_ERR_UNSUPPORTED, "33 pairs"),
+    (dict(pairs=(2147483647, 2147483647, 12, 0)), B.EPD_ERR_INVALID_ARG, "pairs"),
+    (dict(tokens=-1), B.EPD_ERR_SHAPE, "tokens"),
+    (dict(stride=9), B.EPD_ERR_SHAPE, "position_stride"),
+    (dict(positions=None), B.EPD_ERR_INVALID_ARG, "NULL"),
+    (dict(inverse=2), B.EPD_ERR_INVALID_ARG, "inverse"),
+    (dict(tensors=[]), B.EPD_ERR_INVALID_ARG, "num_tensors"),
+    (dict(tensors=[{}] * 5), B.EPD_ERR_INVALID_ARG, "num_tensors"),
+    (dict(tensors=[{}, dict(input=None)]), B.EPD_ERR_INVALID_ARG, "tensor 1"),
+    (dict(tensors=[dict(output=None)]), B.EPD_ERR_INVALID_ARG, "NULL"),
+    (dict(tensors=[dict(input=0x10001)]), B.EPD_ERR_INVALID_ARG, "aligned"),
+    (dict(tensors=[dict(heads=257)]), B.EPD_ERR_UNSUPPORTED, "heads"),
+    (dict(tensors=[dict(heads=-1)]), B.EPD_ERR_UNSUPPORTED, "heads"),
+    (dict(tensors=[dict(in_token=-64)]), B.EPD_ERR_SHAPE, "stride"),
+    (dict(tensors=[dict(out_head=1 << 41)]), B.EPD_ERR_SHAPE, "stride"),
+    (dict(tensors=[dict(out_token=0)]), B.EPD_ERR_SHAPE, "overlap"),
+    (dict(tensors=[dict(out_head=63)]), B.EPD_ERR_SHAPE, "overlap"),
+    (dict(tensors=[dict(out_token=255)]), B.EPD_ERR_SHAPE, "overlap"),
+    (dict(tensors=[dict(out_token=64, out_head=639)]), B.EPD_ERR_SHAPE, "overlap"),
+    (dict(tensors=[dict(output=0x10000, in_token=512)]), B.EPD_ERR_SHAPE, "in place"),
+])
+def test_rope_refusals(kw, status, needle):
+    st, msg = rope(**kw)
+    assert st == status and needle in msg, msg
+
+
+def test_rope_calls_without_work_launch_nothing():
+    assert rope(tokens=0)[0] == B.EPD_OK
+    assert rope(tokens=0, tensors=[dict(input=None, output=None)])[0] == B.EPD_OK
+    assert rope(tensors=[dict(heads=0, input=None, output=None)])[0] == B.EPD_OK
+    assert rope(cfg=C.POINTER(B.epd_rope_cfg)())[0] == B.EPD_ERR_INVALID_ARG
+
+
+# ------------------------------------------------------------------ positions
+
+def pos(spans, cu, start=None, t_step=1, positions=0x1000, stride=1 << 40):
+    span, cu = np.array(spans, dtype=np.int32).reshape(-1, 3), np.array(cu, dtype=np.int32)
+    st0 = None if start is None else np.array(start, dtype=np.int32)
+    st = B.lib.epd_rope_positions(span.ctypes.data, cu.ctypes.data, len(cu) - 1, None if st0 is None else st0.ctypes.data, t_step, positions, stride, None, None)
+    return st, B.epd_op_last_error()
+
+
+@pytest.mark.parametrize("kw,needle", [
+    (dict(spans=[(-1, 0, 0)], cu=[0, 1]), "span 0"),
+    (dict(spans=[(3, 0, 0), (0, 2, 2)], cu=[0, 2]), "span 1"),
+    (dict(spans=[(1, 2, 0)], cu=[0, 1]), "span 0"),
+    (dict(spans=[(1, -2, -2)], cu=[0, 1]), "span 0"),
+    (dict(spans=[(3, 0, 0)], cu=[1, 1]), "start at 0"),
+    (dict(spans=[(3, 0, 0), (3, 0, 0)], cu=[0, 2, 1]), "decreases"),
+    (dict(spans=[(2, 65536, 65536)], cu=[0, 1]), "too many tokens"),
+    (dict(spans=[(2 ** 31 - 1, 0, 0), (1, 0, 0)], cu=[0, 1, 2]), "more than"),
+    (dict(spans=[(3, 0, 0)], cu=[0, 1], start=[2 ** 31 - 3]), "position"),
+    (dict(spans=[(2 ** 16, 1, 1)], cu=[0, 1], t_step=2 ** 16), "position"),
+    (dict(spans=[(3, 0, 0), (1, 2, 2)], cu=[0, 2], stride=6), "position_stride"),
+])
+def test_position_refusals(kw, needle):
+    st, msg = pos(**kw)
+    assert st == B.EPD_ERR_SHAPE and needle in msg, msg
+
+
+def test_position_arguments():
+    assert pos([(1, 0, 0)], [0, 1], positions=None)[0] == B.EPD_ERR_INVALID_ARG
+    assert pos([(1, 0, 0)], [0, 1], t_step=-1)[0] == B.EPD_ERR_INVALID_ARG
+    assert pos([], [0])[0] == B.EPD_OK and pos([(0, 0, 0)], [0, 0, 1])[0] == B.EPD_OK       # no tokens: nothing to launch
+    with pytest.raises(ValueError):
+        B.epd_rope_positions([(1, 0, 0)], [0, 2], None, 1, 0x1000, 64, 0)
