@@ -51,7 +51,11 @@ typedef enum {
 
 typedef enum { EPD_F32 = 0, EPD_BF16 = 1 } epd_dtype;
 typedef enum { EPD_LAYERNORM = 0, EPD_RMSNORM = 1 } epd_norm;
-typedef enum { EPD_GELU_ERF = 0, EPD_GELU_TANH = 1 } epd_act;
+typedef enum {
+  EPD_GELU_ERF = 0, EPD_GELU_TANH = 1,
+  /* gated: act(gate) * up, act = SiLU (x sigmoid(x)) or GELU; see epd_layer_weights.fc1_w */
+  EPD_SWIGLU = 2, EPD_GEGLU_ERF = 3, EPD_GEGLU_TANH = 4
+} epd_act;
 typedef enum { EPD_ROPE_NONE = 0, EPD_ROPE_2D = 2, EPD_ROPE_3D = 3 } epd_rope;
 
 /* Per-layer tensors: DEVICE pointers, element type = cfg.dtype. */
@@ -64,8 +68,8 @@ typedef struct {
   const void* proj_b;  /* [D] or NULL                                              */
   const void* norm2_g; /* [D]                                                      */
   const void* norm2_b; /* [D], NULL for RMSNorm                                    */
-  const void* fc1_w;   /* [F, D]                                                   */
-  const void* fc1_b;   /* [F] or NULL                                              */
+  const void* fc1_w;   /* [F, D]; gated activations: [2F, D], gate rows, then up rows */
+  const void* fc1_b;   /* [F] (gated: [2F]) or NULL                                */
   const void* fc2_w;   /* [D, F]                                                   */
   const void* fc2_b;   /* [D] or NULL                                              */
 } epd_layer_weights;
@@ -317,6 +321,54 @@ epd_status epd_rope_apply(const epd_rope_cfg* cfg, const epd_rope_tensor* tensor
 epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, int32_t num_sequences,
                               const int32_t* start, int32_t t_step, int32_t* positions,
                               int64_t position_stride, int32_t* next_out, void* stream);
+
+/* Gated MLP:  G | U = X Wgu^T (+ b),  H = act(G) * U,  Y = H Wd^T (+ b).  bf16 multiplies on the matrix cores with
+ * fp32 sums and rounds H and, in the backward pass, dG and dU to bf16; fp32 computes in fp32.  The encoder's own MLP takes the same weights (epd_layer_weights, act = EPD_SWIGLU ...). */
+typedef struct {
+  uint32_t struct_size; /* sizeof(epd_gated_mlp_cfg)                                                */
+  int32_t dtype;        /* epd_dtype of X, Y, weights, gradients                                    */
+  int32_t hidden;       /* D; bf16: a multiple of 8                                                 */
+  int32_t mlp_dim;      /* F; bf16: a multiple of 8; D * F < 2^30                                   */
+  int32_t act;          /* EPD_SWIGLU, EPD_GEGLU_ERF or EPD_GEGLU_TANH                              */
+  int32_t use_bias;     /* 1: both linears have a bias                                              */
+  int32_t max_tokens;   /* largest `tokens` of any call; < 2^22                                     */
+  int32_t training;     /* 1: the workspace also serves epd_gated_mlp_backward                      */
+} epd_gated_mlp_cfg;
+typedef struct {        /* device, dense; bf16: 16-byte aligned                                     */
+  const void* gate_up_w; /* [2F, D]: gate rows, then up rows                                        */
+  const void* gate_up_b; /* [2F], ignored when use_bias == 0                                        */
+  const void* down_w;    /* [D, F]                                                                  */
+  const void* down_b;    /* [D], ignored when use_bias == 0                                         */
+} epd_gated_mlp_weights;
+typedef struct {        /* device, cfg.dtype; NULL = not wanted; written, not added to              */
+  void* dx;             /* [tokens, D], rows ld_dx apart                                            */
+  int64_t ld_dx;
+  void* gate_up_w;      /* [2F, D]                                                                  */
+  void* gate_up_b;      /* [2F]                                                                     */
+  void* down_w;         /* [D, F]                                                                   */
+  void* down_b;         /* [D]                                                                      */
+} epd_gated_mlp_grads;
+
+/* Bytes of device workspace (256-byte aligned) that a call with `cfg` needs; 0 when cfg is invalid. */
+uint64_t epd_gated_mlp_workspace_bytes(const epd_gated_mlp_cfg* cfg);
+
+/* Y = MLP(X).
+ *   x, y    device [tokens, D], rows ld_x / ld_y >= D elements apart (bf16: multiples of 8, 16-byte aligned); y may
+ *           be x (with the same rows)
+ *   tokens  0 .. max_tokens; 0 launches nothing
+ *   saved   device fp32 [tokens, 2F] (either dtype) or NULL: receives G | U for epd_gated_mlp_backward
+ * Nothing in the workspace is kept from one call to the next. */
+epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weights* weights, const void* x,
+                         int64_t ld_x, int32_t tokens, void* y, int64_t ld_y, void* saved, void* workspace,
+                         uint64_t workspace_bytes, void* stream);
+
+/* Gradients of sum(Y * dY): those of `grads` that are not NULL.  x, weights and tokens as in the forward call that
+ * wrote `saved`; dx may be dy (with the same rows) where no gradient of down_w or down_b is wanted, and must not overlap
+ * x.  tokens = 0 clears the gradients of the weights. */
+epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weights* weights,
+                                  const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, int32_t tokens,
+                                  const void* saved, const epd_gated_mlp_grads* grads, void* workspace,
+                                  uint64_t workspace_bytes, void* stream);
 
 /* Release host-side state (events, pinned staging).  The workspace stays the caller's. */
 epd_status epd_encode_destroy(epd_handle h);

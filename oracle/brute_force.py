@@ -44,7 +44,9 @@ def _norm(cfg, x, g, b):
 
 
 def _act(cfg, v):
-    if cfg.act == "gelu_erf":
+    if cfg.act == "swiglu":
+        return v / (1.0 + math.exp(-v)) if v >= 0.0 else v * math.exp(v) / (1.0 + math.exp(v))
+    if cfg.act in ("gelu_erf", "geglu_erf"):
         return 0.5 * v * (1.0 + math.erf(v / math.sqrt(2.0)))
     return 0.5 * v * (1.0 + math.tanh(math.sqrt(2.0 / math.pi) * (v + 0.044715 * v * v * v)))
 
@@ -136,7 +138,12 @@ def encode(cfg, gw, layers, patches, cu_seqlens, grid_thw, coord_offset=(0, 0, 0
             flat = [o[i][h][c] for h in range(H) for c in range(d)]
             upd = _affine(flat, proj_w, proj_b)
             x[i] = [x[i][c] + upd[c] for c in range(D)]
-            hid = [_act(cfg, u) for u in _affine(_norm(cfg, x[i], n2g, n2b), f1w, f1b)]
+            hid = _affine(_norm(cfg, x[i], n2g, n2b), f1w, f1b)
+            if cfg.act in ("swiglu", "geglu_erf", "geglu_tanh"):      # gate rows, then up rows
+                f = len(hid) // 2
+                hid = [_act(cfg, hid[j]) * hid[f + j] for j in range(f)]
+            else:
+                hid = [_act(cfg, u) for u in hid]
             upd = _affine(hid, f2w, f2b)
             x[i] = [x[i][c] + upd[c] for c in range(D)]
     if cfg.final_norm:

@@ -24,7 +24,8 @@ anywhere in the paper: end-to-end parity is pinned only through those parts and 
 agreement of the two independently written paths.
 
 ``cfg`` is any object with the attributes: num_layers, hidden, num_heads, head_dim, mlp_dim,
-norm ("layernorm" | "rmsnorm"), norm_eps, act ("gelu_erf" | "gelu_tanh"), rope ("none" |
+norm ("layernorm" | "rmsnorm"), norm_eps, act ("gelu_erf" | "gelu_tanh"; gated, with fc1_w [2 * mlp_dim, hidden]:
+"swiglu" | "geglu_erf" | "geglu_tanh"), rope ("none" |
 "2d" | "3d"), rope_pairs (nt, nh, nw), rope_base, final_norm, merge.
 """
 
@@ -94,7 +95,18 @@ def gelu_tanh(x):
     return 0.5 * x * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (x + 0.044715 * x ** 3)))
 
 
+def gated_activation(cfg, x):
+    """act(gate) * up: the columns of x are the gate half, then the up half."""
+    f = x.shape[-1] // 2
+    gate, up = np.asarray(x, F64)[..., :f], np.asarray(x, F64)[..., f:]
+    if cfg.act == "swiglu":
+        return gate / (1.0 + np.exp(-gate)) * up
+    return (gelu_erf(gate) if cfg.act == "geglu_erf" else gelu_tanh(gate)) * up
+
+
 def activation(cfg, x):
+    if cfg.act in ("swiglu", "geglu_erf", "geglu_tanh"):
+        return gated_activation(cfg, x)
     return gelu_erf(x) if cfg.act == "gelu_erf" else gelu_tanh(x)
 
 

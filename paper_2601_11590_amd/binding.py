@@ -21,7 +21,9 @@ EPD_OK, EPD_ERR_INVALID_ARG, EPD_ERR_UNSUPPORTED, EPD_ERR_SHAPE, EPD_ERR_WORKSPA
 EPD_MISS = 1
 EPD_F32, EPD_BF16 = 0, 1
 EPD_LAYERNORM, EPD_RMSNORM = 0, 1
-EPD_GELU_ERF, EPD_GELU_TANH = 0, 1
+EPD_GELU_ERF, EPD_GELU_TANH, EPD_SWIGLU, EPD_GEGLU_ERF, EPD_GEGLU_TANH = 0, 1, 2, 3, 4
+_GATED = {"swiglu": EPD_SWIGLU, "geglu_erf": EPD_GEGLU_ERF, "geglu_tanh": EPD_GEGLU_TANH}
+_ACTS = {"gelu_erf": EPD_GELU_ERF, "gelu_tanh": EPD_GELU_TANH, **_GATED}
 EPD_ROPE_NONE, EPD_ROPE_2D, EPD_ROPE_3D = 0, 2, 3
 EPD_ROPE_SECTIONS, EPD_ROPE_INTERLEAVED = 0, 1
 EPD_ROPE_LADDER_AXIS, EPD_ROPE_LADDER_HEAD = 0, 1
@@ -69,12 +71,29 @@ class epd_rope_tensor(C.Structure):
                 ("out_token", C.c_int64), ("out_head", C.c_int64), ("heads", C.c_int32)]
 
 
+class epd_gated_mlp_cfg(C.Structure):
+    _fields_ = [(n, C.c_uint32 if n == "struct_size" else C.c_int32)
+                for n in ("struct_size", "dtype", "hidden", "mlp_dim", "act", "use_bias", "max_tokens", "training")]
+
+
+_GATED_FIELDS = ["gate_up_w", "gate_up_b", "down_w", "down_b"]
+
+
+class epd_gated_mlp_weights(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in _GATED_FIELDS]
+
+
+class epd_gated_mlp_grads(C.Structure):
+    _fields_ = [("dx", C.c_void_p), ("ld_dx", C.c_int64)] + [(n, C.c_void_p) for n in _GATED_FIELDS]
+
+
 EXPORTS = ["epd_encode_workspace_bytes", "epd_encode_create", "epd_encode", "epd_encode_destroy",
            "epd_encode_last_error", "epd_encode_debug_hidden", "epd_encode_set_timing", "epd_encode_set_tuning", "epd_encode_set_compute_units",
            "epd_encode_get_timing", "epd_preprocess", "epd_encode_cached", "epd_store_create",
            "epd_store_destroy", "epd_store_last_error", "epd_store_hash", "epd_store_hash_noalloc", "epd_store_lookup", "epd_store_insert",
            "epd_store_stats", "epd_probe_stream_read", "epd_probe_mfma_rate", "epd_probe_gemm_plan"]
-OPERATOR_EXPORTS = ["epd_op_last_error", "epd_rope_apply", "epd_rope_positions"]    # the operators beside the encoder
+OPERATOR_EXPORTS = ["epd_op_last_error", "epd_rope_apply", "epd_rope_positions", "epd_gated_mlp_workspace_bytes", "epd_gated_mlp",
+                    "epd_gated_mlp_backward"]    # the operators beside the encoder
 
 
 def _load() -> C.CDLL:
@@ -138,6 +157,14 @@ def _load() -> C.CDLL:
     lib.epd_rope_positions.restype = C.c_int
     lib.epd_rope_positions.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64,
                                        C.c_void_p, C.c_void_p]
+    lib.epd_gated_mlp_workspace_bytes.restype = C.c_uint64
+    lib.epd_gated_mlp_workspace_bytes.argtypes = [C.POINTER(epd_gated_mlp_cfg)]
+    lib.epd_gated_mlp.restype = C.c_int
+    lib.epd_gated_mlp.argtypes = [C.POINTER(epd_gated_mlp_cfg), C.POINTER(epd_gated_mlp_weights), C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
+                                  C.c_int64, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
+    lib.epd_gated_mlp_backward.restype = C.c_int
+    lib.epd_gated_mlp_backward.argtypes = [C.POINTER(epd_gated_mlp_cfg), C.POINTER(epd_gated_mlp_weights), C.c_void_p, C.c_int64, C.c_void_p,
+                                           C.c_int64, C.c_int32, C.c_void_p, C.POINTER(epd_gated_mlp_grads), C.c_void_p, C.c_uint64, C.c_void_p]
     return lib
 
 
@@ -352,7 +379,7 @@ def make_cfg(cfg, max_tokens: int, max_segments: int, max_items: int) -> epd_enc
     c.mlp_dim, c.in_channels, c.patch, c.temporal_patch = cfg.mlp_dim, cfg.in_channels, cfg.patch, cfg.temporal_patch
     c.norm = {"layernorm": EPD_LAYERNORM, "rmsnorm": EPD_RMSNORM}[cfg.norm]
     c.norm_eps = cfg.norm_eps
-    c.act = {"gelu_erf": EPD_GELU_ERF, "gelu_tanh": EPD_GELU_TANH}[cfg.act]
+    c.act = _ACTS[cfg.act]
     c.use_bias = 1 if cfg.use_bias else 0
     c.rope = {"none": EPD_ROPE_NONE, "2d": EPD_ROPE_2D, "3d": EPD_ROPE_3D}[cfg.rope]
     c.rope_base = cfg.rope_base
@@ -654,6 +681,100 @@ class Rope:
         with _on(positions.device) as stream:
             epd_rope_apply(self.cfg, arr, positions.data_ptr() or 256, positions.stride(0), T, inverse, stream)
         return list(out)
+
+
+def epd_gated_mlp_workspace_bytes(cfg: epd_gated_mlp_cfg) -> int:
+    return int(lib.epd_gated_mlp_workspace_bytes(C.byref(cfg)))
+
+
+def epd_gated_mlp(cfg: epd_gated_mlp_cfg, weights: epd_gated_mlp_weights, x: int, ld_x: int, tokens: int, y: int, ld_y: int,
+                  saved: Optional[int], workspace: int, workspace_bytes: int, stream: int) -> None:
+    _op_check(lib.epd_gated_mlp(C.byref(cfg), C.byref(weights), x, ld_x, tokens, y, ld_y, saved, workspace, workspace_bytes, stream))
+
+
+def epd_gated_mlp_backward(cfg: epd_gated_mlp_cfg, weights: epd_gated_mlp_weights, x: int, ld_x: int, dy: int, ld_dy: int, tokens: int,
+                           saved: int, grads: epd_gated_mlp_grads, workspace: int, workspace_bytes: int, stream: int) -> None:
+    _op_check(lib.epd_gated_mlp_backward(C.byref(cfg), C.byref(weights), x, ld_x, dy, ld_dy, tokens, saved, C.byref(grads), workspace,
+                                         workspace_bytes, stream))
+
+
+class GatedMLP:
+    """Y = (act(X Wg^T) * (X Wu^T)) Wd^T with optional biases, and its backward pass.  Owns the workspace of its calls, so one call at
+    a time: calls on other streams have to be ordered by the caller, as do replays of graphs that captured calls of one object.
+    Weights are passed with every call, as a dict of gate_up_w [2F, D] (gate rows, then up rows), down_w [D, F] and, with biases,
+    gate_up_b [2F], down_b [D]."""
+
+    def __init__(self, dtype: str, hidden: int, mlp_dim: int, act: str = "swiglu", max_tokens: int = 1, use_bias: bool = False,
+                 training: bool = False, device: str = "cuda:0"):
+        c = self.cfg = epd_gated_mlp_cfg()
+        c.struct_size = C.sizeof(epd_gated_mlp_cfg)
+        c.dtype, c.act = {"f32": EPD_F32, "bf16": EPD_BF16}[dtype], _GATED[act]
+        c.hidden, c.mlp_dim, c.max_tokens, c.use_bias, c.training = hidden, mlp_dim, max_tokens, int(use_bias), int(training)
+        self.hidden, self.mlp_dim, self.dtype = hidden, mlp_dim, torch_dtype(dtype)
+        self.workspace_bytes = epd_gated_mlp_workspace_bytes(c)
+        if self.workspace_bytes == 0:
+            raise EpdError(EPD_ERR_INVALID_ARG, epd_op_last_error())
+        dev = torch.device(device)
+        self.device = torch.device(dev.type, torch.cuda.current_device()) if dev.index is None else dev
+        self.workspace = torch.empty(self.workspace_bytes + 256, dtype=torch.uint8, device=self.device)
+        self._base = (self.workspace.data_ptr() + 255) // 256 * 256
+        self._stream = torch.cuda.current_stream(self.device).cuda_stream
+        self._shapes = {"gate_up_w": (2 * mlp_dim, hidden), "down_w": (hidden, mlp_dim)}
+        if use_bias:
+            self._shapes.update(gate_up_b=(2 * mlp_dim,), down_b=(hidden,))
+
+    def _weights(self, weights) -> epd_gated_mlp_weights:
+        w = epd_gated_mlp_weights()
+        for n, shape in self._shapes.items():
+            t = weights[n]
+            if t.shape != shape or t.dtype != self.dtype or t.device != self.device or not t.is_contiguous():
+                raise ValueError("%s must be a contiguous %s %s on %s" % (n, list(shape), self.dtype, self.device))
+            setattr(w, n, t.data_ptr())
+        return w
+
+    def _rows(self, t: torch.Tensor, name: str, tokens: Optional[int] = None) -> torch.Tensor:
+        if t.dim() != 2 or t.shape[1] != self.hidden or t.dtype != self.dtype or t.device != self.device or (t.stride(1) != 1 and t.numel()) or (tokens is not None and t.shape[0] != tokens):
+            raise ValueError("%s must be [tokens, %d] of %s on %s with contiguous rows" % (name, self.hidden, self.dtype, self.device))
+        return t
+
+    @staticmethod
+    def _ld(t: torch.Tensor) -> int:
+        return max(t.stride(0), t.shape[1]) if t.shape[0] < 2 else t.stride(0)      # one row: its stride means nothing
+
+    def _used_on(self, stream: int) -> None:
+        if stream != self._stream:            # the allocator may not hand the workspace on before this stream is through
+            self.workspace.record_stream(torch.cuda.current_stream(self.device))
+
+    def forward(self, weights, x: torch.Tensor, save: bool = False, out: Optional[torch.Tensor] = None):
+        """x: [tokens, D], rows any stride apart.  Returns y, or (y, saved) with what ``backward`` needs."""
+        T = self._rows(x, "x").shape[0]
+        w = self._weights(weights)
+        y = torch.empty((T, self.hidden), dtype=self.dtype, device=self.device) if out is None else self._rows(out, "out", T)
+        saved = torch.empty((T, 2 * self.mlp_dim), dtype=torch.float32, device=self.device) if save else None
+        with _on(self.device) as stream:
+            self._used_on(stream)
+            epd_gated_mlp(self.cfg, w, x.data_ptr(), self._ld(x), T, y.data_ptr(), self._ld(y), None if saved is None else saved.data_ptr(),
+                          self._base, self.workspace_bytes, stream)
+        return (y, saved) if save else y
+
+    def backward(self, weights, x: torch.Tensor, dy: torch.Tensor, saved: torch.Tensor, want: Optional[Sequence[str]] = None) -> Dict[str, torch.Tensor]:
+        """Gradients of sum(y * dy) by x ("dx") and by the weights; ``want`` names those to compute (all)."""
+        T = self._rows(x, "x").shape[0]
+        self._rows(dy, "dy", T)
+        if saved.shape != (T, 2 * self.mlp_dim) or saved.dtype != torch.float32 or saved.device != self.device or not saved.is_contiguous():
+            raise ValueError("saved must be what forward returned for these rows")
+        shapes = {"dx": (T, self.hidden), **self._shapes}
+        grads, out = epd_gated_mlp_grads(), {}
+        for n in (shapes if want is None else want):
+            out[n] = torch.empty(shapes[n], dtype=self.dtype, device=self.device)
+            setattr(grads, n, out[n].data_ptr())
+        grads.ld_dx = self.hidden
+        w = self._weights(weights)
+        with _on(self.device) as stream:
+            self._used_on(stream)
+            epd_gated_mlp_backward(self.cfg, w, x.data_ptr(), self._ld(x), dy.data_ptr(), self._ld(dy), T, saved.data_ptr(), grads, self._base,
+                                   self.workspace_bytes, stream)
+        return out
 
 
 EPI_STORE, EPI_GELU, EPI_RESIDUAL, EPI_QKV = 0, 1, 2, 3

@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libepd_encode.so")
 STAMP = LIB + ".hash"         # source_hash() of the sources LIB was built from
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["epd_api.hip", "plan_norm.hip", "preprocess.hip", "mm_store.hip", "probe.hip", "kernels_f32.hip", "gemm_bf16.hip", "attn_bf16.hip",
-           "rope.hip"]
+           "rope.hip", "gated_mlp.hip"]
 
 # packed fp32 instructions are switched off for every kernel (hipcc -O3 would otherwise form
 # them from ordinary float code)
@@ -86,7 +86,7 @@ def build(verbose: bool = False, extra_flags=()) -> str:
     # compiler moved no register while a read into it was pending (see check_lds_waits.py)
     from . import check_lds_waits
     check_lds_waits.check_sources(hipcc, [*FLAGS, *extra_flags],
-                                  [os.path.join(CSRC, s) for s in ("gemm_bf16.hip", "attn_bf16.hip")])
+                                  [os.path.join(CSRC, s) for s in ("gemm_bf16.hip", "gated_mlp.hip", "attn_bf16.hip")])
     out = _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
     if verbose and out.strip():
         print(out)

@@ -53,6 +53,8 @@ struct Layout {
 
 constexpr size_t kAbsent = (size_t)-1;
 
+bool gated(const epd_encode_cfg& c) { return c.act >= EPD_SWIGLU; }
+
 int q_tile(const epd_encode_cfg& c, int max_seg_len) { return attn_q_tile(c.dtype == EPD_BF16, c.head_dim, max_seg_len); }
 
 Layout make_layout(const epd_encode_cfg& c) {
@@ -71,6 +73,7 @@ Layout make_layout(const epd_encode_cfg& c) {
   L.fpad = bf ? (int)align_up((size_t)c.mlp_dim, 64) : c.mlp_dim;
   L.vt_stride = (int)align_up((size_t)c.max_tokens + (size_t)c.max_segments * kVtAlign, kVtAlign);
   const bool ln = c.norm == EPD_LAYERNORM, bias = c.use_bias != 0;
+  const size_t F1 = gated(c) ? 2 * F : F;     // rows of fc1
   size_t off = 0;
   auto take = [&](size_t bytes, bool present = true) {
     if (!present) return kAbsent;
@@ -94,8 +97,8 @@ Layout make_layout(const epd_encode_cfg& c) {
     w.proj_b = take(D * es, bias);
     w.norm2_g = take(D * es);
     w.norm2_b = take(D * es, ln);
-    w.fc1_w = take(F * D * es);
-    w.fc1_b = take(F * es, bias);
+    w.fc1_w = take(F1 * D * es);
+    w.fc1_b = take(F1 * es, bias);
     w.fc2_w = take(D * (size_t)L.fpad * es);
     w.fc2_b = take(D * es, bias);
   }
@@ -139,7 +142,7 @@ epd_status validate_cfg(const epd_encode_cfg* c, bool need_buffers, std::string&
   }
   if (c->dtype != EPD_F32 && c->dtype != EPD_BF16) { err = "cfg.dtype invalid"; return EPD_ERR_INVALID_ARG; }
   if (c->norm != EPD_LAYERNORM && c->norm != EPD_RMSNORM) { err = "cfg.norm invalid"; return EPD_ERR_INVALID_ARG; }
-  if (c->act != EPD_GELU_ERF && c->act != EPD_GELU_TANH) { err = "cfg.act invalid"; return EPD_ERR_INVALID_ARG; }
+  if (c->act < EPD_GELU_ERF || c->act > EPD_GEGLU_TANH) { err = "cfg.act invalid"; return EPD_ERR_INVALID_ARG; }
   if (c->rope != EPD_ROPE_NONE && c->rope != EPD_ROPE_2D && c->rope != EPD_ROPE_3D) {
     err = "cfg.rope invalid"; return EPD_ERR_INVALID_ARG;
   }
@@ -323,7 +326,7 @@ epd_status epd_encode_create(const epd_encode_cfg* cfg, epd_handle* out) {
   };
   const Layout& L = h->L;
   const epd_weights& w = *cfg->weights;
-  const size_t es = L.es, D = cfg->hidden, F = cfg->mlp_dim;
+  const size_t es = L.es, D = cfg->hidden, F = cfg->mlp_dim, F1 = gated(*cfg) ? 2 * F : F;
 #define EPD_CW(dst, src, bytes)                                         \
   do {                                                                  \
     epd_status s_ = copy_weight(h, dst, src, bytes);                    \
@@ -347,8 +350,8 @@ epd_status epd_encode_create(const epd_encode_cfg* cfg, epd_handle* out) {
     EPD_CW(d.proj_b, s.proj_b, D * es);
     EPD_CW(d.norm2_g, s.norm2_g, D * es);
     EPD_CW(d.norm2_b, s.norm2_b, D * es);
-    EPD_CW(d.fc1_w, s.fc1_w, F * D * es);
-    EPD_CW(d.fc1_b, s.fc1_b, F * es);
+    EPD_CW(d.fc1_w, s.fc1_w, F1 * D * es);
+    EPD_CW(d.fc1_b, s.fc1_b, F1 * es);
     if (L.fpad == (int)F) {
       EPD_CW(d.fc2_w, s.fc2_w, D * F * es);
     } else {   // rows of mlp_dim elements into rows of fpad, the pad cleared
@@ -363,7 +366,7 @@ epd_status epd_encode_create(const epd_encode_cfg* cfg, epd_handle* out) {
     if (L.fold_rms) {
       // norm2 -> fc1 in every block; norm1 -> qkv from the second block on (the first block's
       // norm1 follows the patch embedding and runs as a kernel)
-      launch_fold_gamma(h->ws + d.fc1_w, h->ws + d.norm2_g, (int)F, (int)D, 0);
+      launch_fold_gamma(h->ws + d.fc1_w, h->ws + d.norm2_g, (int)F1, (int)D, 0);
       if (l > 0) launch_fold_gamma(h->ws + d.qkv_w, h->ws + d.norm1_g, 3 * (int)D, (int)D, 0);
     }
   }
@@ -504,14 +507,16 @@ epd_status epd_encode(epd_handle h, const void* packed_patches, const int32_t* c
   }
 
   auto gemm = [&](int step, GemmArgs& g, int k_counted = 0) {   // k_counted: K without padding
-    StepTimer tm(h, step, 2.0 * g.M * (double)g.N * (k_counted ? k_counted : g.K), st);
+    StepTimer tm(h, step, 2.0 * g.M * (double)(g.epilogue == EPI_GATED ? 2 * g.gate_rows : g.N) * (k_counted ? k_counted : g.K), st);
     g.zeros = h->ws + L.zeros;
     // operands that live in the workspace -- all but the caller's patches -- may be read past their last row (see make_layout)
     g.overread_a = g.A != packed_patches;
     g.overread_w = 1;
     g.tile_cfg = h->tile_cfg;
     g.compute_units = h->compute_units;
-    if (bf) launch_gemm_bf16(g, st); else launch_gemm_f32(g, st);
+    if (!bf) launch_gemm_f32(g, st);
+    else if (g.epilogue == EPI_GATED) launch_gemm_bf16_gated(g, st);
+    else launch_gemm_bf16(g, st);
   };
   auto norm = [&](const void* gma, const void* bta, void* dst) {
     StepTimer tm(h, EPD_STEP_NORM, (double)T * D * (4.0 + L.es), st);
@@ -565,11 +570,15 @@ epd_status epd_encode(epd_handle h, const void* packed_patches, const int32_t* c
       gemm(EPD_STEP_PROJ, g);
     }
     if (!L.fold_rms) norm(h->at<void>(w.norm2_g), h->at<void>(w.norm2_b), Xn);
-    {  // Hd = GELU(Xn W1^T + b1)
+    {  // Hd = GELU(Xn W1^T + b1), or act(Xn Wg^T + bg) * (Xn Wu^T + bu)
       GemmArgs g{};
       if (L.fold_rms) consume_stats(g);
       g.A = Xn; g.lda = D; g.W = h->at<void>(w.fc1_w); g.bias = h->at<void>(w.fc1_b);
       g.M = T; g.N = F; g.K = D; g.epilogue = EPI_GELU; g.act = c.act; g.out = Hd; g.ldo = L.fpad;
+      if (gated(c)) {
+        g.epilogue = EPI_GATED; g.gate_rows = F; g.N = bf ? (int)align_up((size_t)F, 16) * 2 : 2 * F;
+        g.act = c.act == EPD_SWIGLU ? 2 : c.act == EPD_GEGLU_TANH ? 1 : 0;
+      }
       gemm(EPD_STEP_FC1, g);
     }
     {  // X += Hd W2^T + b2

@@ -14,9 +14,14 @@ enum Epilogue : int {
   EPI_STORE = 0,     // out[m][n] = acc + bias               (out dtype: see out_f32)
   EPI_GELU = 1,      // out[m][n] = act(acc + bias)
   EPI_RESIDUAL = 2,  // resid[m][n] += acc + bias            (fp32 residual stream, in place)
-  EPI_QKV = 3        // columns < qk_cols: rotate adjacent pairs by rot[m][.], store to out;
+  EPI_QKV = 3,       // columns < qk_cols: rotate adjacent pairs by rot[m][.], store to out;
                      // columns >= qk_cols: V.  fp32 path stores V to out as well; the bf16
                      // path stores V transposed into vt[(n - qk_cols)][vcol[m]].
+  EPI_GATED = 4,     // W holds gate_rows gate rows, then as many up rows:
+                     // out[m][c] = act(gate_c + bias_c) * (up_c + bias_(gate_rows + c));  bf16: N = 2 *
+                     // round_up(gate_rows, 16), fp32: N = 2 * gate_rows.  gu (if any) gets both factors
+  EPI_DGATED = 5     // acc = dH[m][c], N = gate_rows; from gu's G and U: dgu[m][c] = dH U act'(G),
+                     // dgu[m][gate_rows + c] = dH act(G), out[m][c] = act(G) U
 };
 
 struct GemmArgs {
@@ -29,7 +34,7 @@ struct GemmArgs {
   const void* bias;     // [N] or nullptr
   int M, N, K;
   int epilogue;         // Epilogue
-  int act;              // 0 = GELU erf, 1 = GELU tanh (EPI_GELU)
+  int act;              // 0 = GELU erf, 1 = GELU tanh (EPI_GELU, EPI_GATED, EPI_DGATED), 2 = SiLU (the gated ones)
   void* out;            // [M, ldo]
   int ldo;
   int out_f32;          // bf16 path only: 1 = out is fp32 (patch embed writes the residual stream)
@@ -65,6 +70,12 @@ struct GemmArgs {
   int group_m;          // bf16 path: row tiles per rasterisation group (set by the launcher)
   int rot_lds;          // bf16 path, EPI_QKV: 1 = the rotary table comes through LDS where it fits (set by the launcher)
   int compute_units;    // bf16 path: compute units the launch will run on (a CU-masked stream); 0 = all of the device's
+  // EPI_GATED, EPI_DGATED
+  int gate_rows;        // channels c; bf16: a multiple of 8
+  void* gu;             // fp32 [M, ldgu]: pre-activations, G in columns [0, gate_rows), U behind it (EPI_GATED: written, or nullptr)
+  int ldgu;
+  void* dgu;            // [M, lddgu] (EPI_DGATED)
+  int lddgu;
   int name_tag;         // bf16 path, EPI_RESIDUAL: 1 = the second MLP GEMM (a kernel name of its own in
                         //   profiles; the code is the same)
 };
@@ -140,6 +151,7 @@ void launch_norm(const float* x, const void* gamma, const void* beta, void* out,
 void launch_gemm_f32(const GemmArgs& g, hipStream_t s);
 bool launch_attn_f32(const AttnArgs& a, hipStream_t s);   // false: head_dim not covered
 void launch_gemm_bf16(const GemmArgs& g, hipStream_t s);
+void launch_gemm_bf16_gated(const GemmArgs& g, hipStream_t s);   // EPI_STORE (bf16 out), EPI_GATED, EPI_DGATED; zeros, overread_* are not used
 // How launch_gemm_bf16 would tile g on a chip of compute_units units (<= 0: the current device's;
 // host only, launches nothing): the tile of the first or only launch, and the rows that launch
 // covers when the rest is left to a second launch of smaller tiles (0 = one launch covers all).

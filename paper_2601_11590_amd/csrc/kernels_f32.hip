@@ -25,11 +25,29 @@ __device__ __forceinline__ float gelu_f32(float v, int act) {
   return 0.5f * v * (1.0f + tanhf(u));
 }
 
+// Gate of a gated MLP: act(g), and its derivative d (see gate_act_d of the bf16 kernels for the formulas).
+__device__ __forceinline__ float gate_f32(float g, int act, float& d) {
+  if (act == 0) {
+    const float cdf = 0.5f * (1.0f + erff(g * 0.70710678118654752440f));
+    d = cdf + g * 0.39894228040143267794f * expf(-0.5f * g * g);
+    return g * cdf;
+  }
+  if (act == 1) {
+    const float z = fminf(g * g, 1e30f), u = 0.79788456080286535588f * (g + 0.044715f * z * g), t = tanhf(u);
+    d = 0.5f * (1.0f + t) + 0.5f * g * (1.0f - t * t) * 0.79788456080286535588f * (1.0f + 3.0f * 0.044715f * z);
+    return 0.5f * g * (1.0f + t);
+  }
+  const float p = 1.0f / (1.0f + expf(-g));
+  d = p * (1.0f + g * (1.0f - p));
+  return g * p;
+}
+
 // A block of NW waves.  SPLIT: all of them share one 16 T x 16 T tile and take its K in turn, 32 at a
 // time, and their sums meet in LDS; otherwise NW = 4 and each has a tile of its own, 2 x 2.
+// GATE: EPI_GATED (column 2 c of the product is channel c's gate, 2 c + 1 its up factor) or EPI_DGATED.
 // VEC: rows start 16-byte aligned and K (and a gathered piece) is a multiple of 4; otherwise 16-byte
 // loads from any float's address, and the last of a row taken apart.
-template <int T, int NW, bool SPLIT, bool VEC>
+template <int T, int NW, bool SPLIT, bool VEC, bool GATE = false>
 __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
   constexpr int WT = 16 * T, BT = SPLIT ? WT : 2 * WT;       // wave and block tile
   constexpr int LD = BT + 4, COPIES = SPLIT ? NW : 1;
@@ -49,7 +67,9 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
   for (int t = 0; t < T; ++t) {                              // rows beyond the matrix repeat the last one: never stored
     am[t] = min(m0 + wm + t * 16 + l16, g.M - 1);
     arow[t] = A + (size_t)am[t] * g.lda;
-    wrow[t] = W + (size_t)min(n0 + wn + t * 16 + l16, g.N - 1) * g.K;
+    int n = min(n0 + wn + t * 16 + l16, g.N - 1);
+    if (GATE && g.epilogue == EPI_GATED) n = (n >> 1) + (n & 1) * g.gate_rows;
+    wrow[t] = W + (size_t)n * g.K;
   }
   auto load4 = [&](const float* row, int k) {                // row[k .. k + 3], zero from K on
     if constexpr (VEC) {
@@ -140,6 +160,28 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
 #pragma unroll
     for (int w = 1; w < COPIES; ++w) v += *(const f32x4*)&acc_lds[w][r][c];
     const int left = min(4, g.N - n);
+    if constexpr (GATE) {
+      float* const gu = (float*)g.gu + (size_t)m * g.ldgu;
+      if (g.epilogue == EPI_GATED) {
+        for (int j = 0; j < left; j += 2) {
+          const int ch = (n + j) >> 1;
+          const float gate = v[j] + (bias ? bias[ch] : 0.f), up = v[j + 1] + (bias ? bias[g.gate_rows + ch] : 0.f);
+          float d;
+          out[(size_t)m * g.ldo + ch] = gate_f32(gate, g.act, d) * up;
+          if (g.gu) { gu[ch] = gate; gu[g.gate_rows + ch] = up; }
+        }
+      } else {
+        float* const dgu = (float*)g.dgu + (size_t)m * g.lddgu;
+        for (int j = 0; j < left; ++j) {
+          float d;
+          const float up = gu[g.gate_rows + n + j], a = gate_f32(gu[n + j], g.act, d);
+          dgu[n + j] = v[j] * up * d;
+          dgu[g.gate_rows + n + j] = v[j] * a;
+          out[(size_t)m * g.ldo + n + j] = a * up;
+        }
+      }
+      continue;
+    }
     if (bias)
       for (int j = 0; j < left; ++j) v[j] += bias[n + j];
     if (g.epilogue == EPI_QKV && g.rot) {
@@ -172,7 +214,10 @@ template <int T, int NW, bool SPLIT> static void launch_tile_f32(const GemmArgs&
   const dim3 grid((g.N + BT - 1) / BT, (g.M + BT - 1) / BT);
   const int piece = g.gather ? g.K / g.gather_n : g.K;
   const bool vec = piece % 4 == 0 && g.lda % 4 == 0 && (((size_t)g.A | (size_t)g.W) & 15) == 0;
-  if (vec) hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, true>), grid, dim3(64 * NW), 0, s, g);
+  if (g.epilogue == EPI_GATED || g.epilogue == EPI_DGATED) {
+    if (vec) hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, true, true>), grid, dim3(64 * NW), 0, s, g);
+    else hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, false, true>), grid, dim3(64 * NW), 0, s, g);
+  } else if (vec) hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, true>), grid, dim3(64 * NW), 0, s, g);
   else hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, false>), grid, dim3(64 * NW), 0, s, g);
 }
 

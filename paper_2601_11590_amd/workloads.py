@@ -28,6 +28,9 @@ _LAYER_TENSORS = ("norm1_g", "norm1_b", "qkv_w", "qkv_b", "proj_w", "proj_b",
                   "norm2_g", "norm2_b", "fc1_w", "fc1_b", "fc2_w", "fc2_b")
 
 
+GATED_ACTS = ("swiglu", "geglu_erf", "geglu_tanh")   # fc1 holds 2 * mlp_dim rows, H = act(gate) * up
+
+
 @dataclass(frozen=True)
 class EncoderConfig:
     """Static description of one encoder; field names follow the C-ABI config struct."""
@@ -46,7 +49,7 @@ class EncoderConfig:
     out_dim: int
     in_channels: int = 3
     norm_eps: float = 1e-6
-    act: str = "gelu_erf"      # "gelu_erf" | "gelu_tanh"
+    act: str = "gelu_erf"      # "gelu_erf" | "gelu_tanh" | one of GATED_ACTS
     use_bias: bool = True
     rope_base: float = 10000.0
     final_norm: bool = True
@@ -236,13 +239,14 @@ def packed_patches(cfg: EncoderConfig, grids: Sequence[Tuple[int, int, int]], se
 
 def _tensor_shape(cfg: EncoderConfig, name: str) -> Tuple[int, ...]:
     D, F = cfg.hidden, cfg.mlp_dim
+    F1 = 2 * F if cfg.act in GATED_ACTS else F      # rows of fc1: gate, then up
     return {
         "patch_w": (D, cfg.patch_dim), "patch_b": (D,),
         "final_norm_g": (D,), "final_norm_b": (D,),
         "merge_w": (cfg.out_dim, cfg.merge * cfg.merge * D), "merge_b": (cfg.out_dim,),
         "norm1_g": (D,), "norm1_b": (D,), "qkv_w": (3 * D, D), "qkv_b": (3 * D,),
         "proj_w": (D, D), "proj_b": (D,), "norm2_g": (D,), "norm2_b": (D,),
-        "fc1_w": (F, D), "fc1_b": (F,), "fc2_w": (D, F), "fc2_b": (D,),
+        "fc1_w": (F1, D), "fc1_b": (F1,), "fc2_w": (D, F), "fc2_b": (D,),
     }[name]
 
 

@@ -23,7 +23,8 @@ def test_every_declared_operator_is_exported():
 
 
 def test_structs_and_enums_match_the_header(tmp_path):
-    structs = {"epd_rope_cfg": B.epd_rope_cfg, "epd_rope_tensor": B.epd_rope_tensor}
+    structs = {"epd_rope_cfg": B.epd_rope_cfg, "epd_rope_tensor": B.epd_rope_tensor, "epd_gated_mlp_cfg": B.epd_gated_mlp_cfg,
+               "epd_gated_mlp_weights": B.epd_gated_mlp_weights, "epd_gated_mlp_grads": B.epd_gated_mlp_grads}
     lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "epd_encode.h"', "int main(void) {"]
     want = []
     for name, t in structs.items():
@@ -32,7 +33,8 @@ def test_structs_and_enums_match_the_header(tmp_path):
         for f, _ in t._fields_:
             lines.append('printf("%%zu\\n", offsetof(%s, %s));' % (name, {"input": "in", "output": "out"}.get(f, f)))
             want.append(getattr(t, f).offset)
-    for e in ("EPD_ROPE_SECTIONS", "EPD_ROPE_INTERLEAVED", "EPD_ROPE_LADDER_AXIS", "EPD_ROPE_LADDER_HEAD", "EPD_ROPE_HALF", "EPD_ROPE_ADJACENT"):
+    for e in ("EPD_ROPE_SECTIONS", "EPD_ROPE_INTERLEAVED", "EPD_ROPE_LADDER_AXIS", "EPD_ROPE_LADDER_HEAD", "EPD_ROPE_HALF", "EPD_ROPE_ADJACENT",
+              "EPD_SWIGLU", "EPD_GEGLU_ERF", "EPD_GEGLU_TANH"):
         lines.append('printf("%%d\\n", (int)%s);' % e)
         want.append(getattr(B, e))
     src = tmp_path / "probe.c"
@@ -143,3 +145,114 @@ def test_position_arguments():
     assert pos([], [0])[0] == B.EPD_OK and pos([(0, 0, 0)], [0, 0, 1])[0] == B.EPD_OK       # no tokens: nothing to launch
     with pytest.raises(ValueError):
         B.epd_rope_positions([(1, 0, 0)], [0, 2], None, 1, 0x1000, 64, 0)
+
+
+# ------------------------------------------------------------------ gated MLP
+
+def mlp_cfg(**change):
+    c = B.epd_gated_mlp_cfg()
+    base = dict(struct_size=C.sizeof(B.epd_gated_mlp_cfg), dtype=B.EPD_BF16, hidden=64, mlp_dim=128, act=B.EPD_SWIGLU, use_bias=1, max_tokens=100, training=1)
+    base.update(change)
+    for k, v in base.items():
+        setattr(c, k, v)
+    return c
+
+
+def mlp(backward=False, cfg=None, x=0x10000, ld_x=64, tokens=10, y=0x20000, ld_y=64, saved=0x30000, workspace=0x100000, size=1 << 40, weights=None, grads=None, **change):
+    c = mlp_cfg(**change) if cfg is None else cfg
+    w = B.epd_gated_mlp_weights(0x40000, 0x50000, 0x60000, 0x70000)
+    for k, v in (weights or {}).items():
+        setattr(w, k, v)
+    if backward:
+        g = B.epd_gated_mlp_grads(0x80000, 64, 0x90000, 0xA0000, 0xB0000, 0xC0000)
+        for k, v in (grads or {}).items():
+            setattr(g, k, v)
+        st = B.lib.epd_gated_mlp_backward(C.byref(c), C.byref(w), x, ld_x, y, ld_y, tokens, saved, C.byref(g), workspace, size, None)
+    else:
+        st = B.lib.epd_gated_mlp(C.byref(c), C.byref(w), x, ld_x, tokens, y, ld_y, saved, workspace, size, None)
+    return st, B.epd_op_last_error()
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("kw,status,needle", [
+    (dict(struct_size=8), B.EPD_ERR_INVALID_ARG, "struct_size"),
+    (dict(dtype=3), B.EPD_ERR_INVALID_ARG, "dtype"),
+    (dict(use_bias=2), B.EPD_ERR_INVALID_ARG, "use_bias"),
+    (dict(training=-1), B.EPD_ERR_INVALID_ARG, "training"),
+    (dict(act=B.EPD_GELU_ERF), B.EPD_ERR_INVALID_ARG, "gated"),
+    (dict(act=5), B.EPD_ERR_INVALID_ARG, "gated"),
+    (dict(hidden=0), B.EPD_ERR_INVALID_ARG, "positive"),
+    (dict(mlp_dim=-8), B.EPD_ERR_INVALID_ARG, "positive"),
+    (dict(max_tokens=0), B.EPD_ERR_INVALID_ARG, "positive"),
+    (dict(hidden=60), B.EPD_ERR_UNSUPPORTED, "multiples of 8"),
+    (dict(mlp_dim=4), B.EPD_ERR_UNSUPPORTED, "multiples of 8"),
+    (dict(hidden=65536, mlp_dim=16384), B.EPD_ERR_UNSUPPORTED, "2^30"),
+    (dict(mlp_dim=131080), B.EPD_ERR_UNSUPPORTED, "131072"),
+    (dict(max_tokens=1 << 22), B.EPD_ERR_UNSUPPORTED, "max_tokens"),
+    (dict(tokens=101), B.EPD_ERR_SHAPE, "tokens"),
+    (dict(tokens=-1), B.EPD_ERR_SHAPE, "tokens"),
+    (dict(weights=dict(gate_up_w=None)), B.EPD_ERR_INVALID_ARG, "NULL"),
+    (dict(weights=dict(down_w=None)), B.EPD_ERR_INVALID_ARG, "NULL"),
+    (dict(weights=dict(gate_up_b=None)), B.EPD_ERR_INVALID_ARG, "NULL"),
+    (dict(weights=dict(down_b=None)), B.EPD_ERR_INVALID_ARG, "NULL"),
+    (dict(weights=dict(down_w=0x60008)), B.EPD_ERR_UNSUPPORTED, "aligned"),
+    (dict(workspace=None), B.EPD_ERR_WORKSPACE, "workspace"),
+    (dict(workspace=0x100010), B.EPD_ERR_WORKSPACE, "aligned"),
+    (dict(size=1000), B.EPD_ERR_WORKSPACE, "required"),
+    (dict(x=None), B.EPD_ERR_INVALID_ARG, "x is NULL"),
+    (dict(y=None), B.EPD_ERR_INVALID_ARG, "NULL"),
+    (dict(x=0x10008), B.EPD_ERR_UNSUPPORTED, "16 bytes"),
+    (dict(ld_x=63), B.EPD_ERR_SHAPE, "rows of x"),
+    (dict(ld_x=68), B.EPD_ERR_UNSUPPORTED, "16 bytes"),
+    (dict(ld_y=1 << 22), B.EPD_ERR_SHAPE, "rows of"),
+    (dict(saved=0x30004), B.EPD_ERR_UNSUPPORTED, "saved"),
+    (dict(dtype=B.EPD_F32, x=0x10002), B.EPD_ERR_UNSUPPORTED, "4 (fp32)"),
+])
+def test_gated_mlp_refusals(backward, kw, status, needle):
+    st, msg = mlp(backward, **kw)
+    assert st == status and needle in msg, msg
+
+
+@pytest.mark.parametrize("kw,status,needle", [
+    (dict(training=0), B.EPD_ERR_INVALID_ARG, "training"),
+    (dict(saved=None), B.EPD_ERR_INVALID_ARG, "saved"),
+    (dict(use_bias=0), B.EPD_ERR_INVALID_ARG, "biases"),
+    (dict(grads=dict(dx=0x80008)), B.EPD_ERR_UNSUPPORTED, "dx"),
+    (dict(grads=dict(ld_dx=8)), B.EPD_ERR_SHAPE, "dx"),
+    (dict(grads=dict(down_w=0x80004)), B.EPD_ERR_UNSUPPORTED, "gradients"),
+])
+def test_gated_mlp_backward_refusals(kw, status, needle):
+    st, msg = mlp(True, **kw)
+    assert st == status and needle in msg, msg
+
+
+def test_gated_mlp_without_tokens_and_null_arguments():
+    assert mlp(tokens=0, x=None, y=None, saved=None)[0] == B.EPD_OK
+    st = B.lib.epd_gated_mlp(None, None, None, 0, 0, None, 0, None, None, 0, None)
+    assert st == B.EPD_ERR_INVALID_ARG
+    w = B.epd_gated_mlp_weights(0x40000, 0x50000, 0x60000, 0x70000)
+    st = B.lib.epd_gated_mlp_backward(C.byref(mlp_cfg()), C.byref(w), 0x1000, 64, 0x1000, 64, 4, 0x1000, None, 0x100000, 1 << 40, None)
+    assert st == B.EPD_ERR_INVALID_ARG and "grads" in B.epd_op_last_error()
+
+
+def test_gated_mlp_workspace():
+    assert B.epd_gated_mlp_workspace_bytes(mlp_cfg(hidden=60)) == 0
+    small = B.epd_gated_mlp_workspace_bytes(mlp_cfg(training=0))
+    assert small == 100 * 128 * 2 and small % 256 == 0
+    assert B.epd_gated_mlp_workspace_bytes(mlp_cfg(training=0, max_tokens=1, mlp_dim=8)) == 256
+    big = B.epd_gated_mlp_workspace_bytes(mlp_cfg(hidden=3200, mlp_dim=12800, max_tokens=32768))
+    assert 32768 * 12800 * 2 < big < 32768 * (12800 * 16 + 3200 * 8) + 3200 * 12800 * 8
+
+
+def test_encoder_takes_gated_activations_only_by_their_names():
+    from paper_2601_11590_amd import workloads as W
+    cfg = W.EncoderConfig(name="t", dtype="bf16", num_layers=1, hidden=64, num_heads=1, head_dim=64, mlp_dim=128, patch=4, temporal_patch=1, norm="rmsnorm",
+                          rope="2d", rope_pairs=(0, 16, 16), out_dim=64)
+    plain = B.epd_encode_workspace_bytes(B.make_cfg(cfg, 64, 4, 4))
+    for act in W.GATED_ACTS:
+        assert B.epd_encode_workspace_bytes(B.make_cfg(cfg.replace(act=act), 64, 4, 4)) == plain + 128 * 64 * 2 + 128 * 2     # the up rows and their biases
+    c = B.make_cfg(cfg, 64, 4, 4)
+    c.act = 5
+    assert B.epd_encode_workspace_bytes(c) == 0
+    with pytest.raises(KeyError):
+        B.make_cfg(cfg.replace(act="reglu"), 64, 4, 4)
