@@ -602,21 +602,18 @@ def epd_rope_positions(span_thw: np.ndarray, cu_spans: np.ndarray, start: Option
     return after
 
 
-class _on:
-    """Makes a tensor's device the current one around a call, where it is not."""
+def _on(index: int, call, *args):
+    """call(*args, stream) with the device's current stream, the device made the current one around it where it is not.
+    (The raw stream, where this torch has it: the objects of torch.cuda cost a call for one token a third of its time.)"""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    stream = raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+    if torch.cuda.current_device() == index:
+        return call(*args, stream)
+    with torch.cuda.device(index):
+        return call(*args, stream)
 
-    def __init__(self, device: torch.device):
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-        self.device = device
 
-    def __enter__(self) -> int:
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+_SPAN_LEAST = np.array([0, 1, 1], dtype=np.int32)
 
 
 def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str = "cuda:0", out: Optional[torch.Tensor] = None):
@@ -625,8 +622,8 @@ def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str 
     sequence int32 [sequences])."""
     span = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
     cu = np.ascontiguousarray(cu_spans, dtype=np.int32)
-    used = span[:int(cu[-1])].astype(np.int64)
-    tokens = max(0, int(np.where(used[:, 1] == 0, used[:, 0], used.prod(axis=1)).sum()))
+    used = np.maximum(span[:int(cu[-1])], _SPAN_LEAST).astype(np.int64)        # a text is n x 1 x 1 tokens
+    tokens = int((used[:, 0] * used[:, 1] * used[:, 2]).sum())
     dev = torch.device(device) if out is None else out.device
     if dev.index is None:
         dev = torch.device(dev.type, torch.cuda.current_device())
@@ -634,9 +631,7 @@ def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str 
         out = torch.empty((3, tokens), dtype=torch.int32, device=dev)
     if not out.is_cuda or out.dtype != torch.int32 or out.dim() != 2 or out.shape[0] != 3 or out.shape[1] < tokens or (out.shape[1] and out.stride(1) != 1):
         raise ValueError("out must be a device int32 [3, >= tokens] whose rows are contiguous")
-    with _on(dev) as stream:
-        after = epd_rope_positions(span, cu, start, t_step, out.data_ptr() or 256, out.stride(0), stream)      # no tokens: nothing is written
-    return out, after
+    return out, _on(dev.index, epd_rope_positions, span, cu, start, t_step, out.data_ptr() or 256, out.stride(0))      # no tokens: nothing is written
 
 
 class Rope:
@@ -662,24 +657,28 @@ class Rope:
         """tensors: one to four of [tokens, heads, head_dim] (views with any strides but the last), positions int32 [axes, tokens].
         Returns the turned tensors: ``out``, which may be ``tensors`` itself, or new ones.  ``inverse`` turns back: the gradients of
         the inputs, given those of the outputs."""
-        T = positions.shape[-1]
-        if not positions.is_cuda or positions.dtype != torch.int32 or positions.dim() != 2 or positions.shape[0] != self.axes or (T > 1 and positions.stride(1) != 1):
+        dev, axes = positions.get_device(), positions.shape
+        if dev < 0 or positions.dtype != torch.int32 or len(axes) != 2 or axes[0] != self.axes or (axes[1] > 1 and positions.stride(1) != 1):
             raise ValueError("positions must be a device int32 [%d, tokens] whose rows are contiguous" % self.axes)
+        T, d = axes[1], self.head_dim
+
+        def strides(v, shape):
+            if v.get_device() != dev or v.dtype != self.dtype or v.shape != shape or len(shape) != 3 or shape[0] != T or shape[2] != d:
+                raise ValueError("tensors must be [tokens, heads, %d] of %s on the positions' device" % (d, self.dtype))
+            a, b, c = v.stride()
+            if c != 1 and v.numel():
+                raise ValueError("the elements of a head must be contiguous")
+            return a, b
+
+        rows = [strides(x, x.shape) for x in tensors]
         if out is None:
             out = [torch.empty(x.shape, dtype=self.dtype, device=x.device) for x in tensors]
-        if len(out) != len(tensors):
+        elif len(out) != len(tensors):
             raise ValueError("as many outputs as tensors")
         arr = (epd_rope_tensor * len(tensors))()
-        for a, x, y in zip(arr, tensors, out):
-            for v in (x, y):
-                if v.device != positions.device or v.dtype != self.dtype or v.dim() != 3 or v.shape[0] != T or v.shape[2] != self.head_dim or v.shape != x.shape:
-                    raise ValueError("tensors must be [tokens, heads, %d] of %s on the positions' device" % (self.head_dim, self.dtype))
-                if v.stride(2) != 1 and v.numel():
-                    raise ValueError("the elements of a head must be contiguous")
-            si, so = x.stride(), y.stride()
-            a.input, a.output, a.in_token, a.in_head, a.out_token, a.out_head, a.heads = x.data_ptr(), y.data_ptr(), si[0], si[1], so[0], so[1], x.shape[1]
-        with _on(positions.device) as stream:
-            epd_rope_apply(self.cfg, arr, positions.data_ptr() or 256, positions.stride(0), T, inverse, stream)
+        for i, (x, y, r) in enumerate(zip(tensors, out, rows)):
+            arr[i] = (x.data_ptr(), y.data_ptr(), *r, *strides(y, x.shape), x.shape[1])
+        _on(dev, epd_rope_apply, self.cfg, arr, positions.data_ptr() or 256, positions.stride(0), T, inverse)
         return list(out)
 
 
@@ -718,7 +717,7 @@ class GatedMLP:
         self.device = torch.device(dev.type, torch.cuda.current_device()) if dev.index is None else dev
         self.workspace = torch.empty(self.workspace_bytes + 256, dtype=torch.uint8, device=self.device)
         self._base = (self.workspace.data_ptr() + 255) // 256 * 256
-        self._stream = torch.cuda.current_stream(self.device).cuda_stream
+        self._stream = torch.cuda.current_stream(self.device).cuda_stream       # on which the workspace may be handed on
         self._shapes = {"gate_up_w": (2 * mlp_dim, hidden), "down_w": (hidden, mlp_dim)}
         if use_bias:
             self._shapes.update(gate_up_b=(2 * mlp_dim,), down_b=(hidden,))
@@ -727,40 +726,44 @@ class GatedMLP:
         w = epd_gated_mlp_weights()
         for n, shape in self._shapes.items():
             t = weights[n]
-            if t.shape != shape or t.dtype != self.dtype or t.device != self.device or not t.is_contiguous():
+            if t.shape != shape or t.dtype != self.dtype or t.get_device() != self.device.index or not t.is_contiguous():
                 raise ValueError("%s must be a contiguous %s %s on %s" % (n, list(shape), self.dtype, self.device))
             setattr(w, n, t.data_ptr())
         return w
 
-    def _rows(self, t: torch.Tensor, name: str, tokens: Optional[int] = None) -> torch.Tensor:
-        if t.dim() != 2 or t.shape[1] != self.hidden or t.dtype != self.dtype or t.device != self.device or (t.stride(1) != 1 and t.numel()) or (tokens is not None and t.shape[0] != tokens):
-            raise ValueError("%s must be [tokens, %d] of %s on %s with contiguous rows" % (name, self.hidden, self.dtype, self.device))
-        return t
+    def _rows(self, t: torch.Tensor, name: str, tokens: Optional[int] = None):
+        """Address of the rows and what they are apart."""
+        shape = t.shape
+        if len(shape) != 2 or shape[1] != self.hidden or t.dtype != self.dtype or t.get_device() != self.device.index or (tokens is not None and shape[0] != tokens):
+            raise ValueError("%s must be [tokens, %d] of %s on %s" % (name, self.hidden, self.dtype, self.device))
+        ld, one = t.stride()
+        if one != 1 and t.numel() and self.hidden > 1:
+            raise ValueError("the rows of %s must be contiguous" % name)
+        return t.data_ptr(), max(ld, self.hidden) if shape[0] < 2 else ld      # one row: its stride means nothing
 
-    @staticmethod
-    def _ld(t: torch.Tensor) -> int:
-        return max(t.stride(0), t.shape[1]) if t.shape[0] < 2 else t.stride(0)      # one row: its stride means nothing
-
-    def _used_on(self, stream: int) -> None:
-        if stream != self._stream:            # the allocator may not hand the workspace on before this stream is through
-            self.workspace.record_stream(torch.cuda.current_stream(self.device))
+    def _call(self, call, *args) -> None:
+        def on(*a):
+            if a[-1] != self._stream:         # the allocator may not hand the workspace on before this stream is through
+                self.workspace.record_stream(torch.cuda.current_stream(self.device))
+            call(*a)
+        _on(self.device.index, on, *args)
 
     def forward(self, weights, x: torch.Tensor, save: bool = False, out: Optional[torch.Tensor] = None):
         """x: [tokens, D], rows any stride apart.  Returns y, or (y, saved) with what ``backward`` needs."""
-        T = self._rows(x, "x").shape[0]
-        w = self._weights(weights)
-        y = torch.empty((T, self.hidden), dtype=self.dtype, device=self.device) if out is None else self._rows(out, "out", T)
+        px, ld_x = self._rows(x, "x")
+        T = x.shape[0]
+        y = torch.empty((T, self.hidden), dtype=self.dtype, device=self.device) if out is None else out
+        py, ld_y = self._rows(y, "out", T)
         saved = torch.empty((T, 2 * self.mlp_dim), dtype=torch.float32, device=self.device) if save else None
-        with _on(self.device) as stream:
-            self._used_on(stream)
-            epd_gated_mlp(self.cfg, w, x.data_ptr(), self._ld(x), T, y.data_ptr(), self._ld(y), None if saved is None else saved.data_ptr(),
-                          self._base, self.workspace_bytes, stream)
+        self._call(epd_gated_mlp, self.cfg, self._weights(weights), px, ld_x, T, py, ld_y, None if saved is None else saved.data_ptr(), self._base,
+                   self.workspace_bytes)
         return (y, saved) if save else y
 
     def backward(self, weights, x: torch.Tensor, dy: torch.Tensor, saved: torch.Tensor, want: Optional[Sequence[str]] = None) -> Dict[str, torch.Tensor]:
         """Gradients of sum(y * dy) by x ("dx") and by the weights; ``want`` names those to compute (all)."""
-        T = self._rows(x, "x").shape[0]
-        self._rows(dy, "dy", T)
+        px, ld_x = self._rows(x, "x")
+        T = x.shape[0]
+        pdy, ld_dy = self._rows(dy, "dy", T)
         if saved.shape != (T, 2 * self.mlp_dim) or saved.dtype != torch.float32 or saved.device != self.device or not saved.is_contiguous():
             raise ValueError("saved must be what forward returned for these rows")
         shapes = {"dx": (T, self.hidden), **self._shapes}
@@ -769,11 +772,7 @@ class GatedMLP:
             out[n] = torch.empty(shapes[n], dtype=self.dtype, device=self.device)
             setattr(grads, n, out[n].data_ptr())
         grads.ld_dx = self.hidden
-        w = self._weights(weights)
-        with _on(self.device) as stream:
-            self._used_on(stream)
-            epd_gated_mlp_backward(self.cfg, w, x.data_ptr(), self._ld(x), dy.data_ptr(), self._ld(dy), T, saved.data_ptr(), grads, self._base,
-                                   self.workspace_bytes, stream)
+        self._call(epd_gated_mlp_backward, self.cfg, self._weights(weights), px, ld_x, pdy, ld_dy, T, saved.data_ptr(), grads, self._base, self.workspace_bytes)
         return out
 
 

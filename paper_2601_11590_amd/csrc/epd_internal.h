@@ -76,6 +76,9 @@ struct GemmArgs {
   int ldgu;
   void* dgu;            // [M, lddgu] (EPI_DGATED)
   int lddgu;
+  float* sums;          // EPI_DGATED, bf16 path: fp32 [rows of sums, 2 * gate_rows] or nullptr: sums of dG | dU over the rows of each wave,
+  int sum_row0;         //   from row sum_row0 on, two rows per tile of the launch along M
+  int a_rows, w_rows;   // products of the gated MLP: 1 = the operand stands [K, rows], lda / ldw apart (ldw is always set there)
   int name_tag;         // bf16 path, EPI_RESIDUAL: 1 = the second MLP GEMM (a kernel name of its own in
                         //   profiles; the code is the same)
 };
@@ -149,9 +152,20 @@ void launch_plan(PlanArgs& p, hipStream_t s);
 void launch_norm(const float* x, const void* gamma, const void* beta, void* out, int T, int D,
                  float eps, bool rms, bool bf16, hipStream_t s);
 void launch_gemm_f32(const GemmArgs& g, hipStream_t s);
+// fp32 products of the gated MLP (EPI_STORE without bias or with, EPI_GATED, EPI_DGATED) and column sums, in one launch
+struct F32Sum { const float* in; float* out; int rows, cols, ld; };      // cols = 0: none
+struct F32Group {
+  GemmArgs g[3];
+  F32Sum sum[2];
+  int n, first[4];      // products; first is set by the launcher
+  long t16;             // 16 x 16 tiles and longest K of the products that the tile is chosen by (count_f32): a call's products
+  int k;                //   whether wanted or not, so that a gradient has the same bits in every call
+};
+void count_f32(F32Group& a, int M, int N, int K);
+hipError_t launch_gemm_f32_group(F32Group& a, hipStream_t s);
 bool launch_attn_f32(const AttnArgs& a, hipStream_t s);   // false: head_dim not covered
 void launch_gemm_bf16(const GemmArgs& g, hipStream_t s);
-void launch_gemm_bf16_gated(const GemmArgs& g, hipStream_t s);   // EPI_STORE (bf16 out), EPI_GATED, EPI_DGATED; zeros, overread_* are not used
+int launch_gemm_bf16_gated(const GemmArgs& g, hipStream_t s);   // EPI_STORE (bf16 out), EPI_GATED, EPI_DGATED; zeros, overread_* are not used
 // How launch_gemm_bf16 would tile g on a chip of compute_units units (<= 0: the current device's;
 // host only, launches nothing): the tile of the first or only launch, and the rows that launch
 // covers when the rest is left to a second launch of smaller tiles (0 = one launch covers all).

@@ -8,8 +8,8 @@
 // Backward, from dY and the saved G, U:
 //   dH = dY Wd;  dU = dH act(G), dG = dH U act'(G), H = act(G) U   in the epilogue of the first product (EPI_DGATED)
 //   dX = dG Wg + dU Wu;  dWgu = (dG | dU)^T X;  dWd = dY^T H;  biases: column sums of dG | dU and dY
-// Every product is A W^T with K contiguous in both operands; the operands whose rows run along the other axis are turned by
-// a transpose kernel first.  Rounded to bf16 on the way, beside the outputs: H, dG and dU, each once, as operands of
+// Every product is A W^T.  Where K runs along the rows of an operand the ping-pong loop reads it transposed from LDS; products
+// too small for its tiles have the operand turned by a kernel first, whichever the model prices lower.  Rounded to bf16 on the way, beside the outputs: H, dG and dU, each once, as operands of
 // matrix instructions; G and U are kept in fp32, sums are fp32 throughout.
 #include "gemm_bf16_tile.h"
 #include "op_error.h"
@@ -125,11 +125,11 @@ template <int NW, int U, bool GATED> static hipError_t launch_few(const FewArgs&
 }
 
 // ------------------------------------------------------------------------------ transpose, column sums
-// out[c][r] = in[r][c], r < R, c < C; zeros for R <= r < ldo.  Tiles of 64 x 64 through LDS; bf16: 16 bytes per access on
+// out[c][r] = in[r][c], r < R, c < C; zeros for R <= r < ldo.  Tiles of 64 x 64 through LDS, 16 bytes per access on
 // both sides (C, ldi, ldo multiples of 8).  Bound: HBM.
-template <typename E> struct TransposeArgs { const E* in; E* out; int R, C, ldi, ldo; };
+struct TransposeArgs { const uint16_t* in; uint16_t* out; int R, C, ldi, ldo; };
 
-__global__ __launch_bounds__(256) void transpose_bf16_kernel(TransposeArgs<uint16_t> a) {
+__global__ __launch_bounds__(256) void transpose_bf16_kernel(TransposeArgs a) {
   __shared__ uint16_t tile[64][66];
   const int tid = threadIdx.x, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
 #pragma unroll
@@ -152,52 +152,45 @@ __global__ __launch_bounds__(256) void transpose_bf16_kernel(TransposeArgs<uint1
   }
 }
 
-__global__ __launch_bounds__(256) void transpose_f32_kernel(TransposeArgs<float> a) {
-  __shared__ float tile[64][65];
-  const int tid = threadIdx.x, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
-  for (int i = tid; i < 64 * 64; i += 256) {
-    const int r = i >> 6, c = i & 63;
-    tile[r][c] = r0 + r < a.R && c0 + c < a.C ? a.in[(size_t)(r0 + r) * a.ldi + c0 + c] : 0.f;
-  }
-  __syncthreads();
-  for (int i = tid; i < 64 * 64; i += 256) {
-    const int c = i >> 6, r = i & 63;
-    if (c0 + c < a.C && r0 + r < a.ldo) a.out[(size_t)(c0 + c) * a.ldo + r0 + r] = tile[r][c];
-  }
-}
-
-static hipError_t transpose(bool bf16, const void* in, int ldi, void* out, int ldo, int R, int C, hipStream_t s) {
-  const dim3 grid((ldo + 63) / 64, (C + 63) / 64);
-  if (bf16) {
-    TransposeArgs<uint16_t> a{(const uint16_t*)in, (uint16_t*)out, R, C, ldi, ldo};
-    void* args[] = {(void*)&a};
-    return hipLaunchKernel((const void*)transpose_bf16_kernel, grid, dim3(256), args, 0, s);
-  }
-  TransposeArgs<float> a{(const float*)in, (float*)out, R, C, ldi, ldo};
+static hipError_t transpose(const void* in, int ldi, void* out, int ldo, int R, int C, hipStream_t s) {
+  TransposeArgs a{(const uint16_t*)in, (uint16_t*)out, R, C, ldi, ldo};
   void* args[] = {(void*)&a};
-  return hipLaunchKernel((const void*)transpose_f32_kernel, grid, dim3(256), args, 0, s);
+  return hipLaunchKernel((const void*)transpose_bf16_kernel, dim3((ldo + 63) / 64, (C + 63) / 64), dim3(256), args, 0, s);
 }
 
-// out[r] = sum of in[r][0 .. n): the gradient of a bias, from rows that were turned.  A wave per row, fp32.
-template <typename E> __global__ __launch_bounds__(256) void row_sum_kernel(const E* in, E* out, int R, int n, int ld) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (r >= R) return;
-  float sum = 0.f;
-  for (int k = lane; k < n; k += 64) sum += (float)in[(size_t)r * ld + k];
+// Column sums for the gradients of the biases, in two steps with fixed orders: partial sums of rows, fp32, then these over the
+// parts.  (dG | dU leaves its partial sums in the epilogue that makes it.)
+struct PartSums { const __bf16* in; float* out; int rows, cols, ld, per; };       // out[p][c] over rows p * per ...
+__global__ __launch_bounds__(256) void part_sums_kernel(PartSums a) {
+  const int c = (blockIdx.y * 256 + threadIdx.x) * 8, r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.rows);
+  if (c >= a.cols) return;
+  float v[8] = {};
+#pragma unroll 4
+  for (int r = r0; r < r1; ++r) {
+    const bf16x8 x = *(const bf16x8*)(a.in + (size_t)r * a.ld + c);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (lane == 0) out[r] = (E)sum;
+    for (int j = 0; j < 8; ++j) v[j] += (float)x[j];
+  }
+  float* const to = a.out + (size_t)blockIdx.x * a.cols + c;
+  *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
+  *(float4*)(to + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-static hipError_t row_sums(bool bf16, const void* in, void* out, int R, int n, int ld, hipStream_t s) {
-  void* args[] = {(void*)&in, (void*)&out, (void*)&R, (void*)&n, (void*)&ld};
-  return hipLaunchKernel(bf16 ? (const void*)row_sum_kernel<__bf16> : (const void*)row_sum_kernel<float>, dim3((R + 3) / 4), dim3(256), args, 0, s);
-}
-
-// Columns [c0, c1) of rows of `ld` 16-bit values cleared (c0, c1 multiples of 8).
-__global__ __launch_bounds__(256) void clear_columns_kernel(uint16_t* p, int R, int c0, int c1, int ld) {
-  const int per = (c1 - c0) / 8, i = blockIdx.x * 256 + threadIdx.x, r = i / per, c = i - r * per;
-  if (r < R) *(uint4*)(p + (size_t)r * ld + c0 + c * 8) = make_uint4(0u, 0u, 0u, 0u);
+struct SumParts { const float* in; __bf16* out; int parts, cols; };
+struct SumPartsArgs { SumParts job[2]; int blocks0; };                            // blocks of 64 columns: those of job 0, then of job 1
+__global__ __launch_bounds__(256) void sum_parts_kernel(SumPartsArgs a) {
+  __shared__ float part[4][64];
+  const bool second = (int)blockIdx.x >= a.blocks0;
+  const SumParts& s = a.job[second];
+  const int c = ((int)blockIdx.x - (second ? a.blocks0 : 0)) * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
+  float v = 0.f;
+  if (c < s.cols) {
+#pragma unroll 8
+    for (int p = g; p < s.parts; p += 4) v += s.in[(size_t)p * s.cols + c];
+  }
+  part[g][threadIdx.x & 63] = v;
+  __syncthreads();
+  if (g == 0 && c < s.cols) s.out[c] = (__bf16)((part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]));
 }
 
 // All of a dense array cleared.
@@ -213,28 +206,126 @@ static hipError_t clear(bool bf16, void* p, int64_t n, hipStream_t s) {
 // ------------------------------------------------------------------------------ products
 template <int EPI> static void launch_gated_epi(const GemmArgs& g, hipStream_t s) { launch_epi<EPI, OUT_BF16, false, true>(g, s); }
 
+// operands that stand [K, rows]: the tiles of the ping-pong loop (A: those whose wave rows are whole blocks of 64)
+template <int EPI, int KROWS> static void launch_krows(const GemmArgs& g, hipStream_t s) {
+  if (g.tile_cfg == 3) launch_cfg<T2, EPI, OUT_BF16, false, true, KROWS>(g, s);
+  else if (KROWS == 2 && g.tile_cfg == 6) launch_cfg<T5, EPI, OUT_BF16, false, true, 2>(g, s);
+  else launch_cfg<T0, EPI, OUT_BF16, false, true, KROWS>(g, s);
+}
+
 static void launch_gated_whole(const GemmArgs& g, hipStream_t s) {
-  if (g.epilogue == EPI_GATED) launch_gated_epi<EPI_GATED>(g, s);
+  if (g.a_rows) launch_krows<EPI_STORE, 3>(g, s);
+  else if (g.w_rows && g.epilogue == EPI_DGATED) launch_krows<EPI_DGATED, 2>(g, s);
+  else if (g.w_rows) launch_krows<EPI_STORE, 2>(g, s);
+  else if (g.epilogue == EPI_GATED) launch_gated_epi<EPI_GATED>(g, s);
   else if (g.epilogue == EPI_DGATED) launch_gated_epi<EPI_DGATED>(g, s);
   else launch_gated_epi<EPI_STORE>(g, s);
 }
 
-// EPI_STORE, EPI_GATED or EPI_DGATED with operands that are not read past their ends; cut as the encoder's are.
-void launch_gemm_bf16_gated(const GemmArgs& g, hipStream_t s) {
-  if (g.M <= 0 || g.N <= 0) return;
-  const TilePlan plan = g.tile_cfg == 0 ? plan_tiles(g.M, g.N, g.K, g.epilogue, true, g.compute_units > 0 ? g.compute_units : num_cus()) : TilePlan{0, 0, 0.0, 0};
-  if (plan.body_rows <= 0) { launch_gated_whole(g, s); return; }
+// Time of a launch of these products in us: per round of blocks alpha * K / 1024 + beta[epilogue] (the last round, of a
+// share f of the blocks, last0 + last1 * f of that), and `launch`.  Fitted to 199 shapes in every tile (hidden 1024, 1152 and 3200, 65 ... 32 768
+// tokens, forward and backward products, random operands): 7 ... 12 % off in the mean, and the tile it ranks first is within 3 % of
+// the fastest in 178 of them, 1 % off in the mean.  The encoder's own planner (plan_tiles) ranks its launches beside attention and
+// keeps its constants; it offers 256 x 128 tiles to residual adds only, which here win wherever a narrow output fills one round
+// of them (6272 x 1024 x 8192: 93 us, 112 in 128 x 128 tiles, 142 in 256 x 256).
+//   An operand that stands [K, rows] costs alpha what reading fragments in halves of 8 bytes costs: a factor for W, and for both
+// (0: no kernel).  25 600 x 3200 x 8192 in 256 x 256 tiles 1093 us, 1044 with both operands turned, which takes 170 more; 8192 x 3200 x
+// 25 600, W alone, 1072 and 1065 + 60.
+struct ProductTile { int cfg, bm, bn, blocks; double last0, last1, alpha, launch, beta[4], rows_w, rows_both; };     // beta: store, gated, gated and saved, dgated
+constexpr ProductTile kProductTiles[] = {
+  {0, 256, 256, 1, 0.62, 0.28, 23.8, 3.4, {6.0, 6.9, 13.2, 32.0}, 1.02, 1.07},
+  {2, 256, 128, 1, 0.62, 0.25, 14.1, 3.9, {4.1, 3.9, 9.0, 17.4}, 1.10, 1.18},
+  {4, 128, 128, 2, 0.51, 0.44, 16.1, 3.4, {2.5, 0.6, 3.8, 11.4}, 0.0, 0.0},
+  {5, 320, 256, 1, 0.64, 0.30, 28.4, 1.7, {8.9, 10.1, 17.3, 42.5}, 1.04, 0.0},
+  {7, 64, 64, 2, 0.54, 0.49, 6.6, 3.1, {1.3, 1.5, 2.0, 3.0}, 0.0, 0.0},
+  {8, 64, 128, 2, 0.48, 0.55, 10.3, 3.4, {1.9, 1.1, 2.3, 5.4}, 0.0, 0.0},
+};
+
+static double rows_factor(const ProductTile& t, const GemmArgs& g) { return g.a_rows ? t.rows_both : g.w_rows ? t.rows_w : 1.0; }      // 0: the tile has no such kernel
+
+static double product_cost(const ProductTile& t, long M, long N, double K, int kind, long cus) {
+  const long tiles = ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn), slots = cus * t.blocks, full = tiles / slots, rest = tiles % slots;
+  return t.launch + ((double)full + (rest ? t.last0 + t.last1 * (double)rest / (double)slots : 0.0)) * (t.alpha * K / 1024.0 + t.beta[kind]);
+}
+
+// One launch of the cheapest tile, or whole rounds of a large one and the rest of the rows in the cheapest for them:
+// 8192 x 3200 x 25 600 is 416 tiles of 256 x 256, priced two rounds (1075 us); 6080 rows in one round of 320 x 256 and 2112 in one of 256 x 128 take 980.
+static TilePlan plan_product(const GemmArgs& g, long cus) {
+  const int kind = g.epilogue == EPI_GATED ? (g.gu ? 2 : 1) : g.epilogue == EPI_DGATED ? 3 : 0;
+  auto best_tile = [&](long rows, double& cost) {
+    int best = 0;
+    cost = 1e300;
+    for (const ProductTile& t : kProductTiles) {
+      const double f = rows_factor(t, g), c = product_cost(t, rows, g.N, f * g.K, kind, cus);
+      if (f > 0.0 && c < cost) { cost = c; best = t.cfg; }
+    }
+    return best;
+  };
+  TilePlan plan = {0, 0, 0.0, 0};
+  plan.tile = best_tile(g.M, plan.cost);
+  const double keep = 0.95 * plan.cost;          // a second launch has to be worth it: nothing hides its ramp
+  for (const ProductTile& t : kProductTiles) {
+    const double f = rows_factor(t, g);
+    if (t.blocks != 1 || f == 0.0) continue;     // the large tiles
+    const long tm = ((long)g.M + t.bm - 1) / t.bm, tn = ((long)g.N + t.bn - 1) / t.bn, full = tm * tn / cus;
+    for (long rounds = full; rounds >= 1 && rounds >= full - 1; --rounds) {
+      const long body = std::min(rounds * cus / tn, (long)g.M / t.bm) * t.bm;
+      if (body < 1 || body >= g.M) continue;
+      double tail;
+      const int tail_tile = best_tile(g.M - body, tail);
+      const double cost = product_cost(t, body, g.N, f * g.K, kind, cus) + tail;
+      if (cost < keep && cost < plan.cost) plan = {t.cfg, (int)body, cost, tail_tile};
+    }
+  }
+  return plan;
+}
+
+static int tile_rows(int tile) { return tile == 5 ? 320 : tile == 4 ? 128 : tile >= 7 ? 64 : 256; }
+
+// EPI_STORE, EPI_GATED or EPI_DGATED with operands that are not read past their ends.  Returns the rows of g.sums that the
+// launches fill (two per tile along M).
+int launch_gemm_bf16_gated(const GemmArgs& args, hipStream_t s) {
+  if (args.M <= 0 || args.N <= 0) return 0;
+  GemmArgs g = args;
+  TilePlan plan = {0, 0, 0.0, 0};
+  if (g.tile_cfg == 0) {
+    plan = plan_product(g, g.compute_units > 0 ? g.compute_units : num_cus());
+    g.tile_cfg = plan.tile + 1;
+  }
+  auto sum_rows = [](const GemmArgs& x) { return (x.M + tile_rows(x.tile_cfg - 1) - 1) / tile_rows(x.tile_cfg - 1) * 2; };
+  if (plan.body_rows <= 0) { launch_gated_whole(g, s); return sum_rows(g); }
   const size_t mb = plan.body_rows;
   GemmArgs body = g, tail = g;
-  body.M = (int)mb; body.tile_cfg = plan.tile + 1;
+  body.M = (int)mb;
   tail.M = g.M - (int)mb; tail.tile_cfg = plan.tail_tile + 1;
-  tail.A = (const __bf16*)g.A + mb * g.lda;
+  tail.A = (const __bf16*)g.A + (g.a_rows ? mb : mb * g.lda);
+  tail.sum_row0 = g.sum_row0 + sum_rows(body);
   if (g.out) tail.out = (__bf16*)g.out + mb * g.ldo;
   if (g.gu) tail.gu = (float*)g.gu + mb * g.ldgu;
   if (g.dgu) tail.dgu = (__bf16*)g.dgu + mb * g.lddgu;
   if (g.stats_in) tail.stats_in = g.stats_in + mb * g.stats_n;
   launch_gated_whole(body, s);
   launch_gated_whole(tail, s);
+  return sum_rows(body) + sum_rows(tail);
+}
+
+// A product whose operands stand [K, rows] (g.a_rows, g.w_rows): as they stand, or turned into a_t and w_t (rows of round_up(K, 8))
+// first, which costs a pass over them at about 4.5 TB/s and a launch each.  sum_rows: see launch_gemm_bf16_gated.
+static hipError_t launch_product(GemmArgs g, void* a_t, void* w_t, hipStream_t s, int* sum_rows = nullptr) {
+  const long cus = num_cus();
+  GemmArgs t = g;
+  double turn = 0.0;
+  t.K = (g.K + 7) / 8 * 8;
+  if (g.a_rows) { t.A = a_t; t.lda = t.K; t.a_rows = 0; turn += 3.0 + 4.0 * g.K * (double)g.M / 4.5e6; }
+  if (g.w_rows) { t.W = w_t; t.ldw = t.K; t.w_rows = 0; turn += 3.0 + 4.0 * g.K * (double)g.N / 4.5e6; }
+  if (plan_product(t, cus).cost + turn < plan_product(g, cus).cost) {
+    if (g.a_rows) if (hipError_t e = transpose(g.A, g.lda, a_t, t.lda, g.K, g.M, s)) return e;
+    if (g.w_rows) if (hipError_t e = transpose(g.W, g.ldw, w_t, t.ldw, g.K, g.N, s)) return e;
+    g = t;
+  }
+  const int rows = launch_gemm_bf16_gated(g, s);
+  if (sum_rows) *sum_rows = rows;
+  return hipSuccess;
 }
 
 }  // namespace epd
@@ -245,9 +336,12 @@ namespace {
 
 // ------------------------------------------------------------------ workspace layout (bytes)
 struct GatedLayout {
-  int es, Tp, P2, Dp;                   // element size; tokens, 2 F and D padded to whole K steps (bf16)
-  size_t h, wd_t, wgu_t, dgu, dgu_t, h_t, x_t, dy_t, total;
+  int es;                               // element size
+  size_t h, dgu, a_t, w_t, sums_gu, sums_d, total;
 };
+
+constexpr int kParts = 512;             // partial sums of dY at most, of 64 rows or more each
+int part_rows(int tokens) { return std::max(64, (tokens + kParts - 1) / kParts); }
 
 GatedLayout gated_layout(const epd_gated_mlp_cfg& c) {
   GatedLayout L;
@@ -255,19 +349,17 @@ GatedLayout gated_layout(const epd_gated_mlp_cfg& c) {
   auto up = [](size_t v, size_t a) { return (v + a - 1) / a * a; };
   const size_t D = c.hidden, F = c.mlp_dim, T = c.max_tokens;
   L.es = bf ? 2 : 4;
-  L.Tp = (int)(bf ? up(T, 64) : T); L.P2 = (int)(bf ? up(2 * F, 64) : 2 * F); L.Dp = (int)(bf ? up(D, 8) : D);
   size_t off = 0;
-  auto take = [&](size_t elements) { const size_t o = off; off = up(off + elements * L.es, 256); return o; };
-  L.h = take(T * F);
-  L.wd_t = L.wgu_t = L.dgu = L.dgu_t = L.h_t = L.x_t = L.dy_t = 0;
-  if (c.training) {
-    L.wd_t = take(F * L.Dp);
-    L.wgu_t = take(D * L.P2);
-    L.dgu = take(T * L.P2);
-    L.dgu_t = take(2 * F * L.Tp);
-    L.h_t = take(F * L.Tp);
-    L.x_t = take(D * L.Tp);
-    L.dy_t = take(D * L.Tp);
+  auto take = [&](size_t bytes) { const size_t o = off; off = up(off + bytes, 256); return o; };
+  L.h = take(T * F * L.es);
+  L.dgu = L.a_t = L.w_t = L.sums_gu = L.sums_d = 0;
+  if (c.training) L.dgu = take(T * 2 * F * L.es);
+  if (c.training && bf) {
+    const size_t Tp = up(T, 8);
+    L.a_t = take(std::max(2 * F, D) * Tp * L.es);                                   // (dG | dU)^T, dY^T
+    L.w_t = take(std::max(std::max(D, F) * Tp, 2 * F * D) * L.es);                  // X^T, H^T, Wd^T, Wgu^T
+    L.sums_gu = take(c.use_bias ? (up(T, 64) / 32 + 2) * 2 * F * 4 : 0);            // two rows per tile of 64 rows or more; a cut launch has a tile more
+    L.sums_d = take(c.use_bias ? std::min<size_t>(kParts, (T + 63) / 64) * D * 4 : 0);
   }
   L.total = off;
   return L;
@@ -285,7 +377,8 @@ epd_status check_cfg(const char* who, const epd_gated_mlp_cfg* c) {
   if (c->dtype == EPD_BF16 && (c->hidden % 8 || c->mlp_dim % 8)) return op_fail(EPD_ERR_UNSUPPORTED, "%s: bf16: hidden and mlp_dim must be multiples of 8", who);
   if (c->hidden > 65536 || c->mlp_dim > 131072 || (int64_t)c->hidden * c->mlp_dim >= (1ll << 30))
     return op_fail(EPD_ERR_UNSUPPORTED, "%s: hidden %d, mlp_dim %d: at most 65536, 131072 and 2^30 together", who, c->hidden, c->mlp_dim);
-  if (c->max_tokens >= kMaxTokens || (int64_t)c->max_tokens * c->mlp_dim >= (1ll << 36) || (int64_t)c->max_tokens * c->hidden >= (1ll << 36))
+  // (a launch has fewer than 2^32 threads: tiles of 128 x 128 and 256 threads, fp32 64 x 64)
+  if (c->max_tokens >= kMaxTokens || (int64_t)c->max_tokens * std::max(c->mlp_dim, c->hidden) >= (c->dtype == EPD_BF16 ? 1ll << 36 : 1ll << 33))
     return op_fail(EPD_ERR_UNSUPPORTED, "%s: max_tokens %d too large", who, c->max_tokens);
   return EPD_OK;
 }
@@ -324,11 +417,6 @@ struct LastError {
   }
 };
 
-void gemm(const epd_gated_mlp_cfg& c, GemmArgs& g, hipStream_t s) {
-  if (c.dtype == EPD_BF16) launch_gemm_bf16_gated(g, s);
-  else launch_gemm_f32(g, s);
-}
-
 }  // namespace
 
 extern "C" {
@@ -360,21 +448,28 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
     if (e != hipSuccess) return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e));
     return EPD_OK;
   }
-  const LastError last;
-  {
-    GemmArgs g{};
-    g.A = x; g.lda = (int)ld_x; g.W = w->gate_up_w; g.bias = c.use_bias ? w->gate_up_b : nullptr;
-    g.M = T; g.N = bf ? (F + 15) / 16 * 32 : 2 * F; g.K = D; g.epilogue = EPI_GATED; g.act = act_code(c);
-    g.gate_rows = F; g.out = H; g.ldo = F; g.gu = saved; g.ldgu = 2 * F;
-    gemm(c, g, st);
+  GemmArgs up{}, down{};
+  up.A = x; up.lda = (int)ld_x; up.W = w->gate_up_w; up.ldw = D; up.bias = c.use_bias ? w->gate_up_b : nullptr;
+  up.M = T; up.N = bf ? (F + 15) / 16 * 32 : 2 * F; up.K = D; up.epilogue = EPI_GATED; up.act = act_code(c);
+  up.gate_rows = F; up.out = H; up.ldo = F; up.gu = saved; up.ldgu = 2 * F;
+  down.A = H; down.lda = F; down.W = w->down_w; down.ldw = F; down.bias = c.use_bias ? w->down_b : nullptr;
+  down.M = T; down.N = D; down.K = F; down.epilogue = EPI_STORE; down.out = y; down.ldo = (int)ld_y;
+  hipError_t e;
+  if (bf) {
+    const LastError last;
+    launch_gemm_bf16_gated(up, st);
+    launch_gemm_bf16_gated(down, st);
+    e = last.now();
+  } else {
+    F32Group a{}, b{};
+    a.n = b.n = 1;
+    a.g[0] = up; b.g[0] = down;
+    count_f32(a, up.M, up.N, up.K);
+    count_f32(b, down.M, down.N, down.K);
+    e = launch_gemm_f32_group(a, st);
+    if (e == hipSuccess) e = launch_gemm_f32_group(b, st);
   }
-  {
-    GemmArgs g{};
-    g.A = H; g.lda = F; g.W = w->down_w; g.bias = c.use_bias ? w->down_b : nullptr;
-    g.M = T; g.N = D; g.K = F; g.epilogue = EPI_STORE; g.out = y; g.ldo = (int)ld_y;
-    gemm(c, g, st);
-  }
-  if (hipError_t e = last.now()) return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e));
+  if (e != hipSuccess) return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e));
   return EPD_OK;
 }
 
@@ -407,54 +502,57 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
   if (grads->dx) if (epd_status s = check_rows(who, "dx", c, grads->dx, grads->ld_dx)) return s;
   const GatedLayout L = gated_layout(c);
   char* const ws = (char*)workspace;
-  const int T = tokens, Tp = bf ? (T + 63) / 64 * 64 : T, P2 = L.P2;
-  const bool want_gu = grads->gate_up_w || grads->gate_up_b, want_d = grads->down_w || grads->down_b;
+  const int T = tokens, iD = c.hidden, iF = c.mlp_dim;
+  const bool want_gu = grads->gate_up_w || grads->gate_up_b, want_h = grads->dx || want_gu || grads->down_w;
+  // dH = dY Wd, and at once dG, dU and H
+  GemmArgs dh{}, dx{}, dgu{}, dd{};
+  dh.A = dy; dh.lda = (int)ld_dy; dh.M = T; dh.N = iF; dh.K = iD; dh.epilogue = EPI_DGATED; dh.act = act_code(c);
+  dh.gate_rows = iF; dh.gu = (void*)saved; dh.ldgu = 2 * iF; dh.dgu = ws + L.dgu; dh.lddgu = 2 * iF; dh.out = ws + L.h; dh.ldo = iF;
+  // dX = (dG | dU) Wgu,  dWgu = (dG | dU)^T X,  dWd = dY^T H
+  dx.A = ws + L.dgu; dx.lda = 2 * iF; dx.M = T; dx.N = iD; dx.K = 2 * iF; dx.epilogue = EPI_STORE; dx.out = grads->dx; dx.ldo = (int)grads->ld_dx;
+  dgu.M = 2 * iF; dgu.N = iD; dgu.epilogue = EPI_STORE; dgu.out = grads->gate_up_w; dgu.ldo = iD;
+  dd.M = iD; dd.N = iF; dd.epilogue = EPI_STORE; dd.out = grads->down_w; dd.ldo = iF;
+  dh.W = w->down_w; dh.ldw = iF; dh.w_rows = 1;
+  dx.W = w->gate_up_w; dx.ldw = iD; dx.w_rows = 1;
+  dgu.A = ws + L.dgu; dgu.lda = 2 * iF; dgu.a_rows = 1; dgu.W = x; dgu.ldw = (int)ld_x; dgu.w_rows = 1; dgu.K = T;
+  dd.A = dy; dd.lda = (int)ld_dy; dd.a_rows = 1; dd.W = ws + L.h; dd.ldw = iF; dd.w_rows = 1; dd.K = T;
+  if (!bf) {
+    F32Group a{}, b{};
+    a.n = 1; a.g[0] = dh;
+    count_f32(a, dh.M, dh.N, dh.K);
+    for (const GemmArgs* g : {&dx, &dgu, &dd}) count_f32(b, g->M, g->N, g->K);
+    if (want_h && !ok(launch_gemm_f32_group(a, st))) return failed();
+    if (grads->dx) b.g[b.n++] = dx;
+    if (grads->gate_up_w) b.g[b.n++] = dgu;
+    if (grads->down_w) b.g[b.n++] = dd;
+    if (grads->gate_up_b) b.sum[0] = F32Sum{(const float*)(ws + L.dgu), (float*)grads->gate_up_b, T, 2 * iF, 2 * iF};
+    if (grads->down_b) b.sum[1] = F32Sum{(const float*)dy, (float*)grads->down_b, T, iD, (int)ld_dy};
+    if ((b.n || b.sum[0].cols || b.sum[1].cols) && !ok(launch_gemm_f32_group(b, st))) return failed();
+    return EPD_OK;
+  }
   const LastError last;
-  if (grads->dx || want_gu || grads->down_w) {
-    // dH = dY Wd, and at once dG, dU and H
-    if (!ok(transpose(bf, w->down_w, (int)F, ws + L.wd_t, L.Dp, (int)D, (int)F, st))) return failed();
-    GemmArgs g{};
-    g.A = dy; g.lda = (int)ld_dy; g.W = ws + L.wd_t; g.ldw = L.Dp;
-    g.M = T; g.N = (int)F; g.K = (int)D; g.epilogue = EPI_DGATED; g.act = act_code(c);
-    g.gate_rows = (int)F; g.gu = (void*)saved; g.ldgu = (int)(2 * F); g.dgu = ws + L.dgu; g.lddgu = P2; g.out = ws + L.h; g.ldo = (int)F;
-    gemm(c, g, st);
+  SumPartsArgs sums{};
+  if (want_h) {
+    if (grads->gate_up_b) dh.sums = (float*)(ws + L.sums_gu);
+    int rows = 0;
+    if (!ok(launch_product(dh, nullptr, ws + L.w_t, st, &rows))) return failed();
+    if (grads->gate_up_b) sums.job[0] = SumParts{dh.sums, (__bf16*)grads->gate_up_b, rows, 2 * iF};
   }
-  if (grads->dx) {                       // dX = (dG | dU) Wgu
-    if (P2 != 2 * F) {
-      int r = T, c0 = (int)(2 * F), c1 = P2;
-      uint16_t* p = (uint16_t*)(ws + L.dgu);
-      void* args[] = {(void*)&p, (void*)&r, (void*)&c0, (void*)&c1, (void*)&c1};
-      const int64_t n = (int64_t)T * ((P2 - 2 * F) / 8);
-      if (!ok(hipLaunchKernel((const void*)clear_columns_kernel, dim3((int)((n + 255) / 256)), dim3(256), args, 0, st))) return failed();
-    }
-    if (!ok(transpose(bf, w->gate_up_w, (int)D, ws + L.wgu_t, P2, (int)(2 * F), (int)D, st))) return failed();
-    GemmArgs g{};
-    g.A = ws + L.dgu; g.lda = P2; g.W = ws + L.wgu_t; g.ldw = P2;
-    g.M = T; g.N = (int)D; g.K = P2; g.epilogue = EPI_STORE; g.out = grads->dx; g.ldo = (int)grads->ld_dx;
-    gemm(c, g, st);
+  if (grads->down_b) {
+    const int per = part_rows(T), parts = (T + per - 1) / per;
+    PartSums p{(const __bf16*)dy, (float*)(ws + L.sums_d), T, iD, (int)ld_dy, per};
+    void* args[] = {(void*)&p};
+    if (!ok(hipLaunchKernel((const void*)part_sums_kernel, dim3(parts, (iD + 2047) / 2048), dim3(256), args, 0, st))) return failed();
+    sums.job[1] = SumParts{p.out, (__bf16*)grads->down_b, parts, iD};
   }
-  if (want_gu) {                         // dWgu = (dG | dU)^T X
-    if (!ok(transpose(bf, ws + L.dgu, P2, ws + L.dgu_t, Tp, T, (int)(2 * F), st))) return failed();
-    if (grads->gate_up_b && !ok(row_sums(bf, ws + L.dgu_t, grads->gate_up_b, (int)(2 * F), T, Tp, st))) return failed();
-    if (grads->gate_up_w) {
-      if (!ok(transpose(bf, x, (int)ld_x, ws + L.x_t, Tp, T, (int)D, st))) return failed();
-      GemmArgs g{};
-      g.A = ws + L.dgu_t; g.lda = Tp; g.W = ws + L.x_t; g.ldw = Tp;
-      g.M = (int)(2 * F); g.N = (int)D; g.K = Tp; g.epilogue = EPI_STORE; g.out = grads->gate_up_w; g.ldo = (int)D;
-      gemm(c, g, st);
-    }
+  if (sums.job[0].cols || sums.job[1].cols) {
+    sums.blocks0 = (sums.job[0].cols + 63) / 64;
+    void* args[] = {(void*)&sums};
+    if (!ok(hipLaunchKernel((const void*)sum_parts_kernel, dim3(sums.blocks0 + (sums.job[1].cols + 63) / 64), dim3(256), args, 0, st))) return failed();
   }
-  if (want_d) {                          // dWd = dY^T H
-    if (!ok(transpose(bf, dy, (int)ld_dy, ws + L.dy_t, Tp, T, (int)D, st))) return failed();
-    if (grads->down_b && !ok(row_sums(bf, ws + L.dy_t, grads->down_b, (int)D, T, Tp, st))) return failed();
-    if (grads->down_w) {
-      if (!ok(transpose(bf, ws + L.h, (int)F, ws + L.h_t, Tp, T, (int)F, st))) return failed();
-      GemmArgs g{};
-      g.A = ws + L.dy_t; g.lda = Tp; g.W = ws + L.h_t; g.ldw = Tp;
-      g.M = (int)D; g.N = (int)F; g.K = Tp; g.epilogue = EPI_STORE; g.out = grads->down_w; g.ldo = (int)F;
-      gemm(c, g, st);
-    }
-  }
+  if (grads->dx && !ok(launch_product(dx, nullptr, ws + L.w_t, st))) return failed();
+  if (grads->gate_up_w && !ok(launch_product(dgu, ws + L.a_t, ws + L.w_t, st))) return failed();
+  if (grads->down_w && !ok(launch_product(dd, ws + L.a_t, ws + L.w_t, st))) return failed();
   ok(last.now());
   return e == hipSuccess ? EPD_OK : failed();
 }

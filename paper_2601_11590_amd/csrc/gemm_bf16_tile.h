@@ -288,12 +288,72 @@ template <int NA, int NW> __device__ __forceinline__ void read_frags_both(bf16x8
 }
 #undef EPD_DSR
 
-// CLAMP (ping-pong loop, dense rows): as FAST, but nothing past the last row of A or W is read -- both are the caller's.
+// Fragments of an operand that stands [K, rows] in LDS: `ds_read_b64_tr_b16` gives each of 16 lanes one column (row of the
+// operand) of a 4 x 16 block of 16-bit values whose four rows (k) the lanes address, 8 bytes each.  Two of them, four k apart,
+// are the eight k of a lane's fragment.  a[x]: address of block x; k halves and quarters at fixed offsets.  One asm block with its
+// wait, as above; the halves of a fragment are written by different instructions, so each is an output of its own.
+template <int N> __device__ __forceinline__ void join_halves(bf16x8* f, const u32x2* r) {          // f[2 * block + k half]
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const u32x4 v = __builtin_shufflevector(r[2 * i], r[2 * i + 1], 0, 1, 2, 3);
+    f[i] = __builtin_bit_cast(bf16x8, v);
+  }
+}
+#define EPD_TR(d, a, o) "ds_read_b64_tr_b16 %" #d ", %" #a " offset:" #o "\n\t"
+#define EPD_TR4(d0, d1, d2, d3, a) EPD_TR(d0, a, 0) EPD_TR(d1, a, 512) EPD_TR(d2, a, 4096) EPD_TR(d3, a, 4608)
+template <int N> __device__ __forceinline__ void read_frags_tr(bf16x8* f, const uint32_t* a) {
+  static_assert(N == 2 || N == 4, "blocks");
+  u32x2 r[N * 4];
+  if constexpr (N == 2) {
+    asm volatile(EPD_TR4(0, 1, 2, 3, 8) EPD_TR4(4, 5, 6, 7, 9) "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+                 : "v"(a[0]), "v"(a[1]) : "memory");
+  } else {
+    asm volatile(EPD_TR4(0, 1, 2, 3, 16) EPD_TR4(4, 5, 6, 7, 17) EPD_TR4(8, 9, 10, 11, 18) EPD_TR4(12, 13, 14, 15, 19) "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]),
+                   "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]) : "memory");
+  }
+  join_halves<N * 2>(f, r);
+}
+// Both operands' at once (W first): one wait for all of them.
+template <int NW> __device__ __forceinline__ void read_frags_tr_both(bf16x8* f, const uint32_t* a, bf16x8* w, const uint32_t* b) {
+  static_assert(NW == 2 || NW == 4, "blocks");
+  u32x2 r[16], q[NW * 4];
+  if constexpr (NW == 2) {
+    asm volatile(EPD_TR4(16, 17, 18, 19, 28) EPD_TR4(20, 21, 22, 23, 29)
+                 EPD_TR4(0, 1, 2, 3, 24) EPD_TR4(4, 5, 6, 7, 25) EPD_TR4(8, 9, 10, 11, 26) EPD_TR4(12, 13, 14, 15, 27) "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]),
+                   "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15]),
+                   "=&v"(q[0]), "=&v"(q[1]), "=&v"(q[2]), "=&v"(q[3]), "=&v"(q[4]), "=&v"(q[5]), "=&v"(q[6]), "=&v"(q[7])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]) : "memory");
+  } else {
+    asm volatile(EPD_TR4(16, 17, 18, 19, 36) EPD_TR4(20, 21, 22, 23, 37) EPD_TR4(24, 25, 26, 27, 38) EPD_TR4(28, 29, 30, 31, 39)
+                 EPD_TR4(0, 1, 2, 3, 32) EPD_TR4(4, 5, 6, 7, 33) EPD_TR4(8, 9, 10, 11, 34) EPD_TR4(12, 13, 14, 15, 35) "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]),
+                   "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15]),
+                   "=&v"(q[0]), "=&v"(q[1]), "=&v"(q[2]), "=&v"(q[3]), "=&v"(q[4]), "=&v"(q[5]), "=&v"(q[6]), "=&v"(q[7]),
+                   "=&v"(q[8]), "=&v"(q[9]), "=&v"(q[10]), "=&v"(q[11]), "=&v"(q[12]), "=&v"(q[13]), "=&v"(q[14]), "=&v"(q[15])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]) : "memory");
+  }
+  join_halves<8>(f, r);
+  join_halves<NW * 2>(w, q);
+}
+#undef EPD_TR4
+#undef EPD_TR
+
+// CLAMP (ping-pong loop, dense rows): as FAST, but nothing past the last row of A or W is read -- both are the caller's -- and
+// K need not be whole steps (it is a multiple of 8).
 // Rows come in eights: of A, the eight that hold the last row have lane offsets of their own and later ones are replaced by
 // them; the rows of W are whole eights (N, or gate_rows, is a multiple of 8).
 // EPI_GATED: column n of a tile is channel (n / 32) * 16 + n % 16 of the gate (n / 16 even) or the up half, so a lane's two
 // 16-column blocks hold both factors of its channels; W itself stays as it is, its rows are picked at the load.
-template <class T, int EPI, int OUT, bool VMODE, bool GATHER, bool FAST, bool CLAMP = false>
+// KROWS (with CLAMP): bit 0: A stands [K, M], bit 1: W stands [K, N], rows of K lda / ldw apart, so that the products of a backward
+// pass need nothing transposed ahead of them.  A stage of such an operand is blocks of 64 k x 64 rows, 128 bytes per k: loads bring
+// whole lines as before, eight k each, and fragments are read transposed (read_frags_tr).  A wave serves 32 lanes at
+// a time, eight k (0 .. 3 and 8 .. 11) of 32 bytes each, whose 128-byte rows fall on two halves of the banks: the 32-byte pieces of row k
+// are swapped by bits 1 and 3 of k, so that the eight lie in different banks.
+template <class T, int EPI, int OUT, bool VMODE, bool GATHER, bool FAST, bool CLAMP = false, int KROWS = 0>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const int n0, char* const lds) {
   constexpr int BM = T::BM, BN = T::BN, BK = T::BK, NT = T::NT, WM = T::WM, WN = T::WN, TM = T::TM, TN = T::TN;
   constexpr int CPR = T::CPR, LA = T::LA, LW = T::LW;
@@ -321,10 +381,13 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
   //   accumulators that are never stored -- and every load keeps its own per-lane offset.
   constexpr int RPP = NT / CPR;
   static_assert(RPP % 16 == 0, "rows per load instruction");
-  const char* a_base_ptr = (const char*)g.A + (size_t)m0 * g.lda * 2;
+  constexpr bool AK = KROWS & 1, WK = KROWS & 2;
+  static_assert(KROWS == 0 || KROWS == 2 || KROWS == 3, "W, or both");
+  static_assert(KROWS == 0 || (CLAMP && EPI != EPI_GATED && T::PINGPONG && T::WN >= 32 && (!AK || T::WM == 128)), "[K, rows] operands");
+  const char* a_base_ptr = (const char*)g.A + (AK ? (size_t)m0 : (size_t)m0 * g.lda) * 2;
   const int ldw = g.ldw ? g.ldw : g.K;
   constexpr bool GATED = EPI == EPI_GATED;
-  const char* w_base_ptr = (const char*)g.W + (size_t)(GATED ? n0 / 2 : n0) * ldw * 2;
+  const char* w_base_ptr = (const char*)g.W + (WK ? (size_t)n0 : (size_t)(GATED ? n0 / 2 : n0) * ldw) * 2;
   [[maybe_unused]] const int up = GATED ? g.gate_rows : 0;                          // rows from a channel's gate row to its up row
   [[maybe_unused]] const int w_last = (GATED ? g.gate_rows - n0 / 2 : g.N - n0) - 1;     // last channel (row) of W, from w_base_ptr on
   // row of W, from w_base_ptr on, behind column `row` of the tile; CLAMPED: repeats the last one
@@ -687,8 +750,35 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
         }
       }
     };
-    auto load = [&](auto U, auto J, int stage, int kt) {
+    [[maybe_unused]] const int k_chunk = lcol / 2;       // first k of the lane's chunk
+    // [K, rows] operands: load j of a unit is the eight k from `wave` * 8 on of one block of 64 rows; a lane has 8 rows of one k.  Blocks
+    // past the last row are replaced by the last one, in which pieces past it repeat its last.
+    const int kr_col = (((((lane & 7) >> 1) ^ ((lrow >> 1) & 1) ^ ((wave & 1) << 1)) << 1) | (lane & 1)) * 8;
+    [[maybe_unused]] const int a_left = g.M - m0, w_left = g.N - n0;
+    auto kr_edge = [&](int left) { return min(kr_col, (left - 1) % 64 & ~7); };
+    [[maybe_unused]] const uint32_t ka_lane = ((uint32_t)lrow * (uint32_t)g.lda + kr_col) * 2u, kw_lane = ((uint32_t)lrow * (uint32_t)ldw + kr_col) * 2u;
+    [[maybe_unused]] const uint32_t ka_edge = ((uint32_t)lrow * (uint32_t)g.lda + kr_edge(a_left)) * 2u, kw_edge = ((uint32_t)lrow * (uint32_t)ldw + kr_edge(w_left)) * 2u;
+    // LAST: K step kt may be the last one, whose chunks from K on come from a zero buffer (CLAMP only: otherwise K is whole steps)
+    auto load = [&](auto U, auto J, auto LAST, int stage, int kt) {
       constexpr int u = decltype(U)::value, j = decltype(J)::value;
+      if constexpr (u != 1 ? AK : WK) {
+        const int block = u != 1 ? 2 * j + u / 2 : j, left = u != 1 ? a_left : w_left, last = (left - 1) / 64, from = min(block, last);
+        const size_t ld = u != 1 ? g.lda : ldw;
+        char* const dst = lds + (u != 1 ? stage * A_BYTES : S * A_BYTES + stage * W_BYTES) + block * 8192 + wave * 1024;
+        const char* base = (u != 1 ? a_base_ptr : w_base_ptr) + (((size_t)kt * BK + wave * 8) * ld + from * 64) * 2;
+        uint32_t off = from == last ? (u != 1 ? ka_edge : kw_edge) : (u != 1 ? ka_lane : kw_lane);
+        asm volatile("" : "+v"(off));        // see issue()
+        if constexpr (decltype(LAST)::value) {
+          if (ragged_k && kt == nk - 1) {
+            const char* p = base + (size_t)off;
+            if (kt * BK + wave * 8 + lrow >= g.K) p = zeros;
+            __builtin_amdgcn_global_load_lds(EPD_GPTR(p), EPD_LPTR(dst), 16, 0, 0);
+            return;
+          }
+        }
+        __builtin_amdgcn_global_load_lds(EPD_GPTR(base + (size_t)off), EPD_LPTR(dst), 16, 0, 0);
+        return;
+      }
       const int row = tile_row(U, j);
       char* const dst = lds + (u != 1 ? stage * A_BYTES : S * A_BYTES + stage * W_BYTES) + row * ROWB;
       if constexpr (GATHER && u != 1) {
@@ -710,12 +800,30 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
       }
       asm volatile("" : "+v"(off));          // see issue()
       const char* base = u != 1 ? a_base_ptr + ((size_t)from_row * g.lda + (size_t)kt * BK) * 2 : w_base_ptr + ((size_t)from_row * ldw + (size_t)kt * BK) * 2;
+      if constexpr (CLAMP && decltype(LAST)::value) {
+        if (ragged_k && kt == nk - 1) {
+          const char* p = base + (size_t)off;
+          if (kt * BK + k_chunk >= g.K) p = zeros;
+          __builtin_amdgcn_global_load_lds(EPD_GPTR(p), EPD_LPTR(dst), 16, 0, 0);
+          return;
+        }
+      }
       __builtin_amdgcn_global_load_lds(EPD_GPTR(base + (size_t)off), EPD_LPTR(dst), 16, 0, 0);
     };
     auto load_unit = [&](auto U, int stage, int kt) {
       next_rows(U);
-      static_for<PP::loads(decltype(U)::value)>([&](auto J) { load(U, J, stage, kt); });
+      static_for<PP::loads(decltype(U)::value)>([&](auto J) { load(U, J, std::true_type{}, stage, kt); });
     };
+    // [K, rows] fragments: the lane's k row of a block of 64 x 64, its 8 bytes of 32, and the swap of the 32-byte pieces
+    [[maybe_unused]] uint32_t kr_a[4], kr_w[NW];
+    if constexpr (KROWS) {
+      const uint32_t kr_rd = lds0 + (uint32_t)((g4 * 8 + (l16 >> 2)) * 128 + (l16 & 3) * 8);
+      const int kr_swap = (l16 >> 3) | ((g4 & 1) << 1);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) if constexpr (AK) kr_a[x] = kr_rd + (uint32_t)(wm * 2 * 8192 + (x ^ kr_swap) * 32);
+#pragma unroll
+      for (int x = 0; x < NW; ++x) if constexpr (WK) kr_w[x] = kr_rd + (uint32_t)(S * A_BYTES + wn * WN / 64 * 8192 + ((wn * WN % 64 / 16 + x) ^ kr_swap) * 32);
+    }
     bf16x8 pa[2 * PP::NA1], pw[2 * NW];
     // loads ahead of the loop: everything the loop does not issue
     static_for<S>([&](auto TT) {
@@ -729,14 +837,28 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
     __builtin_amdgcn_s_barrier();
     store_row_scale();
     if (wm == 1) __builtin_amdgcn_s_barrier();
-    auto phase = [&](auto P, auto REM, int t, int stg) {
+    auto phase = [&](auto P, auto REM, auto LAST, int t, int stg) {
       constexpr int p = decltype(P)::value, rem = decltype(REM)::value, NA = p ? PP::NA1 : PP::NA0, NM = NA * NW * 2;
       const uint32_t a0 = a_rd0 + stg * A_BYTES, w0 = w_rd0 + stg * W_BYTES;
       static_for<PP::NU>([&](auto U) {
         constexpr int u = decltype(U)::value, ahead = S + (p - PP::q(u) < 0 ? -1 : 0);
         if constexpr (PP::q(u) % NP == p && ahead <= rem) next_rows(U);
       });
-      if constexpr (p == 0) read_frags_both<PP::NA0, NW>(pa, a0, a0 ^ 64u, pw, w0, w0 ^ 64u);
+      if constexpr (KROWS) {
+        // block x of 16 rows: 32 bytes from the others, swapped as the loads did
+        uint32_t at[4], wt[NW];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) if constexpr (AK) at[x] = kr_a[x] + (uint32_t)(stg * A_BYTES + p * 8192);
+#pragma unroll
+        for (int x = 0; x < NW; ++x) if constexpr (WK && p == 0) wt[x] = kr_w[x] + (uint32_t)(stg * W_BYTES);
+        if constexpr (AK && p == 0) {
+          read_frags_tr_both<NW>(pa, at, pw, wt);
+        } else {
+          if constexpr (p == 0) read_frags_tr<NW>(pw, wt);
+          if constexpr (AK) read_frags_tr<NA>(pa, at);
+          else read_frags<NA, p * PP::NA0 * 2048>(pa, a0, a0 ^ 64u);
+        }
+      } else if constexpr (p == 0) read_frags_both<PP::NA0, NW>(pa, a0, a0 ^ 64u, pw, w0, w0 ^ 64u);
       else read_frags<PP::NA1, PP::NA0 * 2048>(pa, a0, a0 ^ 64u);
       constexpr int keep = PP::in_flight(rem, p);
       if constexpr (keep >= 0) wait_vmcnt<keep>();
@@ -758,7 +880,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
               if constexpr (i == NM * (2 * decltype(J)::value + 1) / (2 * n)) {
                 __builtin_amdgcn_sched_barrier(0);
                 int ns = stg + ahead; ns = ns >= S ? ns - S : ns;
-                load(U, J, ns, t + ahead);
+                load(U, J, LAST, ns, t + ahead);
                 __builtin_amdgcn_sched_barrier(0);
               }
             });
@@ -770,14 +892,19 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
       __builtin_amdgcn_sched_barrier(0);
     };
     int t = 0, stg = 0;
-    for (; t + S < nk; ++t) {
-      static_for<NP>([&](auto P) { phase(P, std::integral_constant<int, 2 * S>{}, t, stg); });
+    for (; t + S + (CLAMP ? 1 : 0) < nk; ++t) {
+      static_for<NP>([&](auto P) { phase(P, std::integral_constant<int, 2 * S>{}, std::false_type{}, t, stg); });
+      if (++stg == S) stg = 0;
+    }
+    if (CLAMP && t + S < nk) {               // the step that loads the last one
+      static_for<NP>([&](auto P) { phase(P, std::integral_constant<int, 2 * S>{}, std::true_type{}, t, stg); });
+      ++t;
       if (++stg == S) stg = 0;
     }
     static_for<S>([&](auto R) {              // the last S steps: fewer loads, and fewer to wait for
       constexpr int rem = S - 1 - decltype(R)::value;
       if (nk > rem) {
-        static_for<NP>([&](auto P) { phase(P, std::integral_constant<int, rem>{}, t, stg); });
+        static_for<NP>([&](auto P) { phase(P, std::integral_constant<int, rem>{}, std::true_type{}, t, stg); });
         ++t;
         if (++stg == S) stg = 0;
       }
@@ -1013,6 +1140,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
       const __amdgpu_buffer_rsrc_t d_rows = row_window((const char*)g.dgu + (size_t)(m0 + wm * WM) * d_pitch, (size_t)rows_left * d_pitch);
       const __amdgpu_buffer_rsrc_t h_rows = row_window((const char*)g.out + (size_t)(m0 + wm * WM) * h_pitch, (size_t)rows_left * h_pitch);
       const uint32_t up_off = (uint32_t)g.gate_rows * 2u;
+      f32x4 sum_g = {0.f, 0.f, 0.f, 0.f}, sum_u = {0.f, 0.f, 0.f, 0.f};       // over the lane's rows, of dG and dU before they are rounded
       auto rows = [&](auto ACT) {
         if constexpr (!PREF) {
 #pragma unroll
@@ -1030,13 +1158,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
           for (int w = 0; w < TN16; ++w) {
             const int c = b * TN16 + w;                  // rows c * FR + lane / FC of the wave's tile
             const float4 e = *(const float4*)(stg + schunk(w * FR + lane / FC, lane % FC));
-            const f32x4 dh = __builtin_bit_cast(f32x4, e), gv = __builtin_bit_cast(f32x4, aux[b % AUX][w]), uv = __builtin_bit_cast(f32x4, aux_u[b % AUX][w]);
+            const bool live = c * FR + lane / FC < rows_left;    // rows past the last one repeat it
+            const f32x4 dh = live ? __builtin_bit_cast(f32x4, e) : f32x4{0.f, 0.f, 0.f, 0.f}, gv = __builtin_bit_cast(f32x4, aux[b % AUX][w]), uv = __builtin_bit_cast(f32x4, aux_u[b % AUX][w]);
             float dg[4], du[4], hv[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               float act;
               const float d = gate_act_d<decltype(ACT)::value>(gv[v], act);
               dg[v] = dh[v] * uv[v] * d; du[v] = dh[v] * act; hv[v] = act * uv[v];
+              sum_g[v] += dg[v]; sum_u[v] += du[v];
             }
             __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, pack_bf16x4(dg[0], dg[1], dg[2], dg[3])), d_rows, d_off + (uint32_t)(c * FR) * d_pitch, 0, 0);
             __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, pack_bf16x4(du[0], du[1], du[2], du[3])), d_rows, d_off + (uint32_t)(c * FR) * d_pitch, up_off, 0);
@@ -1049,6 +1179,14 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
       if (g.act == 0) rows(std::integral_constant<int, 0>{});
       else if (g.act == 1) rows(std::integral_constant<int, 1>{});
       else rows(std::integral_constant<int, 2>{});
+      if (g.sums) {                                      // column sums of the wave's rows, one row of `sums` each
+#pragma unroll
+        for (int o = FC; o < 64; o *= 2)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) { sum_g[v] += __shfl_xor(sum_g[v], o); sum_u[v] += __shfl_xor(sum_u[v], o); }
+        float* const to = g.sums + (size_t)(g.sum_row0 + m0 / BM * T::WAVES_M + wm) * (2 * g.gate_rows) + n;
+        if (lane < FC && n < g.N) { *(f32x4*)to = sum_g; *(f32x4*)(to + g.gate_rows) = sum_u; }
+      }
     } else if constexpr (F32_ROWS) {
       const int n = n0 + wn * WN + (lane % FC) * 4;      // N is a multiple of 4: all or nothing
       const bool sums = EPI == EPI_RESIDUAL && g.stats_out != nullptr;
@@ -1239,7 +1377,7 @@ __device__ __forceinline__ void tile_coords(int t, int tiles_m, int tiles_n, int
 // projection, second MLP GEMM) kernel names of their own, so that a profile lists them apart.
 // TAG 2: a product of the gated MLP (clamped operands), whose zeros lie in the code object.
 [[maybe_unused]] static __device__ const uint4 zero_bytes[16] = {};
-template <class T, int EPI, int OUT, bool GATHER, bool FAST, int TAG, bool CLAMP = false>
+template <class T, int EPI, int OUT, bool GATHER, bool FAST, int TAG, bool CLAMP = false, int KROWS = 0>
 __global__ __launch_bounds__(T::NT, T::MINBLK) void gemm_bf16_kernel(GemmArgs g) {
   // + per-row scales of the epilogue + the row numbers of a gathered operand (ping-pong loop)
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS_BYTES + T::BM * 4 + (GATHER && FAST ? T::BM * MAX_PIECES * 4 : 0)];
@@ -1254,7 +1392,7 @@ __global__ __launch_bounds__(T::NT, T::MINBLK) void gemm_bf16_kernel(GemmArgs g)
       return;
     }
   }
-  gemm_tile<T, EPI, OUT, false, GATHER, FAST, CLAMP>(g, m0, n0, lds);
+  gemm_tile<T, EPI, OUT, false, GATHER, FAST, CLAMP, KROWS>(g, m0, n0, lds);
 }
 
 static int num_cus() {
@@ -1268,7 +1406,7 @@ static int num_cus() {
 }
 
 // CLAMPED: operands that may not be read past their ends take the ping-pong loop all the same, with clamps
-template <class T, int EPI, int OUT, bool GATHER, bool CLAMPED = false>
+template <class T, int EPI, int OUT, bool GATHER, bool CLAMPED = false, int KROWS = 0>
 static void launch_cfg(const GemmArgs& g, hipStream_t s) {
   const int tiles_m = (g.M + T::BM - 1) / T::BM, tiles_n = (g.N + T::BN - 1) / T::BN;
   const long blocks = (long)T::MINBLK * (g.compute_units > 0 ? g.compute_units : num_cus());     // of one round
@@ -1293,13 +1431,7 @@ static void launch_cfg(const GemmArgs& g, hipStream_t s) {
   a.group_m = std::min(a.group_m, tiles_m);
   if constexpr (CLAMPED) {
     static_assert(!GATHER, "clamped rows are dense");
-    if constexpr (T::PINGPONG) {
-      if (g.K % T::BK == 0) {
-        hipLaunchKernelGGL((gemm_bf16_kernel<T, EPI, OUT, false, true, 2, true>), dim3(tiles_m * tiles_n), dim3(T::NT), 0, s, a);
-        return;
-      }
-    }
-    hipLaunchKernelGGL((gemm_bf16_kernel<T, EPI, OUT, false, false, 2>), dim3(tiles_m * tiles_n), dim3(T::NT), 0, s, a);
+    hipLaunchKernelGGL((gemm_bf16_kernel<T, EPI, OUT, false, T::PINGPONG, 2, T::PINGPONG, KROWS>), dim3(tiles_m * tiles_n), dim3(T::NT), 0, s, a);
     return;
   } else {
   if constexpr (!GATHER) {

@@ -44,18 +44,21 @@ __device__ __forceinline__ float gate_f32(float g, int act, float& d) {
 
 // A block of NW waves.  SPLIT: all of them share one 16 T x 16 T tile and take its K in turn, 32 at a
 // time, and their sums meet in LDS; otherwise NW = 4 and each has a tile of its own, 2 x 2.
-// GATE: EPI_GATED (column 2 c of the product is channel c's gate, 2 c + 1 its up factor) or EPI_DGATED.
+// OPS: a product of the gated MLP.  EPI_GATED (column 2 c of the product is channel c's gate, 2 c + 1 its up factor),
+// EPI_DGATED, or EPI_STORE; either operand may stand with its rows along memory (a_rows, w_rows): a lane's four k are then
+// four rows, and the 16 lanes of a block read 64 bytes of each, so nothing is transposed first.
 // VEC: rows start 16-byte aligned and K (and a gathered piece) is a multiple of 4; otherwise 16-byte
 // loads from any float's address, and the last of a row taken apart.
-template <int T, int NW, bool SPLIT, bool VEC, bool GATE = false>
-__global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
-  constexpr int WT = 16 * T, BT = SPLIT ? WT : 2 * WT;       // wave and block tile
-  constexpr int LD = BT + 4, COPIES = SPLIT ? NW : 1;
+template <int T, int NW, bool SPLIT> struct F32Tile {
+  static constexpr int WT = 16 * T, BT = SPLIT ? WT : 2 * WT;       // wave and block tile
+  static constexpr int LD = BT + 4, COPIES = SPLIT ? NW : 1;
+};
+template <int T, int NW, bool SPLIT, bool VEC, bool OPS>
+__device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int m0, const int n0, float (*acc_lds)[F32Tile<T, NW, SPLIT>::BT][F32Tile<T, NW, SPLIT>::LD]) {
+  constexpr int WT = F32Tile<T, NW, SPLIT>::WT, BT = F32Tile<T, NW, SPLIT>::BT, COPIES = F32Tile<T, NW, SPLIT>::COPIES;
   constexpr int KS = 32;                                     // k per step and wave: two 16-byte loads per row
-  __shared__ __attribute__((aligned(16))) float acc_lds[COPIES][BT][LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g4 = lane >> 4;
-  const int m0 = blockIdx.y * BT, n0 = blockIdx.x * BT;
   const int wm = SPLIT ? 0 : (wave >> 1) * WT, wn = SPLIT ? 0 : (wave & 1) * WT;
   const float* const A = (const float*)g.A;
   const float* const W = (const float*)g.W;
@@ -66,10 +69,10 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
 #pragma unroll
   for (int t = 0; t < T; ++t) {                              // rows beyond the matrix repeat the last one: never stored
     am[t] = min(m0 + wm + t * 16 + l16, g.M - 1);
-    arow[t] = A + (size_t)am[t] * g.lda;
+    arow[t] = A + (size_t)am[t] * (OPS && g.a_rows ? 1 : g.lda);
     int n = min(n0 + wn + t * 16 + l16, g.N - 1);
-    if (GATE && g.epilogue == EPI_GATED) n = (n >> 1) + (n & 1) * g.gate_rows;
-    wrow[t] = W + (size_t)n * g.K;
+    if (OPS && g.epilogue == EPI_GATED) n = (n >> 1) + (n & 1) * g.gate_rows;
+    wrow[t] = W + (size_t)n * (OPS ? (g.w_rows ? 1 : g.ldw) : g.K);
   }
   auto load4 = [&](const float* row, int k) {                // row[k .. k + 3], zero from K on
     if constexpr (VEC) {
@@ -88,7 +91,16 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
       return v;
     }
   };
+  [[maybe_unused]] auto load_rows = [&](const float* row, size_t ld, int k) {       // rows along memory: row[k ld], ...
+    f32x4 v;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = row[(size_t)min(k + c, g.K - 1) * ld];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) if (k + c >= g.K) v[c] = 0.f;
+    return v;
+  };
   auto load_a = [&](int t, int k) {
+    if constexpr (OPS) return g.a_rows ? load_rows(arow[t], g.lda, k) : load4(arow[t], k);
     if (!g.gather) return load4(arow[t], k);
     f32x4 v;
     if constexpr (VEC) {
@@ -119,7 +131,8 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         fa[buf][t][h] = load_a(t, k0 + h * 16 + g4 * 4);
-        fw[buf][t][h] = load4(wrow[t], k0 + h * 16 + g4 * 4);
+        if constexpr (OPS) fw[buf][t][h] = g.w_rows ? load_rows(wrow[t], g.ldw, k0 + h * 16 + g4 * 4) : load4(wrow[t], k0 + h * 16 + g4 * 4);
+        else fw[buf][t][h] = load4(wrow[t], k0 + h * 16 + g4 * 4);
       }
   };
   auto multiply = [&](int buf) {
@@ -160,7 +173,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
 #pragma unroll
     for (int w = 1; w < COPIES; ++w) v += *(const f32x4*)&acc_lds[w][r][c];
     const int left = min(4, g.N - n);
-    if constexpr (GATE) {
+    if (OPS && g.epilogue != EPI_STORE) {
       float* const gu = (float*)g.gu + (size_t)m * g.ldgu;
       if (g.epilogue == EPI_GATED) {
         for (int j = 0; j < left; j += 2) {
@@ -209,15 +222,83 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
   }
 }
 
+template <int T, int NW, bool SPLIT, bool VEC>
+__global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
+  using F = F32Tile<T, NW, SPLIT>;
+  __shared__ __attribute__((aligned(16))) float acc_lds[F::COPIES][F::BT][F::LD];
+  gemm_f32_tile<T, NW, SPLIT, VEC, false>(g, blockIdx.y * F::BT, blockIdx.x * F::BT, acc_lds);
+}
+
+// Up to three products and two sets of column sums in one launch: products of the sizes this path serves leave most of the
+// chip idle, and what is left of a launch is its latency (8 ... 14 us each, the backward pass of 257 tokens through 256 x 1024
+// was 12 launches and 79 us).  Blocks first[i] .. first[i + 1] - 1 make product i; then 16 columns of a sum each, 16 rows at a time.
+template <int T, int NW, bool SPLIT, bool VEC>
+__global__ __launch_bounds__(64 * NW) void gemm_f32_group_kernel(F32Group a) {
+  using F = F32Tile<T, NW, SPLIT>;
+  __shared__ __attribute__((aligned(16))) float acc_lds[F::COPIES][F::BT][F::LD];
+  int b = blockIdx.x, i = 0;
+  while (i < a.n && b >= a.first[i + 1]) ++i;
+  b -= a.first[i];
+  if (i < a.n) {
+    const int tiles_n = (a.g[i].N + F::BT - 1) / F::BT, tm = b / tiles_n;
+    gemm_f32_tile<T, NW, SPLIT, VEC, true>(a.g[i], tm * F::BT, (b - tm * tiles_n) * F::BT, acc_lds);
+    return;
+  }
+  const int blocks0 = (a.sum[0].cols + 15) / 16;
+  const F32Sum& s = a.sum[b >= blocks0];
+  if (b >= blocks0) b -= blocks0;
+  constexpr int RG = 64 * NW / 16;
+  const int c = b * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
+  float v = 0.f;
+  if (c < s.cols) {
+#pragma unroll 8
+    for (int r = r0; r < s.rows; r += RG) v += s.in[(size_t)r * s.ld + c];
+  }
+  float* const part = &acc_lds[0][0][0];                     // [RG][16]
+  part[threadIdx.x] = v;
+  __syncthreads();
+  if (threadIdx.x < 16 && c < s.cols) {
+    for (int k = 1; k < RG; ++k) v += part[k * 16 + threadIdx.x];
+    s.out[c] = v;
+  }
+}
+
+template <int T, int NW, bool SPLIT> static hipError_t launch_group_f32(F32Group& a, hipStream_t s) {
+  using F = F32Tile<T, NW, SPLIT>;
+  static_assert(sizeof(float) * F::COPIES * F::BT * F::LD >= 64 * NW * sizeof(float), "partial sums");
+  bool vec = true;
+  a.first[0] = 0;
+  for (int i = 0; i < a.n; ++i) {
+    const GemmArgs& g = a.g[i];
+    a.first[i + 1] = a.first[i] + ((g.M + F::BT - 1) / F::BT) * ((g.N + F::BT - 1) / F::BT);
+    vec = vec && (g.a_rows || (g.K % 4 == 0 && g.lda % 4 == 0 && (size_t)g.A % 16 == 0)) && (g.w_rows || (g.K % 4 == 0 && g.ldw % 4 == 0 && (size_t)g.W % 16 == 0));
+  }
+  const int blocks = a.first[a.n] + (a.sum[0].cols + 15) / 16 + (a.sum[1].cols + 15) / 16;
+  void* args[] = {(void*)&a};
+  return hipLaunchKernel(vec ? (const void*)gemm_f32_group_kernel<T, NW, SPLIT, true> : (const void*)gemm_f32_group_kernel<T, NW, SPLIT, false>, dim3(blocks), dim3(64 * NW), args, 0, s);
+}
+
+void count_f32(F32Group& a, int M, int N, int K) {
+  a.t16 += (long)((M + 15) / 16) * ((N + 15) / 16);
+  a.k = std::max(a.k, K);
+}
+
+// K over eight waves: 16 x 16 tiles while they are few, or while one of the products is a few tiles of a long K (the backward
+// pass of 257 tokens, 256 x 1024: 23 us; 27 in 32 x 32 tiles, 34 with K over four waves), else 32 x 32 (1000 tokens,
+// 512 x 2048: 202 us backward; 240 in 16 x 16, 305 in 64 x 64 blocks); 64 x 64 blocks of four wave tiles where there are many tiles of
+// a short K (2048 tokens, gate and up of 512 x 2048: 177 us, 191 in 32 x 32).
+hipError_t launch_gemm_f32_group(F32Group& a, hipStream_t s) {
+  if (a.t16 <= 1024 || (a.k >= 1024 && a.t16 <= 3500)) return launch_group_f32<1, 8, true>(a, s);
+  if (a.t16 >= 20000 && a.k <= 512) return launch_group_f32<2, 4, false>(a, s);
+  return launch_group_f32<2, 8, true>(a, s);
+}
+
 template <int T, int NW, bool SPLIT> static void launch_tile_f32(const GemmArgs& g, hipStream_t s) {
   constexpr int BT = SPLIT ? 16 * T : 32 * T;
   const dim3 grid((g.N + BT - 1) / BT, (g.M + BT - 1) / BT);
   const int piece = g.gather ? g.K / g.gather_n : g.K;
   const bool vec = piece % 4 == 0 && g.lda % 4 == 0 && (((size_t)g.A | (size_t)g.W) & 15) == 0;
-  if (g.epilogue == EPI_GATED || g.epilogue == EPI_DGATED) {
-    if (vec) hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, true, true>), grid, dim3(64 * NW), 0, s, g);
-    else hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, false, true>), grid, dim3(64 * NW), 0, s, g);
-  } else if (vec) hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, true>), grid, dim3(64 * NW), 0, s, g);
+  if (vec) hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, true>), grid, dim3(64 * NW), 0, s, g);
   else hipLaunchKernelGGL((gemm_f32_kernel<T, NW, SPLIT, false>), grid, dim3(64 * NW), 0, s, g);
 }
 
@@ -228,6 +309,15 @@ template <int T, int NW, bool SPLIT> static void launch_tile_f32(const GemmArgs&
 // together, where 64 x 64 tiles of vector arithmetic took 34 - 144 and 428 together.
 void launch_gemm_f32(const GemmArgs& g, hipStream_t s) {
   if (g.M <= 0 || g.N <= 0) return;
+  if (g.epilogue == EPI_GATED) {                   // an encoder's gated MLP
+    F32Group a{};
+    a.n = 1;
+    a.g[0] = g;
+    a.g[0].ldw = g.ldw ? g.ldw : g.K;
+    count_f32(a, g.M, g.N, g.K);
+    (void)launch_gemm_f32_group(a, s);             // a failure is the runtime's last error, as those of the other launches
+    return;
+  }
   const long t16 = (long)((g.M + 15) / 16) * ((g.N + 15) / 16), t32 = (long)((g.M + 31) / 32) * ((g.N + 31) / 32);
   if (t16 <= 256 && g.K >= 512) launch_tile_f32<1, 8, true>(g, s);
   else if (t16 <= 1024) launch_tile_f32<1, 4, true>(g, s);

@@ -176,6 +176,34 @@ __global__ __launch_bounds__(256) void rope_positions_kernel(PosArgs a) {
   a.out[2 * a.stride + tok] = s.pos + c;
 }
 
+// Axis and turns per position of every pair.  A pure function of the configuration, which a program keeps from call to
+// call: the last table of the thread is kept with it (64 powers are 2.5 us of a call for one token).
+static void pair_table(const epd_rope_cfg& c, int pairs, RopeArgs& a) {
+  struct Table { epd_rope_cfg of; double turns[kRopePairs]; uint8_t axis[kRopePairs]; };
+  static thread_local Table t = {};
+  bool same = t.of.struct_size == c.struct_size && t.of.axes == c.axes && t.of.layout == c.layout && t.of.ladder == c.ladder && t.of.base == c.base;
+  for (int x = 0; same && x < c.axes; ++x) same = t.of.pairs[x] == c.pairs[x];
+  if (!same) {
+    int p = 0;
+    auto put = [&](int x, int j) {
+      const double f = std::pow(c.base, c.ladder == EPD_ROPE_LADDER_AXIS ? -(double)j / c.pairs[x] : -(double)p / pairs);
+      t.axis[p] = (uint8_t)x;
+      t.turns[p++] = f / 6.283185307179586476925;
+    };
+    if (c.layout == EPD_ROPE_SECTIONS) {
+      for (int x = 0; x < c.axes; ++x)
+        for (int j = 0; j < c.pairs[x]; ++j) put(x, j);
+    } else {
+      for (int j = 0; p < pairs; ++j)
+        for (int x = 0; x < c.axes; ++x)
+          if (j < c.pairs[x]) put(x, j);
+    }
+    t.of = c;
+  }
+  std::copy(t.turns, t.turns + pairs, a.turns);
+  std::copy(t.axis, t.axis + pairs, a.axis);
+}
+
 }  // namespace epd
 
 using namespace epd;
@@ -206,20 +234,7 @@ epd_status epd_rope_apply(const epd_rope_cfg* c, const epd_rope_tensor* tensors,
   RopeArgs a{};
   const bool bf = c->dtype == EPD_BF16, adjacent = c->pairing == EPD_ROPE_ADJACENT;
   const size_t es = bf ? 2 : 4;
-  int p = 0;
-  auto put = [&](int x, int j) {
-    const double f = std::pow(c->base, c->ladder == EPD_ROPE_LADDER_AXIS ? -(double)j / c->pairs[x] : -(double)p / pairs);
-    a.axis[p] = (uint8_t)x;
-    a.turns[p++] = f / 6.283185307179586476925;
-  };
-  if (c->layout == EPD_ROPE_SECTIONS) {
-    for (int x = 0; x < c->axes; ++x)
-      for (int j = 0; j < c->pairs[x]; ++j) put(x, j);
-  } else {
-    for (int j = 0; p < pairs; ++j)
-      for (int x = 0; x < c->axes; ++x)
-        if (j < c->pairs[x]) put(x, j);
-  }
+  pair_table(*c, pairs, a);
   // elements per access: what every pointer, stride and the pairs allow, 16 bytes at most
   int vec = bf ? 8 : 4, heads = 0;
   auto fits = [&](int64_t v) { while (vec > 1 && v % vec) vec /= 2; };
