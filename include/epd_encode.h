@@ -323,7 +323,8 @@ epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, 
                               int64_t position_stride, int32_t* next_out, void* stream);
 
 /* Gated MLP:  G | U = X Wgu^T (+ b),  H = act(G) * U,  Y = H Wd^T (+ b).  bf16 multiplies on the matrix cores with
- * fp32 sums and rounds H and, in the backward pass, dG and dU to bf16; fp32 computes in fp32.  The encoder's own MLP takes the same weights (epd_layer_weights, act = EPD_SWIGLU ...). */
+ * fp32 sums and rounds H and, in the backward pass, dG and dU to bf16 (act(G) and act'(G) U are saved to 12 bits of
+ * mantissa); fp32 computes in fp32.  The encoder's own MLP takes the same weights (epd_layer_weights, act = EPD_SWIGLU ...). */
 typedef struct {
   uint32_t struct_size; /* sizeof(epd_gated_mlp_cfg)                                                */
   int32_t dtype;        /* epd_dtype of X, Y, weights, gradients                                    */
@@ -352,11 +353,15 @@ typedef struct {        /* device, cfg.dtype; NULL = not wanted; written, not ad
 /* Bytes of device workspace (256-byte aligned) that a call with `cfg` needs; 0 when cfg is invalid. */
 uint64_t epd_gated_mlp_workspace_bytes(const epd_gated_mlp_cfg* cfg);
 
+/* Bytes of `saved` for a call with that many tokens; 0 when cfg is invalid or tokens is out of range (or 0). */
+uint64_t epd_gated_mlp_saved_bytes(const epd_gated_mlp_cfg* cfg, int32_t tokens);
+
 /* Y = MLP(X).
  *   x, y    device [tokens, D], rows ld_x / ld_y >= D elements apart (bf16: multiples of 8, 16-byte aligned); y may
  *           be x (with the same rows)
  *   tokens  0 .. max_tokens; 0 launches nothing
- *   saved   device fp32 [tokens, 2F] (either dtype) or NULL: receives G | U for epd_gated_mlp_backward
+ *   saved   device, epd_gated_mlp_saved_bytes(cfg, tokens) bytes, aligned as x, or NULL: receives what
+ *           epd_gated_mlp_backward needs of this call (its layout is the library's: about 7 F bytes a token in bf16, 8 F in fp32)
  * Nothing in the workspace is kept from one call to the next. */
 epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weights* weights, const void* x,
                          int64_t ld_x, int32_t tokens, void* y, int64_t ld_y, void* saved, void* workspace,

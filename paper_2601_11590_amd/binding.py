@@ -92,8 +92,8 @@ EXPORTS = ["epd_encode_workspace_bytes", "epd_encode_create", "epd_encode", "epd
            "epd_encode_get_timing", "epd_preprocess", "epd_encode_cached", "epd_store_create",
            "epd_store_destroy", "epd_store_last_error", "epd_store_hash", "epd_store_hash_noalloc", "epd_store_lookup", "epd_store_insert",
            "epd_store_stats", "epd_probe_stream_read", "epd_probe_mfma_rate", "epd_probe_gemm_plan"]
-OPERATOR_EXPORTS = ["epd_op_last_error", "epd_rope_apply", "epd_rope_positions", "epd_gated_mlp_workspace_bytes", "epd_gated_mlp",
-                    "epd_gated_mlp_backward"]    # the operators beside the encoder
+OPERATOR_EXPORTS = ["epd_op_last_error", "epd_rope_apply", "epd_rope_positions", "epd_gated_mlp_workspace_bytes", "epd_gated_mlp_saved_bytes",
+                    "epd_gated_mlp", "epd_gated_mlp_backward"]    # the operators beside the encoder
 
 
 def _load() -> C.CDLL:
@@ -159,6 +159,8 @@ def _load() -> C.CDLL:
                                        C.c_void_p, C.c_void_p]
     lib.epd_gated_mlp_workspace_bytes.restype = C.c_uint64
     lib.epd_gated_mlp_workspace_bytes.argtypes = [C.POINTER(epd_gated_mlp_cfg)]
+    lib.epd_gated_mlp_saved_bytes.restype = C.c_uint64
+    lib.epd_gated_mlp_saved_bytes.argtypes = [C.POINTER(epd_gated_mlp_cfg), C.c_int32]
     lib.epd_gated_mlp.restype = C.c_int
     lib.epd_gated_mlp.argtypes = [C.POINTER(epd_gated_mlp_cfg), C.POINTER(epd_gated_mlp_weights), C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
                                   C.c_int64, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
@@ -587,19 +589,30 @@ def epd_rope_apply(cfg: epd_rope_cfg, tensors, positions: int, position_stride: 
 def epd_rope_positions(span_thw: np.ndarray, cu_spans: np.ndarray, start: Optional[np.ndarray], t_step: int, positions: int,
                        position_stride: int, stream: int) -> np.ndarray:
     """Returns the next position of every sequence, int32 [num_sequences]."""
-    span = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
-    cu = np.ascontiguousarray(cu_spans, dtype=np.int32)
-    if cu.ndim != 1 or len(cu) < 1 or (len(cu) > 1 and int(cu.max()) > len(span)):
-        raise ValueError("cu_spans must be [num_sequences + 1] and end within the spans")
+    span, cu = _spans(span_thw, cu_spans)
     n = len(cu) - 1
     if start is not None:
         start = np.ascontiguousarray(start, dtype=np.int32)
         if start.shape != (n,):
             raise ValueError("start must be [num_sequences]")
     after = np.empty(n, dtype=np.int32)
-    _op_check(lib.epd_rope_positions(span.ctypes.data, cu.ctypes.data, n, None if start is None else start.ctypes.data, t_step, positions,
-                                     position_stride, after.ctypes.data, stream))
+    _op_check(lib.epd_rope_positions(_address(span), _address(cu), n, None if start is None else _address(start), t_step, positions, position_stride,
+                                     _address(after), stream))
     return after
+
+
+def _address(a: np.ndarray) -> int:
+    return a.__array_interface__["data"][0]       # (a.ctypes.data makes an object for it)
+
+
+def _spans(span_thw, cu_spans):
+    if type(span_thw) is not np.ndarray or span_thw.dtype != np.int32 or span_thw.ndim != 2 or span_thw.shape[1] != 3 or not span_thw.flags.c_contiguous:
+        span_thw = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
+    if type(cu_spans) is not np.ndarray or cu_spans.dtype != np.int32 or not cu_spans.flags.c_contiguous:
+        cu_spans = np.ascontiguousarray(cu_spans, dtype=np.int32)
+    if cu_spans.ndim != 1 or len(cu_spans) < 1 or int(cu_spans.max()) > len(span_thw):
+        raise ValueError("cu_spans must be [num_sequences + 1] and end within the spans")
+    return span_thw, cu_spans
 
 
 def _on(index: int, call, *args):
@@ -620,8 +633,7 @@ def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str 
     """(t, h, w) positions of sequences of texts (n, 0, 0) and items (t, h, w), sequence s being the spans
     [cu_spans[s], cu_spans[s + 1]) and starting at start[s].  Returns (int32 device tensor [3, tokens], next position of every
     sequence int32 [sequences])."""
-    span = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
-    cu = np.ascontiguousarray(cu_spans, dtype=np.int32)
+    span, cu = _spans(span_thw, cu_spans)
     used = np.maximum(span[:int(cu[-1])], _SPAN_LEAST).astype(np.int64)        # a text is n x 1 x 1 tokens
     tokens = int((used[:, 0] * used[:, 1] * used[:, 2]).sum())
     dev = torch.device(device) if out is None else out.device
@@ -670,20 +682,28 @@ class Rope:
                 raise ValueError("the elements of a head must be contiguous")
             return a, b
 
-        rows = [strides(x, x.shape) for x in tensors]
-        if out is None:
-            out = [torch.empty(x.shape, dtype=self.dtype, device=x.device) for x in tensors]
-        elif len(out) != len(tensors):
+        if out is not None and len(out) != len(tensors):
             raise ValueError("as many outputs as tensors")
-        arr = (epd_rope_tensor * len(tensors))()
-        for i, (x, y, r) in enumerate(zip(tensors, out, rows)):
-            arr[i] = (x.data_ptr(), y.data_ptr(), *r, *strides(y, x.shape), x.shape[1])
+        arr, made = (epd_rope_tensor * len(tensors))(), []
+        for i, x in enumerate(tensors):
+            shape = x.shape
+            si = strides(x, shape)
+            if out is None:
+                y, so = torch.empty(shape, dtype=self.dtype, device=x.device), (shape[1] * d, d)
+            else:
+                y, so = out[i], strides(out[i], shape)
+            made.append(y)
+            arr[i] = (x.data_ptr(), y.data_ptr(), *si, *so, shape[1])
         _on(dev, epd_rope_apply, self.cfg, arr, positions.data_ptr() or 256, positions.stride(0), T, inverse)
-        return list(out)
+        return made
 
 
 def epd_gated_mlp_workspace_bytes(cfg: epd_gated_mlp_cfg) -> int:
     return int(lib.epd_gated_mlp_workspace_bytes(C.byref(cfg)))
+
+
+def epd_gated_mlp_saved_bytes(cfg: epd_gated_mlp_cfg, tokens: int) -> int:
+    return int(lib.epd_gated_mlp_saved_bytes(C.byref(cfg), tokens))
 
 
 def epd_gated_mlp(cfg: epd_gated_mlp_cfg, weights: epd_gated_mlp_weights, x: int, ld_x: int, tokens: int, y: int, ld_y: int,
@@ -749,12 +769,12 @@ class GatedMLP:
         _on(self.device.index, on, *args)
 
     def forward(self, weights, x: torch.Tensor, save: bool = False, out: Optional[torch.Tensor] = None):
-        """x: [tokens, D], rows any stride apart.  Returns y, or (y, saved) with what ``backward`` needs."""
+        """x: [tokens, D], rows any stride apart.  Returns y, or (y, saved) with what ``backward`` needs (a uint8 tensor)."""
         px, ld_x = self._rows(x, "x")
         T = x.shape[0]
         y = torch.empty((T, self.hidden), dtype=self.dtype, device=self.device) if out is None else out
         py, ld_y = self._rows(y, "out", T)
-        saved = torch.empty((T, 2 * self.mlp_dim), dtype=torch.float32, device=self.device) if save else None
+        saved = torch.empty(epd_gated_mlp_saved_bytes(self.cfg, T), dtype=torch.uint8, device=self.device) if save else None
         self._call(epd_gated_mlp, self.cfg, self._weights(weights), px, ld_x, T, py, ld_y, None if saved is None else saved.data_ptr(), self._base,
                    self.workspace_bytes)
         return (y, saved) if save else y
@@ -764,7 +784,7 @@ class GatedMLP:
         px, ld_x = self._rows(x, "x")
         T = x.shape[0]
         pdy, ld_dy = self._rows(dy, "dy", T)
-        if saved.shape != (T, 2 * self.mlp_dim) or saved.dtype != torch.float32 or saved.device != self.device or not saved.is_contiguous():
+        if saved.dim() != 1 or saved.shape[0] != epd_gated_mlp_saved_bytes(self.cfg, T) or saved.dtype != torch.uint8 or saved.device != self.device or not saved.is_contiguous():
             raise ValueError("saved must be what forward returned for these rows")
         shapes = {"dx": (T, self.hidden), **self._shapes}
         grads, out = epd_gated_mlp_grads(), {}

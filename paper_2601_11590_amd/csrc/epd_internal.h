@@ -19,9 +19,10 @@ enum Epilogue : int {
                      // path stores V transposed into vt[(n - qk_cols)][vcol[m]].
   EPI_GATED = 4,     // W holds gate_rows gate rows, then as many up rows:
                      // out[m][c] = act(gate_c + bias_c) * (up_c + bias_(gate_rows + c));  bf16: N = 2 *
-                     // round_up(gate_rows, 16), fp32: N = 2 * gate_rows.  gu (if any) gets both factors
-  EPI_DGATED = 5     // acc = dH[m][c], N = gate_rows; from gu's G and U: dgu[m][c] = dH U act'(G),
-                     // dgu[m][gate_rows + c] = dH act(G), out[m][c] = act(G) U
+                     // round_up(gate_rows, 16), fp32: N = 2 * gate_rows.  bf16: keep_* (if any) get P = act(G) and
+                     // Q = U act'(G); fp32: gu (if any) gets G | U
+  EPI_DGATED = 5     // acc = dH[m][c], N = gate_rows; dgu[m][c] = dH Q, dgu[m][gate_rows + c] = dH P;
+                     // fp32: from gu, and out[m][c] = act(G) U
 };
 
 struct GemmArgs {
@@ -72,8 +73,9 @@ struct GemmArgs {
   int compute_units;    // bf16 path: compute units the launch will run on (a CU-masked stream); 0 = all of the device's
   // EPI_GATED, EPI_DGATED
   int gate_rows;        // channels c; bf16: a multiple of 8
-  void* gu;             // fp32 [M, ldgu]: pre-activations, G in columns [0, gate_rows), U behind it (EPI_GATED: written, or nullptr)
+  void* gu;             // fp32 path, [M, ldgu]: pre-activations, G in columns [0, gate_rows), U behind it (EPI_GATED: written, or nullptr)
   int ldgu;
+  void *keep_p, *keep_q, *keep_low;   // bf16 path, [M, gate_rows] of 2, 2 and 1 bytes (EPI_GATED: written, or nullptr)
   void* dgu;            // [M, lddgu] (EPI_DGATED)
   int lddgu;
   float* sums;          // EPI_DGATED, bf16 path: fp32 [rows of sums, 2 * gate_rows] or nullptr: sums of dG | dU over the rows of each wave,

@@ -5,12 +5,12 @@
 // Forward, many tokens: two products of the bf16 GEMM family.  The first makes gate and up columns of the same channels in
 // one tile and multiplies them where the accumulators stand (EPI_GATED), so that G and U never meet memory unless a backward
 // pass wants them.  Forward, few tokens: see few_tokens_kernel.
-// Backward, from dY and the saved G, U:
-//   dH = dY Wd;  dU = dH act(G), dG = dH U act'(G), H = act(G) U   in the epilogue of the first product (EPI_DGATED)
+// Backward, from dY and the saved H, P, Q (fp32: G, U):
+//   dH = dY Wd;  dU = dH P, dG = dH Q with the saved P = act(G), Q = U act'(G)   in the epilogue of the first product (EPI_DGATED)
 //   dX = dG Wg + dU Wu;  dWgu = (dG | dU)^T X;  dWd = dY^T H;  biases: column sums of dG | dU and dY
 // Every product is A W^T.  Where K runs along the rows of an operand the ping-pong loop reads it transposed from LDS; products
 // too small for its tiles have the operand turned by a kernel first, whichever the model prices lower.  Rounded to bf16 on the way, beside the outputs: H, dG and dU, each once, as operands of
-// matrix instructions; G and U are kept in fp32, sums are fp32 throughout.
+// matrix instructions; P and Q are kept in 20 bits (keep_channels), sums are fp32 throughout.
 #include "gemm_bf16_tile.h"
 #include "op_error.h"
 
@@ -26,8 +26,9 @@ namespace epd {
 // the waves.
 struct FewArgs {
   const void* X; const void* W; const void* bias;
-  void* out; void* gu;                 // gu: see GemmArgs (nullptr: not kept)
-  int ldx, ldo, ldgu, T, N, K, act;
+  void* out;
+  void *keep_p, *keep_q, *keep_low;    // see GemmArgs (nullptr: not kept)
+  int ldx, ldo, T, N, K, act;
 };
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_few;
@@ -104,12 +105,25 @@ __global__ __launch_bounds__(64 * NW) void few_tokens_kernel(FewArgs a) {
     }
     f32x4 o = v[0];
     if constexpr (GATED) {
+      float p[4], q[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = (a.act == 0 ? gate_act<0>(v[0][j]) : a.act == 1 ? gate_act<1>(v[0][j]) : gate_act<2>(v[0][j])) * v[S - 1][j];
-      if (a.gu) {
-        float* const gu = (float*)a.gu + (size_t)m * a.ldgu + n;
-        *(f32x4*)gu = v[0];
-        *(f32x4*)(gu + a.N) = v[S - 1];
+      for (int j = 0; j < 4; ++j) {
+        const float gate = v[0][j], up = v[S - 1][j];
+        if (a.keep_p) {
+          q[j] = (a.act == 0 ? gate_act_d<0>(gate, p[j]) : a.act == 1 ? gate_act_d<1>(gate, p[j]) : gate_act_d<2>(gate, p[j])) * up;
+          o[j] = p[j] * up;
+        } else {
+          o[j] = (a.act == 0 ? gate_act<0>(gate) : a.act == 1 ? gate_act<1>(gate) : gate_act<2>(gate)) * up;
+        }
+      }
+      if (a.keep_p) {
+        const size_t at = (size_t)m * a.N + n;
+        uint2 ph, qh;
+        uint32_t low;
+        keep_channels(p, q, ph, qh, low);
+        *(uint2*)((uint16_t*)a.keep_p + at) = ph;
+        *(uint2*)((uint16_t*)a.keep_q + at) = qh;
+        *(uint32_t*)((uint8_t*)a.keep_low + at) = low;
       }
     }
     *(uint2*)((uint16_t*)a.out + (size_t)m * a.ldo + n) = pack_bf16x4(o[0], o[1], o[2], o[3]);
@@ -251,7 +265,7 @@ static double product_cost(const ProductTile& t, long M, long N, double K, int k
 // One launch of the cheapest tile, or whole rounds of a large one and the rest of the rows in the cheapest for them:
 // 8192 x 3200 x 25 600 is 416 tiles of 256 x 256, priced two rounds (1075 us); 6080 rows in one round of 320 x 256 and 2112 in one of 256 x 128 take 980.
 static TilePlan plan_product(const GemmArgs& g, long cus) {
-  const int kind = g.epilogue == EPI_GATED ? (g.gu ? 2 : 1) : g.epilogue == EPI_DGATED ? 3 : 0;
+  const int kind = g.epilogue == EPI_GATED ? (g.keep_p ? 2 : 1) : g.epilogue == EPI_DGATED ? 3 : 0;
   auto best_tile = [&](long rows, double& cost) {
     int best = 0;
     cost = 1e300;
@@ -301,7 +315,11 @@ int launch_gemm_bf16_gated(const GemmArgs& args, hipStream_t s) {
   tail.A = (const __bf16*)g.A + (g.a_rows ? mb : mb * g.lda);
   tail.sum_row0 = g.sum_row0 + sum_rows(body);
   if (g.out) tail.out = (__bf16*)g.out + mb * g.ldo;
-  if (g.gu) tail.gu = (float*)g.gu + mb * g.ldgu;
+  if (g.keep_p) {
+    tail.keep_p = (uint16_t*)g.keep_p + mb * g.gate_rows;
+    tail.keep_q = (uint16_t*)g.keep_q + mb * g.gate_rows;
+    tail.keep_low = (uint8_t*)g.keep_low + mb * g.gate_rows;
+  }
   if (g.dgu) tail.dgu = (__bf16*)g.dgu + mb * g.lddgu;
   if (g.stats_in) tail.stats_in = g.stats_in + mb * g.stats_n;
   launch_gated_whole(body, s);
@@ -365,6 +383,20 @@ GatedLayout gated_layout(const epd_gated_mlp_cfg& c) {
   return L;
 }
 
+// What a forward call leaves for the backward pass.  bf16: H, P, Q and the bytes that P and Q share (keep_channels), [tokens, F]
+// each; fp32: G | U.
+struct Saved { void *h, *p, *q, *low; size_t total; };
+
+Saved saved_parts(const epd_gated_mlp_cfg& c, void* saved, int64_t tokens) {
+  const size_t n = (size_t)tokens * c.mlp_dim;
+  Saved s{saved, nullptr, nullptr, nullptr, 0};
+  if (c.dtype == EPD_F32) { s.total = n * 8; return s; }
+  const size_t part = (n * 2 + 255) / 256 * 256;
+  if (saved) { s.p = (char*)saved + part; s.q = (char*)saved + 2 * part; s.low = (char*)saved + 3 * part; }
+  s.total = 3 * part + n;
+  return s;
+}
+
 constexpr int kMaxTokens = 1 << 22;      // and leading dimensions: 320 rows stay below 2^32 bytes
 
 epd_status check_cfg(const char* who, const epd_gated_mlp_cfg* c) {
@@ -426,6 +458,12 @@ uint64_t epd_gated_mlp_workspace_bytes(const epd_gated_mlp_cfg* cfg) {
   return gated_layout(*cfg).total;
 }
 
+uint64_t epd_gated_mlp_saved_bytes(const epd_gated_mlp_cfg* cfg, int32_t tokens) {
+  if (check_cfg("epd_gated_mlp_saved_bytes", cfg) != EPD_OK) return 0;
+  if (tokens < 0 || tokens > cfg->max_tokens) { op_fail(EPD_ERR_SHAPE, "epd_gated_mlp_saved_bytes: tokens %d: 0 .. max_tokens %d", tokens, cfg->max_tokens); return 0; }
+  return saved_parts(*cfg, nullptr, tokens).total;
+}
+
 epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weights* w, const void* x, int64_t ld_x, int32_t tokens, void* y, int64_t ld_y,
                          void* saved, void* workspace, uint64_t workspace_bytes, void* stream) {
   const char* const who = "epd_gated_mlp";
@@ -438,12 +476,13 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
   const GatedLayout L = gated_layout(c);
   const bool bf = c.dtype == EPD_BF16;
   const int D = c.hidden, F = c.mlp_dim, T = tokens;
-  void* const H = (char*)workspace + L.h;
+  const Saved keep = saved_parts(c, saved, T);
+  void* const H = bf && saved ? keep.h : (char*)workspace + L.h;
   hipStream_t st = (hipStream_t)stream;
   if (bf && T <= kFewTokens) {
-    FewArgs a{x, w->gate_up_w, c.use_bias ? w->gate_up_b : nullptr, H, saved, (int)ld_x, F, 2 * F, T, F, D, act_code(c)};
+    FewArgs a{x, w->gate_up_w, c.use_bias ? w->gate_up_b : nullptr, H, keep.p, keep.q, keep.low, (int)ld_x, F, T, F, D, act_code(c)};
     hipError_t e = launch_few<4, 4, true>(a, st);
-    FewArgs b{H, w->down_w, c.use_bias ? w->down_b : nullptr, y, nullptr, F, (int)ld_y, 0, T, D, F, 0};
+    FewArgs b{H, w->down_w, c.use_bias ? w->down_b : nullptr, y, nullptr, nullptr, nullptr, F, (int)ld_y, T, D, F, 0};
     if (e == hipSuccess) e = launch_few<8, 4, false>(b, st);
     if (e != hipSuccess) return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e));
     return EPD_OK;
@@ -451,7 +490,9 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
   GemmArgs up{}, down{};
   up.A = x; up.lda = (int)ld_x; up.W = w->gate_up_w; up.ldw = D; up.bias = c.use_bias ? w->gate_up_b : nullptr;
   up.M = T; up.N = bf ? (F + 15) / 16 * 32 : 2 * F; up.K = D; up.epilogue = EPI_GATED; up.act = act_code(c);
-  up.gate_rows = F; up.out = H; up.ldo = F; up.gu = saved; up.ldgu = 2 * F;
+  up.gate_rows = F; up.out = H; up.ldo = F;
+  if (bf) { up.keep_p = keep.p; up.keep_q = keep.q; up.keep_low = keep.low; }
+  else { up.gu = saved; up.ldgu = 2 * F; }
   down.A = H; down.lda = F; down.W = w->down_w; down.ldw = F; down.bias = c.use_bias ? w->down_b : nullptr;
   down.M = T; down.N = D; down.K = F; down.epilogue = EPI_STORE; down.out = y; down.ldo = (int)ld_y;
   hipError_t e;
@@ -503,11 +544,14 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
   const GatedLayout L = gated_layout(c);
   char* const ws = (char*)workspace;
   const int T = tokens, iD = c.hidden, iF = c.mlp_dim;
-  const bool want_gu = grads->gate_up_w || grads->gate_up_b, want_h = grads->dx || want_gu || grads->down_w;
-  // dH = dY Wd, and at once dG, dU and H
+  const bool want_gu = grads->gate_up_w || grads->gate_up_b, want_h = grads->dx || want_gu || (!bf && grads->down_w);
+  // dH = dY Wd, and at once dG and dU (fp32: and H)
   GemmArgs dh{}, dx{}, dgu{}, dd{};
   dh.A = dy; dh.lda = (int)ld_dy; dh.M = T; dh.N = iF; dh.K = iD; dh.epilogue = EPI_DGATED; dh.act = act_code(c);
-  dh.gate_rows = iF; dh.gu = (void*)saved; dh.ldgu = 2 * iF; dh.dgu = ws + L.dgu; dh.lddgu = 2 * iF; dh.out = ws + L.h; dh.ldo = iF;
+  dh.gate_rows = iF; dh.dgu = ws + L.dgu; dh.lddgu = 2 * iF;
+  const Saved keep = saved_parts(c, (void*)saved, T);
+  if (bf) { dh.keep_p = keep.p; dh.keep_q = keep.q; dh.keep_low = keep.low; }
+  else { dh.gu = (void*)saved; dh.ldgu = 2 * iF; dh.out = ws + L.h; dh.ldo = iF; }
   // dX = (dG | dU) Wgu,  dWgu = (dG | dU)^T X,  dWd = dY^T H
   dx.A = ws + L.dgu; dx.lda = 2 * iF; dx.M = T; dx.N = iD; dx.K = 2 * iF; dx.epilogue = EPI_STORE; dx.out = grads->dx; dx.ldo = (int)grads->ld_dx;
   dgu.M = 2 * iF; dgu.N = iD; dgu.epilogue = EPI_STORE; dgu.out = grads->gate_up_w; dgu.ldo = iD;
@@ -515,7 +559,7 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
   dh.W = w->down_w; dh.ldw = iF; dh.w_rows = 1;
   dx.W = w->gate_up_w; dx.ldw = iD; dx.w_rows = 1;
   dgu.A = ws + L.dgu; dgu.lda = 2 * iF; dgu.a_rows = 1; dgu.W = x; dgu.ldw = (int)ld_x; dgu.w_rows = 1; dgu.K = T;
-  dd.A = dy; dd.lda = (int)ld_dy; dd.a_rows = 1; dd.W = ws + L.h; dd.ldw = iF; dd.w_rows = 1; dd.K = T;
+  dd.A = dy; dd.lda = (int)ld_dy; dd.a_rows = 1; dd.W = bf ? keep.h : ws + L.h; dd.ldw = iF; dd.w_rows = 1; dd.K = T;
   if (!bf) {
     F32Group a{}, b{};
     a.n = 1; a.g[0] = dh;

@@ -115,6 +115,26 @@ template <int ACT> __device__ __forceinline__ float gate_act_d(float g, float& a
   }
 }
 
+// What the backward pass of a gated MLP needs of a channel beside H: P = act(G) and Q = U act'(G), dU = dH P and dG = dH Q.
+// Each is kept in 20 bits, an fp32 value rounded to 11 bits of mantissa: the upper 16 in an array of its own, four more of P and Q
+// together in a byte.  5 bytes a channel at 2^-12, where bf16 would be 4 and cost the gradients half as much again (3.5e-3 of
+// their norm, 2.3e-3 this way) and fp32 8.
+__device__ __forceinline__ uint32_t keep20(float x) { return __float_as_uint(x) + 0x800u; }
+__device__ __forceinline__ void keep_channels(const float* p, const float* q, uint2& ph, uint2& qh, uint32_t& low) {
+  uint32_t a[4], b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { a[i] = keep20(p[i]); b[i] = keep20(q[i]); }
+  ph = make_uint2(a[0] >> 16 | (a[1] & 0xffff0000u), a[2] >> 16 | (a[3] & 0xffff0000u));
+  qh = make_uint2(b[0] >> 16 | (b[1] & 0xffff0000u), b[2] >> 16 | (b[3] & 0xffff0000u));
+  low = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) low |= ((a[i] >> 12 & 15u) | (b[i] >> 8 & 0xf0u)) << (8 * i);
+}
+__device__ __forceinline__ float kept_channel(uint2 high, uint32_t low, int i, int shift) {       // shift: 0 for P, 4 for Q
+  const uint32_t h = i < 2 ? high.x : high.y;
+  return __uint_as_float((i & 1 ? h & 0xffff0000u : h << 16) | (low >> (8 * i + shift) & 15u) << 12);
+}
+
 enum OutKind : int { OUT_BF16 = 0, OUT_F32 = 1 };
 
 // Sum over aligned groups of G = 8 or 16 consecutive lanes; every lane of a group gets the sum.
@@ -638,8 +658,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
   using LAST = std::integral_constant<int, NSL - 1>;
 
   // What the epilogue adds to or multiplies with the accumulators of a 16-token block: as many fp32 values as it has --
-  // of the residual rows (EPI_RESIDUAL, lanes along rows), or cos and sin of the lane's rotary pairs (EPI_QKV), or G and U
-  // (EPI_DGATED, lanes along rows; the latter in aux_u).
+  // of the residual rows (EPI_RESIDUAL, lanes along rows), or cos and sin of the lane's rotary pairs (EPI_QKV), or what is kept
+  // of the channels (EPI_DGATED, lanes along rows: P and Q in aux, what they share in aux_low).
   // Where all of it is at most 16 loads they are issued behind the last stage hand-over, so that they
   // overlap the last K step; otherwise AUX blocks are kept in flight through the epilogue.
   //   A rotary table that comes through LDS (`table`) needs none of these loads: issued all the same, and waited for
@@ -652,20 +672,26 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
   [[maybe_unused]] constexpr bool ROT_TABLE = HAS_AUX && EPI == EPI_QKV && T::PINGPONG;
   [[maybe_unused]] constexpr int TAB_BYTES = T::LDS_BYTES - T::WAVES_M * T::WAVES_N * 16 * WN * 2;   // what the bf16 staging pieces leave
   const bool table = ROT_TABLE && g.rot && g.rot_lds && BM * g.rot_pairs * 8 <= TAB_BYTES;
-  constexpr int AUX = PREF ? TM16 : EPI == EPI_DGATED ? 2 : BM > 256 ? (EPI == EPI_QKV ? 2 : 3) : 4;
-  [[maybe_unused]] float4 aux[HAS_AUX ? AUX : 1][TN16], aux_u[EPI == EPI_DGATED ? AUX : 1][TN16];
+  constexpr int AUX = PREF ? TM16 : EPI == EPI_DGATED ? (BM > 256 ? 2 : 3) : BM > 256 ? (EPI == EPI_QKV ? 2 : 3) : 4;
+  [[maybe_unused]] float4 aux[HAS_AUX ? AUX : 1][TN16];
+  [[maybe_unused]] uint32_t aux_low[EPI == EPI_DGATED ? AUX : 1][TN16];
   const int rows_left = max(0, min(WM, g.M - m0 - wm * WM));       // rows of the wave's tile that exist
-  [[maybe_unused]] const uint32_t aux_pitch = EPI == EPI_QKV ? (uint32_t)g.rot_pairs * 8u : (uint32_t)(EPI == EPI_DGATED ? g.ldgu : g.ldr) * 4u;
+  [[maybe_unused]] const uint32_t aux_pitch = EPI == EPI_QKV ? (uint32_t)g.rot_pairs * 8u : EPI == EPI_DGATED ? (uint32_t)g.gate_rows * 2u : (uint32_t)g.ldr * 4u;
   [[maybe_unused]] uint32_t aux_off[EPI == EPI_QKV ? TN16 : 1];
-  [[maybe_unused]] __amdgpu_buffer_rsrc_t aux_rows;
+  [[maybe_unused]] __amdgpu_buffer_rsrc_t aux_rows, aux_q, aux_l;
+  if constexpr (EPI == EPI_DGATED) {
+    const size_t at = (size_t)(m0 + wm * WM) * g.gate_rows, n = (size_t)rows_left * g.gate_rows;
+    aux_q = row_window((const uint16_t*)g.keep_q + at, n * 2);
+    aux_l = row_window((const uint8_t*)g.keep_low + at, n);
+  }
   if constexpr (HAS_AUX) {
-    aux_rows = row_window((EPI == EPI_QKV ? (const char*)g.rot : EPI == EPI_DGATED ? (const char*)g.gu : (const char*)g.resid) + (size_t)(m0 + wm * WM) * aux_pitch, (size_t)rows_left * aux_pitch);
+    aux_rows = row_window((EPI == EPI_QKV ? (const char*)g.rot : EPI == EPI_DGATED ? (const char*)g.keep_p : (const char*)g.resid) + (size_t)(m0 + wm * WM) * aux_pitch, (size_t)rows_left * aux_pitch);
     if constexpr (EPI == EPI_QKV) {
 #pragma unroll
       for (int w = 0; w < TN16; ++w) aux_off[w] = (uint32_t)l16 * aux_pitch + (uint32_t)(((n0 + wn * WN + w * 16 + g4 * 4) % g.head_dim) >> 1) * 8u;
     } else {
       const int n = n0 + wn * WN + (lane % FC) * 4;
-      aux_off[0] = n < g.N ? (uint32_t)(lane / FC) * aux_pitch + (uint32_t)n * 4u : OUTSIDE;
+      aux_off[0] = n < g.N ? (uint32_t)(lane / FC) * aux_pitch + (uint32_t)n * (EPI == EPI_DGATED ? 2u : 4u) : OUTSIDE;
     }
   }
   auto load_aux = [&](int b) {
@@ -673,8 +699,13 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
 #pragma unroll
       for (int w = 0; w < TN16; ++w) {
         const uint32_t off = aux_off[EPI == EPI_QKV ? w : 0] + (uint32_t)(b * 16 + (EPI == EPI_QKV ? 0 : w * FR)) * aux_pitch;
-        aux[b % AUX][w] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(aux_rows, off, 0, 0));
-        if constexpr (EPI == EPI_DGATED) aux_u[b % AUX][w] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(aux_rows, off, (uint32_t)g.gate_rows * 4u, 0));
+        if constexpr (EPI == EPI_DGATED) {
+          const float2 ph = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(aux_rows, off, 0, 0)), qh = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(aux_q, off, 0, 0));
+          aux[b % AUX][w] = make_float4(ph.x, ph.y, qh.x, qh.y);
+          aux_low[b % AUX][w] = __builtin_amdgcn_raw_buffer_load_b32(aux_l, (off & OUTSIDE) | (off & ~OUTSIDE) >> 1, 0, 0);
+        } else {
+          aux[b % AUX][w] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(aux_rows, off, 0, 0));
+        }
       }
     }
   };
@@ -1040,8 +1071,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
     // rotary 22 k -> 16 k (its table: 64-byte pieces of rows, half the address unit's rate), plain store 6.0 k -> 3.9 k.
     constexpr bool F32_ROWS = EPI == EPI_RESIDUAL || EPI == EPI_DGATED || OUT == OUT_F32;
     constexpr int SROW = WN * (F32_ROWS ? 4 : 2), CH = SROW / 16, RPI = 64 / CH;   // bytes and 16-byte chunks per staged row, rows per read
-    // EPI_GATED: rows of WN / 2 channels, of H in bf16 and, where they are saved, of G and U in fp32
-    constexpr int STG_BYTES = T::WAVES_M * T::WAVES_N * 16 * (GATED ? WN / 2 * 10 : SROW);
+    // EPI_GATED: rows of WN / 2 channels, of H and, where the channels are kept, 5 bytes of each
+    constexpr int STG_BYTES = T::WAVES_M * T::WAVES_N * 16 * (GATED ? WN / 2 * 7 : SROW);
     static_assert(STG_BYTES + T::WAVES_N * BM * 4 <= T::LDS_BYTES, "staging area");
     if constexpr (BIAS_USED && !BIAS_PRE) load_bias();
     __builtin_amdgcn_s_barrier();                        // the operand stages are dead from here on (all reads of them were waited for)
@@ -1050,31 +1081,30 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
     auto schunk = [](int row, int c) { return row * SROW + ((SROW == 256 ? c ^ row : SROW == 128 ? c ^ T::swz(row) : c ^ ((row >> 2) & 3)) * 16); };
     if constexpr (GATED) {
       // A lane holds both factors of four channels of one token in every two 16-column blocks: H leaves as rows of WN / 2
-      // channels.  64-byte rows go through LDS, 16 bytes a lane, and with them G and U where they are kept for the backward
-      // pass (in fp32: rounded to bf16 they would cost the gradients more than all their other roundings, 3.5e-3 of
-      // their norm where it is 2.3e-3); rows of WN = 32 leave from where the accumulators stand, which touches as many pieces.
+      // channels.  64-byte rows go through LDS, 16 bytes a lane, and with them what is kept for the backward pass; rows of WN = 32
+      // leave from where the accumulators stand, which touches as many pieces.
       constexpr int Q = TN16 / 2, CW = WN / 2;
       constexpr bool STAGED = CW == 32;
       static_assert(CW == 32 || CW == 16, "gated rows");
-      char* const hp = lds + wave * 16 * CW * 10;
-      char* const sp = hp + 16 * CW * 2;                                // G, then U
-      auto h_at = [](int row, int c) { return row * 64 + ((c ^ ((row >> 2) & 3)) * 16); };
-      auto s_at = [](int row, int c) { return row * 128 + ((c ^ T::swz(row)) * 16); };
+      char* const piece = lds + wave * 16 * CW * 7;                     // H, P, Q: 16 rows of 64 bytes each; the shared bytes: 16 of 32
+      auto at = [](int row, int c) { return row * 64 + ((c ^ ((row >> 2) & 3)) * 16); };
       const int c0 = (n0 + wn * WN) / 2;
-      const uint32_t h_pitch = (uint32_t)g.ldo * 2u, s_pitch = (uint32_t)g.ldgu * 4u, up_off = (uint32_t)g.gate_rows * 4u;
-      // first channel and token (of 16, 8) of the lane's stores; gate_rows is a multiple of 8: all or nothing
-      const int hc = c0 + (STAGED ? (lane & 3) * 8 : g4 * 4), hr = STAGED ? lane >> 2 : l16;
-      const int sc = c0 + (STAGED ? (lane & 7) * 4 : g4 * 4), sr = STAGED ? lane >> 3 : l16;
-      const uint32_t h_off = hc < g.gate_rows ? (uint32_t)hr * h_pitch + (uint32_t)hc * 2u : OUTSIDE, s_off = sc < g.gate_rows ? (uint32_t)sr * s_pitch + (uint32_t)sc * 4u : OUTSIDE;
+      // first channel and token (of 16) of the lane's stores, 8 channels staged and 4 direct; gate_rows is a multiple of 8: all or nothing
+      const int cs = c0 + (STAGED ? (lane & 3) * 8 : g4 * 4), rl = STAGED ? lane >> 2 : l16;
+      const bool in = cs < g.gate_rows;
+      const uint32_t h_pitch = (uint32_t)g.ldo * 2u, k_pitch = (uint32_t)g.gate_rows;
+      const uint32_t h_off = in ? (uint32_t)rl * h_pitch + (uint32_t)cs * 2u : OUTSIDE, k_off = in ? (uint32_t)rl * k_pitch + (uint32_t)cs : OUTSIDE / 2;
+      const size_t k_at = (size_t)(m0 + wm * WM) * k_pitch, k_n = g.keep_p ? (size_t)rows_left * k_pitch : 0;
       const __amdgpu_buffer_rsrc_t h_rows = row_window((const char*)g.out + (size_t)(m0 + wm * WM) * h_pitch, (size_t)rows_left * h_pitch);
-      const __amdgpu_buffer_rsrc_t s_rows = row_window((const char*)g.gu + (size_t)(m0 + wm * WM) * s_pitch, g.gu ? (size_t)rows_left * s_pitch : 0);
+      const __amdgpu_buffer_rsrc_t p_rows = row_window((const uint16_t*)g.keep_p + k_at, k_n * 2), q_rows = row_window((const uint16_t*)g.keep_q + k_at, k_n * 2);
+      const __amdgpu_buffer_rsrc_t l_rows = row_window((const uint8_t*)g.keep_low + k_at, k_n);
       float bias[TN16][4];
 #pragma unroll
       for (int w = 0; w < TN16; ++w) {
         bias[w][0] = bf16_bits_to_float(bb[w].x & 0xffff); bias[w][1] = bf16_bits_to_float(bb[w].x >> 16);
         bias[w][2] = bf16_bits_to_float(bb[w].y & 0xffff); bias[w][3] = bf16_bits_to_float(bb[w].y >> 16);
       }
-      // ACT x whether G and U are kept: outside of the loops, one block of code each
+      // ACT x whether the channels are kept: outside of the loops, one block of code each
       auto rows = [&](auto ACT, auto SAVE) {
         constexpr bool save = decltype(SAVE)::value;
 #pragma unroll
@@ -1083,40 +1113,49 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
 #pragma unroll
           for (int q = 0; q < Q; ++q) {
             const f32x4 ga = acc[b >> 1][q][(b & 1) * 2], ua = acc[b >> 1][q][(b & 1) * 2 + 1];
-            f32x4 gv, uv;
-            float hv[4];
+            float hv[4], pv[4], qv[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-              gv[v] = fmaf(ga[v], rs, bias[2 * q][v]);
-              uv[v] = fmaf(ua[v], rs, bias[2 * q + 1][v]);
-              hv[v] = gate_act<decltype(ACT)::value>(gv[v]) * uv[v];
+              const float gate = fmaf(ga[v], rs, bias[2 * q][v]), up = fmaf(ua[v], rs, bias[2 * q + 1][v]);
+              if constexpr (save) {
+                qv[v] = gate_act_d<decltype(ACT)::value>(gate, pv[v]) * up;
+                hv[v] = pv[v] * up;
+              } else {
+                hv[v] = gate_act<decltype(ACT)::value>(gate) * up;
+              }
             }
             const uint2 h = pack_bf16x4(hv[0], hv[1], hv[2], hv[3]);
+            [[maybe_unused]] uint2 ph, qh;
+            [[maybe_unused]] uint32_t low;
+            if constexpr (save) keep_channels(pv, qv, ph, qh, low);
             if constexpr (STAGED) {
-              *(uint2*)(hp + h_at(l16, q * 2 + (g4 >> 1)) + (g4 & 1) * 8) = h;
+              char* const to = piece + at(l16, q * 2 + (g4 >> 1)) + (g4 & 1) * 8;
+              *(uint2*)to = h;
               if constexpr (save) {
-                *(f32x4*)(sp + s_at(l16, q * 4 + g4)) = gv;
-                *(f32x4*)(sp + 16 * CW * 4 + s_at(l16, q * 4 + g4)) = uv;
+                *(uint2*)(to + 1024) = ph;
+                *(uint2*)(to + 2048) = qh;
+                *(uint32_t*)(piece + 3072 + l16 * 32 + q * 16 + g4 * 4) = low;
               }
             } else {
               __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, h), h_rows, h_off + (uint32_t)(b * 16) * h_pitch, 0, 0);
               if constexpr (save) {
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, gv), s_rows, s_off + (uint32_t)(b * 16) * s_pitch, 0, 0);
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, uv), s_rows, s_off + (uint32_t)(b * 16) * s_pitch, up_off, 0);
+                __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, ph), p_rows, 2 * (k_off + (uint32_t)(b * 16) * k_pitch), 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, qh), q_rows, 2 * (k_off + (uint32_t)(b * 16) * k_pitch), 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b32(low, l_rows, k_off + (uint32_t)(b * 16) * k_pitch, 0, 0);
               }
             }
           }
           if constexpr (STAGED) {
             asm volatile("" ::: "memory");     // other lanes' pieces are read below: LDS takes a wave's accesses in order
-            const uint4 h = *(const uint4*)(hp + h_at(hr, lane & 3));
+            const char* const from = piece + at(rl, lane & 3);
+            const uint4 h = *(const uint4*)from;
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, h), h_rows, h_off + (uint32_t)(b * 16) * h_pitch, 0, 0);
             if constexpr (save) {
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const uint4 gv = *(const uint4*)(sp + s_at(k * 8 + sr, lane & 7)), uv = *(const uint4*)(sp + 16 * CW * 4 + s_at(k * 8 + sr, lane & 7));
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, gv), s_rows, s_off + (uint32_t)(b * 16 + k * 8) * s_pitch, 0, 0);
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, uv), s_rows, s_off + (uint32_t)(b * 16 + k * 8) * s_pitch, up_off, 0);
-              }
+              const uint4 ph = *(const uint4*)(from + 1024), qh = *(const uint4*)(from + 2048);
+              const uint2 low = *(const uint2*)(piece + 3072 + rl * 32 + (lane & 3) * 8);
+              __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, ph), p_rows, 2 * (k_off + (uint32_t)(b * 16) * k_pitch), 0, 0);
+              __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, qh), q_rows, 2 * (k_off + (uint32_t)(b * 16) * k_pitch), 0, 0);
+              __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, low), l_rows, k_off + (uint32_t)(b * 16) * k_pitch, 0, 0);
             }
             asm volatile("" ::: "memory");
           }
@@ -1128,57 +1167,49 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
         else if (g.act == 1) rows(std::integral_constant<int, 1>{}, SAVE);
         else rows(std::integral_constant<int, 2>{}, SAVE);
       };
-      if (g.gu) by_act(std::true_type{});
+      if (g.keep_p) by_act(std::true_type{});
       else by_act(std::false_type{});
     } else if constexpr (EPI == EPI_DGATED) {
-      // Rows of dH, turned as in the residual add below, meet the rows of G and U: a lane has four channels of a token and
-      // leaves dG, dU and H there, 8 bytes each, 128 (64) bytes a row: 14 bytes per value, HBM paces it where all
+      // Rows of dH, turned as in the residual add below, meet what was kept of the channels: a lane has four of a token and
+      // leaves dG = dH Q and dU = dH P there, 8 bytes each, 128 (64) bytes a row: 9 bytes per value, HBM paces it where all
       // units are at it.
       const int n = n0 + wn * WN + (lane % FC) * 4;
-      const uint32_t d_pitch = (uint32_t)g.lddgu * 2u, h_pitch = (uint32_t)g.ldo * 2u;
-      const uint32_t d_off = n < g.N ? (uint32_t)(lane / FC) * d_pitch + (uint32_t)n * 2u : OUTSIDE, h_off = n < g.N ? (uint32_t)(lane / FC) * h_pitch + (uint32_t)n * 2u : OUTSIDE;
+      const uint32_t d_pitch = (uint32_t)g.lddgu * 2u;
+      const uint32_t d_off = n < g.N ? (uint32_t)(lane / FC) * d_pitch + (uint32_t)n * 2u : OUTSIDE;
       const __amdgpu_buffer_rsrc_t d_rows = row_window((const char*)g.dgu + (size_t)(m0 + wm * WM) * d_pitch, (size_t)rows_left * d_pitch);
-      const __amdgpu_buffer_rsrc_t h_rows = row_window((const char*)g.out + (size_t)(m0 + wm * WM) * h_pitch, (size_t)rows_left * h_pitch);
       const uint32_t up_off = (uint32_t)g.gate_rows * 2u;
       f32x4 sum_g = {0.f, 0.f, 0.f, 0.f}, sum_u = {0.f, 0.f, 0.f, 0.f};       // over the lane's rows, of dG and dU before they are rounded
-      auto rows = [&](auto ACT) {
-        if constexpr (!PREF) {
+      if constexpr (!PREF) {
 #pragma unroll
-          for (int b = 0; b < AUX; ++b) load_aux(b);
+        for (int b = 0; b < AUX; ++b) load_aux(b);
+      }
+#pragma unroll
+      for (int b = 0; b < TM16; ++b) {
+#pragma unroll
+        for (int w = 0; w < TN16; ++w) {
+          const f32x4 a = acc[b >> 1][w >> 1][(b & 1) * 2 + (w & 1)];
+          *(float4*)(stg + schunk(l16, w * 4 + g4)) = make_float4(a[0], a[1], a[2], a[3]);
         }
+        asm volatile("" ::: "memory");
 #pragma unroll
-        for (int b = 0; b < TM16; ++b) {
+        for (int w = 0; w < TN16; ++w) {
+          const int c = b * TN16 + w;                    // rows c * FR + lane / FC of the wave's tile
+          const float4 e = *(const float4*)(stg + schunk(w * FR + lane / FC, lane % FC)), kept = aux[b % AUX][w];
+          const bool live = c * FR + lane / FC < rows_left;    // rows past the last one repeat it
+          const f32x4 dh = live ? __builtin_bit_cast(f32x4, e) : f32x4{0.f, 0.f, 0.f, 0.f};
+          const uint2 ph = make_uint2(__float_as_uint(kept.x), __float_as_uint(kept.y)), qh = make_uint2(__float_as_uint(kept.z), __float_as_uint(kept.w));
+          float dg[4], du[4];
 #pragma unroll
-          for (int w = 0; w < TN16; ++w) {
-            const f32x4 a = acc[b >> 1][w >> 1][(b & 1) * 2 + (w & 1)];
-            *(float4*)(stg + schunk(l16, w * 4 + g4)) = make_float4(a[0], a[1], a[2], a[3]);
+          for (int v = 0; v < 4; ++v) {
+            dg[v] = dh[v] * kept_channel(qh, aux_low[b % AUX][w], v, 4); du[v] = dh[v] * kept_channel(ph, aux_low[b % AUX][w], v, 0);
+            sum_g[v] += dg[v]; sum_u[v] += du[v];
           }
-          asm volatile("" ::: "memory");
-#pragma unroll
-          for (int w = 0; w < TN16; ++w) {
-            const int c = b * TN16 + w;                  // rows c * FR + lane / FC of the wave's tile
-            const float4 e = *(const float4*)(stg + schunk(w * FR + lane / FC, lane % FC));
-            const bool live = c * FR + lane / FC < rows_left;    // rows past the last one repeat it
-            const f32x4 dh = live ? __builtin_bit_cast(f32x4, e) : f32x4{0.f, 0.f, 0.f, 0.f}, gv = __builtin_bit_cast(f32x4, aux[b % AUX][w]), uv = __builtin_bit_cast(f32x4, aux_u[b % AUX][w]);
-            float dg[4], du[4], hv[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              float act;
-              const float d = gate_act_d<decltype(ACT)::value>(gv[v], act);
-              dg[v] = dh[v] * uv[v] * d; du[v] = dh[v] * act; hv[v] = act * uv[v];
-              sum_g[v] += dg[v]; sum_u[v] += du[v];
-            }
-            __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, pack_bf16x4(dg[0], dg[1], dg[2], dg[3])), d_rows, d_off + (uint32_t)(c * FR) * d_pitch, 0, 0);
-            __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, pack_bf16x4(du[0], du[1], du[2], du[3])), d_rows, d_off + (uint32_t)(c * FR) * d_pitch, up_off, 0);
-            __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, pack_bf16x4(hv[0], hv[1], hv[2], hv[3])), h_rows, h_off + (uint32_t)(c * FR) * h_pitch, 0, 0);
-          }
-          if constexpr (!PREF) { if (b + AUX < TM16) load_aux(b + AUX); }
-          asm volatile("" ::: "memory");
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, pack_bf16x4(dg[0], dg[1], dg[2], dg[3])), d_rows, d_off + (uint32_t)(c * FR) * d_pitch, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, pack_bf16x4(du[0], du[1], du[2], du[3])), d_rows, d_off + (uint32_t)(c * FR) * d_pitch, up_off, 0);
         }
-      };
-      if (g.act == 0) rows(std::integral_constant<int, 0>{});
-      else if (g.act == 1) rows(std::integral_constant<int, 1>{});
-      else rows(std::integral_constant<int, 2>{});
+        if constexpr (!PREF) { if (b + AUX < TM16) load_aux(b + AUX); }
+        asm volatile("" ::: "memory");
+      }
       if (g.sums) {                                      // column sums of the wave's rows, one row of `sums` each
 #pragma unroll
         for (int o = FC; o < 64; o *= 2)

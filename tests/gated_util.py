@@ -55,8 +55,9 @@ def reference(name, w, x, dy=None):
     dh = dy @ wd
     edh = gamma(D) * (dy.abs() @ wd.abs())
     du, dg, hid = dh * a, dh * u * d, a * u
-    edu = edh * a.abs() + dh.abs() * ea + store * du.abs()
-    edg = edh * (u * d).abs() + dh.abs() * (eu * d.abs() + u.abs() * ed) + store * dg.abs()
+    kept = 2.0 ** -12 if dt == torch.bfloat16 else 0.0       # act(G) and U act'(G), saved with 12 bits of mantissa
+    edu = edh * a.abs() + dh.abs() * (ea + kept * a.abs()) + store * du.abs()
+    edg = edh * (u * d).abs() + dh.abs() * (eu * d.abs() + u.abs() * ed + kept * (u * d).abs()) + store * dg.abs()
     eh = ea * u.abs() + a.abs() * eu + store * hid.abs()
     dgu, edgu = torch.cat([dg, du], 1), torch.cat([edg, edu], 1)
 

@@ -244,6 +244,15 @@ def test_gated_mlp_workspace():
     assert 32768 * 12800 * 2 < big < 32768 * (12800 * 16 + 3200 * 8) + 3200 * 12800 * 8
 
 
+def test_gated_mlp_saved_bytes():
+    assert B.epd_gated_mlp_saved_bytes(mlp_cfg(), 10) == 3 * 10 * 128 * 2 + 10 * 128
+    assert B.epd_gated_mlp_saved_bytes(mlp_cfg(mlp_dim=8), 3) == 3 * 256 + 24
+    assert B.epd_gated_mlp_saved_bytes(mlp_cfg(dtype=B.EPD_F32), 10) == 10 * 128 * 8
+    assert B.epd_gated_mlp_saved_bytes(mlp_cfg(), 0) == 0
+    for c, t in ((mlp_cfg(act=0), 1), (mlp_cfg(), 101), (mlp_cfg(), -1)):
+        assert B.epd_gated_mlp_saved_bytes(c, t) == 0 and B.epd_op_last_error()
+
+
 def test_encoder_takes_gated_activations_only_by_their_names():
     from paper_2601_11590_amd import workloads as W
     cfg = W.EncoderConfig(name="t", dtype="bf16", num_layers=1, hidden=64, num_heads=1, head_dim=64, mlp_dim=128, patch=4, temporal_patch=1, norm="rmsnorm",
