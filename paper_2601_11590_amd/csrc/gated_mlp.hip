@@ -20,10 +20,13 @@ namespace epd {
 
 // ------------------------------------------------------------------------------ few tokens
 // out[t][n] = sum_k X[t][k] W[n][k] (+ bias), t < 16 NB; GATED: W's rows n and N + n are the gate and up rows of channel n, and
-// out = act(gate) * up.  Bound: HBM, every weight is read once; so nothing is staged: a lane's 16 bytes of a row of W
-// are its operand of the matrix instruction as they come.  A block makes 16 rows of W for all tokens, its waves take K in
-// turn, 64 at a time (whole 128-byte lines of the rows), U turns of loads at once, and their sums meet in LDS in the order of
-// the waves.
+// out = act(gate) * up.  Bound: HBM, every weight is read once.  A block makes 16 rows of W (of both halves) for all tokens; its
+// waves take K in turn, 64 at a time, each with a ring of S stages of its own in LDS, which direct loads of 8 rows x 128 bytes
+// fill and nobody else reads, so no wave waits for another until their sums meet, in the order of the waves.
+//   What it replaced loaded the operands of the matrix instructions straight to registers, 16 rows x 64 bytes an instruction: half
+// lines of twice as many rows, at 4.1 TB/s where whole lines reach 5.2 (3200 x 12 800, one token: gate and up 40.2 -> 31.7 us, down
+// 22.4 -> 16.8; 16 tokens 52 -> 33.6 and 32 -> 20.7; 64 tokens 90 -> 48 and 70 -> 36; a plain stream of 164 MB takes 29 ... 32 us).  The
+// GEMM's tiles take 46 and 57 us from 64 tokens down, so this one serves up to 64.
 struct FewArgs {
   const void* X; const void* W; const void* bias;
   void* out;
@@ -31,69 +34,103 @@ struct FewArgs {
   int ldx, ldo, T, N, K, act;
 };
 
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_few;
+// N blocks of 16 rows x 64 k of a stage: f[2 * block + k half]; one asm block with its wait, as read_frags
+#define EPD_DSR(d, a, o) "ds_read_b128 %" #d ", %" #a " offset:%" #o "\n\t"
+template <int N> __device__ __forceinline__ void read_stage(bf16x8* f, uint32_t a0, uint32_t a1) {
+  static_assert(N == 1 || N == 2 || N == 4, "blocks");
+  if constexpr (N == 1)
+    asm volatile(EPD_DSR(0, 2, 4) EPD_DSR(1, 3, 4) "s_waitcnt lgkmcnt(0)" : "=&v"(f[0]), "=&v"(f[1]) : "v"(a0), "v"(a1), "n"(0) : "memory");
+  else if constexpr (N == 2)
+    asm volatile(EPD_DSR(0, 4, 6) EPD_DSR(2, 4, 7) EPD_DSR(1, 5, 6) EPD_DSR(3, 5, 7) "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]) : "v"(a0), "v"(a1), "n"(0), "n"(2048) : "memory");
+  else
+    read_frags<4, 0>(f, a0, a1);
+}
+#undef EPD_DSR
 
-template <int NB, int NW, int U, bool GATED>
+template <int NB, int NW, int S, bool GATED>
 __global__ __launch_bounds__(64 * NW) void few_tokens_kernel(FewArgs a) {
-  constexpr int S = GATED ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) float sums[NW][S * NB][16][16];       // [wave][..][token][row]
+  constexpr int WB = GATED ? 2 : 1, STAGE = (WB + NB) * 2048, L = 2 * (WB + NB);     // blocks of 16 rows of W; bytes and loads per stage
+  static_assert((S - 1) * L < 64 && S >= 2, "load counter");
+  static_assert(WB * NB * 1024 <= S * STAGE, "sums");
+  __shared__ __attribute__((aligned(1024))) char lds[NW * S * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l16 = lane & 15, g4 = lane >> 4;
+  const int l16 = lane & 15, g4 = lane >> 4, lrow = lane >> 3;
   const int n0 = blockIdx.x * 16;
-  const uint16_t* const w0 = (const uint16_t*)a.W + (size_t)min(n0 + l16, a.N - 1) * a.K;
-  const uint16_t* const wrow[2] = {w0, w0 + (GATED ? (size_t)a.N * a.K : 0)};
-  const uint16_t* xrow[NB];
+  char* const ring = lds + wave * S * STAGE;
+  // a load brings 8 rows of 64 k; chunk c (8 k) of row r lies in slot c ^ swz(r) of its 128 bytes, so that the 16 rows of a fragment's
+  // read lie in different banks.  Rows past the last one repeat it: they only feed sums that are never stored.
+  auto swz = [](int row) { return (row >> 1) & 7; };
+  uint32_t w_off[2], x_off[2 * NB];
+  int k_at[2];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) xrow[b] = (const uint16_t*)a.X + (size_t)min(b * 16 + l16, a.T - 1) * a.ldx;   // rows beyond T repeat the last one: never stored
-  f32x4 acc[S][NB];
+  for (int h = 0; h < 2; ++h) {
+    const int r = h * 8 + lrow;
+    k_at[h] = ((lane & 7) ^ swz(r)) * 8;
+    w_off[h] = ((uint32_t)(min(n0 + r, a.N - 1) - n0) * (uint32_t)a.K + k_at[h]) * 2u;
 #pragma unroll
-  for (int s = 0; s < S; ++s)
+    for (int b = 0; b < NB; ++b) x_off[b * 2 + h] = ((uint32_t)min(b * 16 + r, a.T - 1) * (uint32_t)a.ldx + k_at[h]) * 2u;
+  }
+  const int nk = (a.K + 63) / 64;
+  const bool ragged = a.K % 64 != 0;                       // K is a multiple of 8: whole chunks come from zeros
+  auto issue = [&](int slot, int kt) {
+    auto one = [&](const char* base, uint32_t off, int h, char* to) {
+      const char* p = base + (size_t)kt * 128 + (size_t)off;
+      if (ragged && kt == nk - 1 && kt * 64 + k_at[h] >= a.K) p = (const char*)zero_bytes;
+      __builtin_amdgcn_global_load_lds(EPD_GPTR(p), EPD_LPTR(to), 16, 0, 0);
+    };
+    char* const to = ring + slot * STAGE;
+#pragma unroll
+    for (int w = 0; w < WB; ++w)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) one((const char*)a.W + ((size_t)n0 + (size_t)w * a.N) * a.K * 2, w_off[h], h, to + w * 2048 + h * 1024);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) one((const char*)a.X, x_off[b * 2 + h], h, to + (WB + b) * 2048 + h * 1024);
+  };
+  f32x4 acc[WB][NB];
+#pragma unroll
+  for (int s = 0; s < WB; ++s)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[s][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto load = [&](const uint16_t* row, int k) {            // 8 values, zeros from K on (K is a multiple of 8)
-    bf16x8 v = {};
-    if (k < a.K) v = *(const bf16x8*)(row + k);
-    return v;
-  };
-  auto stream = [&](const uint16_t* row, int k) {          // weights: read once
-    u32x4_few v = {};
-    if (k < a.K) v = __builtin_nontemporal_load((const u32x4_few*)(row + k));
-    return __builtin_bit_cast(bf16x8, v);
-  };
-  for (int k0 = wave * 64; k0 < a.K; k0 += NW * 64 * U) {
-    bf16x8 w[U][S][2], x[U][NB][2];
+  const int steps = wave < nk ? (nk - wave + NW - 1) / NW : 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      // the k of an instruction is arbitrary as long as both operands agree: a lane takes 16 consecutive ones
-      const int k = k0 + u * NW * 64 + g4 * 16;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int s = 0; s < S; ++s) w[u][s][h] = stream(wrow[s], k + h * 8);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) x[u][b][h] = load(xrow[b], k + h * 8);
-      }
+  for (int s = 0; s < S - 1; ++s) if (s < steps) issue(s, wave + s * NW);
+  const uint32_t rd = (uint32_t)(size_t)EPD_LPTR(ring) + l16 * 128 + ((g4 ^ swz(l16)) * 16);
+  int slot = 0;
+  for (int i = 0; i < steps; ++i) {
+    if (i + S - 1 < steps) {                               // into the slot read last: those reads have returned
+      issue(slot == 0 ? S - 1 : slot - 1, wave + (i + S - 1) * NW);
+      wait_vmcnt<(S - 1) * L>();
+    } else {
+      wait_vmcnt<0>();
     }
+    bf16x8 w[2 * WB], x[2 * NB];
+    const uint32_t at = rd + slot * STAGE;
+    read_stage<WB>(w, at, at ^ 64u);
+    read_stage<NB>(x, at + WB * 2048, (at ^ 64u) + WB * 2048);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int s = 0; s < WB; ++s)
 #pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-          for (int b = 0; b < NB; ++b) acc[s][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[u][s][h], x[u][b][h], acc[s][b], 0, 0, 0);
+        for (int b = 0; b < NB; ++b) acc[s][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[2 * s + h], x[2 * b + h], acc[s][b], 0, 0, 0);
+    if (++slot == S) slot = 0;
   }
+  __syncthreads();                                         // the rings are dead from here on
+  auto* const sums = (float (*)[WB * NB][16][16])lds;      // [wave][..][token][row]
 #pragma unroll
-  for (int s = 0; s < S; ++s)
+  for (int s = 0; s < WB; ++s)
 #pragma unroll
     for (int b = 0; b < NB; ++b) *(f32x4*)&sums[wave][s * NB + b][l16][g4 * 4] = acc[s][b];
   __syncthreads();
   for (int e = tid; e < NB * 64; e += 64 * NW) {           // four rows of W for a token
     const int b = e >> 6, t = (e >> 2) & 15, r = (e & 3) * 4, m = b * 16 + t, n = n0 + r;
     if (m >= a.T || n >= a.N) continue;                    // N is a multiple of 8
-    f32x4 v[S];
+    f32x4 v[WB];
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
+    for (int s = 0; s < WB; ++s) {
       v[s] = *(const f32x4*)&sums[0][s * NB + b][t][r];
 #pragma unroll
       for (int i = 1; i < NW; ++i) v[s] += *(const f32x4*)&sums[i][s * NB + b][t][r];
@@ -108,7 +145,7 @@ __global__ __launch_bounds__(64 * NW) void few_tokens_kernel(FewArgs a) {
       float p[4], q[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float gate = v[0][j], up = v[S - 1][j];
+        const float gate = v[0][j], up = v[WB - 1][j];
         if (a.keep_p) {
           q[j] = (a.act == 0 ? gate_act_d<0>(gate, p[j]) : a.act == 1 ? gate_act_d<1>(gate, p[j]) : gate_act_d<2>(gate, p[j])) * up;
           o[j] = p[j] * up;
@@ -132,10 +169,15 @@ __global__ __launch_bounds__(64 * NW) void few_tokens_kernel(FewArgs a) {
 
 constexpr int kFewTokens = 64;
 
-template <int NW, int U, bool GATED> static hipError_t launch_few(const FewArgs& a, hipStream_t s) {
+// waves per block and stages: the fastest of two to four choices each at hidden 1024, 1152, 3200 and 4096 (they lie within 10 %)
+template <bool GATED> static hipError_t launch_few(const FewArgs& a, hipStream_t s) {
   void* args[] = {(void*)&a};
-  const void* f = a.T <= 16 ? (const void*)few_tokens_kernel<1, NW, U, GATED> : a.T <= 32 ? (const void*)few_tokens_kernel<2, NW, U, GATED> : (const void*)few_tokens_kernel<4, NW, U / 2, GATED>;
-  return hipLaunchKernel(f, dim3((a.N + 15) / 16), dim3(64 * NW), args, 0, s);
+  constexpr int NW1 = GATED ? 4 : 8, NW2 = GATED ? 2 : 8, S2 = GATED ? 4 : 3, NW4 = GATED ? 2 : 4;
+  const void* f = (const void*)few_tokens_kernel<4, NW4, 3, GATED>;
+  int nw = NW4;
+  if (a.T <= 16) { f = (const void*)few_tokens_kernel<1, NW1, 3, GATED>; nw = NW1; }
+  else if (a.T <= 32) { f = (const void*)few_tokens_kernel<2, NW2, S2, GATED>; nw = NW2; }
+  return hipLaunchKernel(f, dim3((a.N + 15) / 16), dim3(64 * nw), args, 0, s);
 }
 
 // ------------------------------------------------------------------------------ transpose, column sums
@@ -237,22 +279,23 @@ static void launch_gated_whole(const GemmArgs& g, hipStream_t s) {
 }
 
 // Time of a launch of these products in us: per round of blocks alpha * K / 1024 + beta[epilogue] (the last round, of a
-// share f of the blocks, last0 + last1 * f of that), and `launch`.  Fitted to 199 shapes in every tile (hidden 1024, 1152 and 3200, 65 ... 32 768
-// tokens, forward and backward products, random operands): 7 ... 12 % off in the mean, and the tile it ranks first is within 3 % of
-// the fastest in 178 of them, 1 % off in the mean.  The encoder's own planner (plan_tiles) ranks its launches beside attention and
-// keeps its constants; it offers 256 x 128 tiles to residual adds only, which here win wherever a narrow output fills one round
-// of them (6272 x 1024 x 8192: 93 us, 112 in 128 x 128 tiles, 142 in 256 x 256).
+// share f of the blocks, last0 + last1 * f of that), and `launch`.  Fitted to 200 shapes in every tile (hidden 1024, 1152 and 3200, 65 ... 32 768
+// tokens, forward and backward products, random operands): 7 ... 12 % off in the mean, and the tile it ranks first is within 3 % of the
+// fastest in 288 of 308 choices, 0.7 % off in the mean.  (Constants fitted to launches on other buffers each time are 0.5 % off there
+// and leave whole passes 2 ... 7 % slower: they price the second launch of a cut higher than it costs inside a pass.)  The encoder's own planner (plan_tiles) ranks its
+// launches beside attention and keeps its constants; it offers 256 x 128 tiles to residual adds only, which here win wherever a narrow
+// output fills one round of them (6272 x 1024 x 8192: 93 us, 112 in 128 x 128 tiles, 142 in 256 x 256).
 //   An operand that stands [K, rows] costs alpha what reading fragments in halves of 8 bytes costs: a factor for W, and for both
 // (0: no kernel).  25 600 x 3200 x 8192 in 256 x 256 tiles 1093 us, 1044 with both operands turned, which takes 170 more; 8192 x 3200 x
 // 25 600, W alone, 1072 and 1065 + 60.
-struct ProductTile { int cfg, bm, bn, blocks; double last0, last1, alpha, launch, beta[4], rows_w, rows_both; };     // beta: store, gated, gated and saved, dgated
+struct ProductTile { int cfg, bm, bn, blocks; double last0, last1, alpha, launch, beta[4], rows_w, rows_both; };     // beta: store, gated, gated and kept, dgated
 constexpr ProductTile kProductTiles[] = {
-  {0, 256, 256, 1, 0.62, 0.28, 23.8, 3.4, {6.0, 6.9, 13.2, 32.0}, 1.02, 1.07},
-  {2, 256, 128, 1, 0.62, 0.25, 14.1, 3.9, {4.1, 3.9, 9.0, 17.4}, 1.10, 1.18},
-  {4, 128, 128, 2, 0.51, 0.44, 16.1, 3.4, {2.5, 0.6, 3.8, 11.4}, 0.0, 0.0},
-  {5, 320, 256, 1, 0.64, 0.30, 28.4, 1.7, {8.9, 10.1, 17.3, 42.5}, 1.04, 0.0},
-  {7, 64, 64, 2, 0.54, 0.49, 6.6, 3.1, {1.3, 1.5, 2.0, 3.0}, 0.0, 0.0},
-  {8, 64, 128, 2, 0.48, 0.55, 10.3, 3.4, {1.9, 1.1, 2.3, 5.4}, 0.0, 0.0},
+  {0, 256, 256, 1, 0.62, 0.28, 23.8, 3.4, {6.0, 6.9, 13.2, 24.4}, 1.02, 1.07},
+  {2, 256, 128, 1, 0.62, 0.25, 14.1, 3.9, {4.1, 3.9, 9.0, 12.7}, 1.10, 1.18},
+  {4, 128, 128, 2, 0.51, 0.44, 16.1, 3.4, {2.5, 0.6, 3.8, 7.0}, 0.0, 0.0},
+  {5, 320, 256, 1, 0.64, 0.30, 28.4, 1.7, {8.9, 10.1, 17.3, 34.0}, 1.04, 0.0},
+  {7, 64, 64, 2, 0.54, 0.49, 6.6, 3.1, {1.3, 1.5, 2.0, 1.7}, 0.0, 0.0},
+  {8, 64, 128, 2, 0.48, 0.55, 10.3, 3.4, {1.9, 1.1, 2.3, 2.7}, 0.0, 0.0},
 };
 
 static double rows_factor(const ProductTile& t, const GemmArgs& g) { return g.a_rows ? t.rows_both : g.w_rows ? t.rows_w : 1.0; }      // 0: the tile has no such kernel
@@ -481,9 +524,9 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
   hipStream_t st = (hipStream_t)stream;
   if (bf && T <= kFewTokens) {
     FewArgs a{x, w->gate_up_w, c.use_bias ? w->gate_up_b : nullptr, H, keep.p, keep.q, keep.low, (int)ld_x, F, T, F, D, act_code(c)};
-    hipError_t e = launch_few<4, 4, true>(a, st);
+    hipError_t e = launch_few<true>(a, st);
     FewArgs b{H, w->down_w, c.use_bias ? w->down_b : nullptr, y, nullptr, nullptr, nullptr, F, (int)ld_y, T, D, F, 0};
-    if (e == hipSuccess) e = launch_few<8, 4, false>(b, st);
+    if (e == hipSuccess) e = launch_few<false>(b, st);
     if (e != hipSuccess) return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e));
     return EPD_OK;
   }
