@@ -306,6 +306,10 @@ epd_status epd_rope_apply(const epd_rope_cfg* cfg, const epd_rope_tensor* tensor
                           const int32_t* positions, int64_t position_stride, int32_t tokens,
                           int32_t inverse, void* stream);
 
+/* Tokens of the first num_spans spans (see epd_rope_positions), for the size of its buffer: host arithmetic.  -1 (and a
+ * message) when a span is inconsistent or the sum passes 2^31 - 1. */
+int64_t epd_rope_tokens(const int32_t* span_thw, int32_t num_spans);
+
 /* (t, h, w) positions of sequences of text and visual tokens (V_m || V_t, section 3.1 "Prefill Stage",
  * Eq. 2; the paper does not say how they are counted).  A sequence starts at p = start[s]; a text of n
  * tokens takes positions p .. p + n - 1 on all three axes, and p moves on by n; an item of (t, h, w) tokens

@@ -92,7 +92,7 @@ EXPORTS = ["epd_encode_workspace_bytes", "epd_encode_create", "epd_encode", "epd
            "epd_encode_get_timing", "epd_preprocess", "epd_encode_cached", "epd_store_create",
            "epd_store_destroy", "epd_store_last_error", "epd_store_hash", "epd_store_hash_noalloc", "epd_store_lookup", "epd_store_insert",
            "epd_store_stats", "epd_probe_stream_read", "epd_probe_mfma_rate", "epd_probe_gemm_plan"]
-OPERATOR_EXPORTS = ["epd_op_last_error", "epd_rope_apply", "epd_rope_positions", "epd_gated_mlp_workspace_bytes", "epd_gated_mlp_saved_bytes",
+OPERATOR_EXPORTS = ["epd_op_last_error", "epd_rope_apply", "epd_rope_tokens", "epd_rope_positions", "epd_gated_mlp_workspace_bytes", "epd_gated_mlp_saved_bytes",
                     "epd_gated_mlp", "epd_gated_mlp_backward"]    # the operators beside the encoder
 
 
@@ -154,6 +154,8 @@ def _load() -> C.CDLL:
     lib.epd_rope_apply.restype = C.c_int
     lib.epd_rope_apply.argtypes = [C.POINTER(epd_rope_cfg), C.POINTER(epd_rope_tensor), C.c_int32, C.c_void_p, C.c_int64,
                                    C.c_int32, C.c_int32, C.c_void_p]
+    lib.epd_rope_tokens.restype = C.c_int64
+    lib.epd_rope_tokens.argtypes = [C.c_void_p, C.c_int32]
     lib.epd_rope_positions.restype = C.c_int
     lib.epd_rope_positions.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64,
                                        C.c_void_p, C.c_void_p]
@@ -586,6 +588,15 @@ def epd_rope_apply(cfg: epd_rope_cfg, tensors, positions: int, position_stride: 
     _op_check(lib.epd_rope_apply(C.byref(cfg), tensors, len(tensors), positions, position_stride, tokens, 1 if inverse else 0, stream))
 
 
+def epd_rope_tokens(span_thw: np.ndarray) -> int:
+    """Tokens of all spans."""
+    span = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
+    tokens = lib.epd_rope_tokens(_address(span), len(span))
+    if tokens < 0:
+        raise EpdError(EPD_ERR_SHAPE, epd_op_last_error())
+    return tokens
+
+
 def epd_rope_positions(span_thw: np.ndarray, cu_spans: np.ndarray, start: Optional[np.ndarray], t_step: int, positions: int,
                        position_stride: int, stream: int) -> np.ndarray:
     """Returns the next position of every sequence, int32 [num_sequences]."""
@@ -626,16 +637,14 @@ def _on(index: int, call, *args):
         return call(*args, stream)
 
 
-_SPAN_LEAST = np.array([0, 1, 1], dtype=np.int32)
-
-
 def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str = "cuda:0", out: Optional[torch.Tensor] = None):
     """(t, h, w) positions of sequences of texts (n, 0, 0) and items (t, h, w), sequence s being the spans
     [cu_spans[s], cu_spans[s + 1]) and starting at start[s].  Returns (int32 device tensor [3, tokens], next position of every
     sequence int32 [sequences])."""
     span, cu = _spans(span_thw, cu_spans)
-    used = np.maximum(span[:int(cu[-1])], _SPAN_LEAST).astype(np.int64)        # a text is n x 1 x 1 tokens
-    tokens = int((used[:, 0] * used[:, 1] * used[:, 2]).sum())
+    tokens = lib.epd_rope_tokens(_address(span), int(cu[-1]))
+    if tokens < 0:
+        raise EpdError(EPD_ERR_SHAPE, epd_op_last_error())
     dev = torch.device(device) if out is None else out.device
     if dev.index is None:
         dev = torch.device(dev.type, torch.cuda.current_device())
@@ -689,7 +698,7 @@ class Rope:
             shape = x.shape
             si = strides(x, shape)
             if out is None:
-                y, so = torch.empty(shape, dtype=self.dtype, device=x.device), (shape[1] * d, d)
+                y, so = x.new_empty(shape), (shape[1] * d, d)
             else:
                 y, so = out[i], strides(out[i], shape)
             made.append(y)

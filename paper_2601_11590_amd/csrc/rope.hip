@@ -176,6 +176,14 @@ __global__ __launch_bounds__(256) void rope_positions_kernel(PosArgs a) {
   a.out[2 * a.stride + tok] = s.pos + c;
 }
 
+// Tokens of a span: -1 where its sizes are inconsistent, -2 where they pass 2^31 - 1.
+static int64_t span_tokens(const int32_t* thw) {
+  const int64_t t = thw[0], h = thw[1], w = thw[2];
+  if (h == 0 && w == 0) return t < 0 ? -1 : t;
+  if (t <= 0 || h <= 0 || w <= 0) return -1;
+  return h * w > INT_MAX || t * (h * w) > INT_MAX ? -2 : t * h * w;
+}
+
 // Axis and turns per position of every pair.  A pure function of the configuration, which a program keeps from call to
 // call: the last table of the thread is kept with it (64 powers are 2.5 us of a call for one token).
 static void pair_table(const epd_rope_cfg& c, int pairs, RopeArgs& a) {
@@ -297,6 +305,16 @@ epd_status epd_rope_apply(const epd_rope_cfg* c, const epd_rope_tensor* tensors,
   return EPD_OK;
 }
 
+int64_t epd_rope_tokens(const int32_t* span_thw, int32_t num_spans) {
+  if (!span_thw || num_spans < 0) { op_fail(EPD_ERR_INVALID_ARG, "epd_rope_tokens: span_thw is NULL or num_spans %d", num_spans); return -1; }
+  int64_t tokens = 0;
+  for (int64_t i = 0; i < num_spans; ++i) {
+    const int64_t n = span_tokens(span_thw + 3 * i);
+    if (n < 0 || (tokens += n) > INT_MAX) { op_fail(EPD_ERR_SHAPE, "epd_rope_tokens: span %lld is inconsistent or passes %d tokens", (long long)i, INT_MAX); return -1; }
+  }
+  return tokens;
+}
+
 epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, int32_t num_sequences, const int32_t* start, int32_t t_step,
                               int32_t* positions, int64_t position_stride, int32_t* next_out, void* stream) {
   if (!span_thw || !cu_spans || !positions) return op_fail(EPD_ERR_INVALID_ARG, "epd_rope_positions: a required pointer is NULL");
@@ -324,10 +342,10 @@ epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, 
       for (int i = cu_spans[s]; i < cu_spans[s + 1]; ++i) {
         const int64_t t = span_thw[3 * (int64_t)i], h = span_thw[3 * (int64_t)i + 1], w = span_thw[3 * (int64_t)i + 2];
         const bool text = h == 0 && w == 0;
-        if (!pass && (text ? t < 0 : (t <= 0 || h <= 0 || w <= 0)))
+        const int64_t count = span_tokens(span_thw + 3 * (int64_t)i);
+        if (!pass && count == -1)
           return op_fail(EPD_ERR_SHAPE, "epd_rope_positions: span %d = (%lld, %lld, %lld): a text is (n, 0, 0), an item has positive sizes", i, (long long)t, (long long)h, (long long)w);
-        if (!pass && !text && (h * w > INT_MAX || t * (h * w) > INT_MAX)) return op_fail(EPD_ERR_SHAPE, "epd_rope_positions: span %d has too many tokens", i);
-        const int64_t count = text ? t : t * h * w;
+        if (!pass && count < 0) return op_fail(EPD_ERR_SHAPE, "epd_rope_positions: span %d has too many tokens", i);
         const int64_t ahead = text ? t : std::max((int64_t)t_step * (t - 1) + 1, std::max(h, w));
         if (pass && count) {
           if (a.n == kPosSpans)

@@ -139,6 +139,15 @@ def test_position_refusals(kw, needle):
     assert st == B.EPD_ERR_SHAPE and needle in msg, msg
 
 
+def test_tokens_of_spans():
+    assert B.epd_rope_tokens([(3, 0, 0), (2, 3, 4), (0, 0, 0)]) == 27 and B.epd_rope_tokens(np.zeros((0, 3))) == 0
+    for bad in ([(-1, 0, 0)], [(1, 0, 2)], [(0, 1, 1)], [(2, 65536, 65536)], [(2 ** 31 - 1, 0, 0), (1, 0, 0)]):
+        with pytest.raises(B.EpdError) as e:
+            B.epd_rope_tokens(bad)
+        assert e.value.status == B.EPD_ERR_SHAPE and "span" in str(e.value)
+    assert B.lib.epd_rope_tokens(None, 1) == -1 and B.lib.epd_rope_tokens(0x1000, -1) == -1
+
+
 def test_position_arguments():
     assert pos([(1, 0, 0)], [0, 1], positions=None)[0] == B.EPD_ERR_INVALID_ARG
     assert pos([(1, 0, 0)], [0, 1], t_step=-1)[0] == B.EPD_ERR_INVALID_ARG
