@@ -365,7 +365,8 @@ uint64_t epd_gated_mlp_saved_bytes(const epd_gated_mlp_cfg* cfg, int32_t tokens)
  *           be x (with the same rows)
  *   tokens  0 .. max_tokens; 0 launches nothing
  *   saved   device, epd_gated_mlp_saved_bytes(cfg, tokens) bytes, aligned as x, or NULL: receives what
- *           epd_gated_mlp_backward needs of this call (its layout is the library's: about 7 F bytes a token in bf16, 8 F in fp32)
+ *           epd_gated_mlp_backward needs of this call (its layout is the library's: about 7 F bytes a token in bf16, 8 F in fp32);
+ *           y has the same bits either way
  * Nothing in the workspace is kept from one call to the next. */
 epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weights* weights, const void* x,
                          int64_t ld_x, int32_t tokens, void* y, int64_t ld_y, void* saved, void* workspace,

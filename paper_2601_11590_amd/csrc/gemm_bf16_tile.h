@@ -89,12 +89,16 @@ __device__ __forceinline__ void rotate_pair(float& a, float& b, float cos, float
 // Gate of a gated MLP: act(g) and act'(g).  SiLU: p = sigmoid(g), g p and p (1 + g (1 - p)).  GELU (erf): g Phi(g) and
 // Phi(g) + g phi(g), Phi from the tail; beyond 7.5
 // the tail's factor is held too (gelu_erf_fast lets it grow: -3e6 at -1e20).  GELU (tanh): with s = sigmoid(2 u(g)), g s and
-// s + g s (1 - s) 2 u'(g).  ACT: GemmArgs::act.
+// s + g s (1 - s) 2 u'(g), u spelled the same in both, so that H has the same bits whether P and Q are kept or not.  ACT:
+// GemmArgs::act.
+__device__ __forceinline__ float gelu_tanh_tail(float g, float z) {         // 1 - s;  z = g^2, held to 1e30
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * 1.44269504088896340736f * (0.79788456080286535588f * fmaf(0.044715f * z, g, g))));
+}
 template <int ACT> __device__ __forceinline__ float gate_act(float g) {
   if constexpr (ACT == 0) {
     const float a = fminf(fabsf(g), 7.5f);
     return fmaf(-a, gauss_tail(a), fmaxf(g, 0.f));
-  } else if constexpr (ACT == 1) return gelu_tanh_fast(g);
+  } else if constexpr (ACT == 1) return g * (1.0f - gelu_tanh_tail(g, fminf(g * g, 1e30f)));
   else return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g));
 }
 template <int ACT> __device__ __forceinline__ float gate_act_d(float g, float& a) {
@@ -104,8 +108,7 @@ template <int ACT> __device__ __forceinline__ float gate_act_d(float g, float& a
     return fmaf(g, 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752044448170368f * g * g), g >= 0.f ? 1.0f - e : e);
   } else if constexpr (ACT == 1) {
     const float z = fminf(g * g, 1e30f);               // beyond, s (1 - s) is 0: no 0 * infinity
-    const float u = 0.79788456080286535588f * fmaf(0.044715f * z, g, g);
-    const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * 1.44269504088896340736f * u)), s = 1.0f - r;
+    const float r = gelu_tanh_tail(g, z), s = 1.0f - r;
     a = g * s;
     return fmaf(a * r, 2.0f * 0.79788456080286535588f * fmaf(3.0f * 0.044715f, z, 1.0f), s);
   } else {
@@ -1134,7 +1137,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
               if constexpr (save) {
                 *(uint2*)(to + 1024) = ph;
                 *(uint2*)(to + 2048) = qh;
-                *(uint32_t*)(piece + 3072 + l16 * 32 + q * 16 + g4 * 4) = low;
+                *(uint32_t*)(piece + 3 * 1024 + l16 * 32 + q * 16 + g4 * 4) = low;
               }
             } else {
               __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, h), h_rows, h_off + (uint32_t)(b * 16) * h_pitch, 0, 0);
@@ -1152,7 +1155,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, h), h_rows, h_off + (uint32_t)(b * 16) * h_pitch, 0, 0);
             if constexpr (save) {
               const uint4 ph = *(const uint4*)(from + 1024), qh = *(const uint4*)(from + 2048);
-              const uint2 low = *(const uint2*)(piece + 3072 + rl * 32 + (lane & 3) * 8);
+              const uint2 low = *(const uint2*)(piece + 3 * 1024 + rl * 32 + (lane & 3) * 8);
               __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, ph), p_rows, 2 * (k_off + (uint32_t)(b * 16) * k_pitch), 0, 0);
               __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, qh), q_rows, 2 * (k_off + (uint32_t)(b * 16) * k_pitch), 0, 0);
               __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, low), l_rows, k_off + (uint32_t)(b * 16) * k_pitch, 0, 0);
