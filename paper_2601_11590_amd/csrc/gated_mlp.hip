@@ -262,17 +262,22 @@ static hipError_t clear(bool bf16, void* p, int64_t n, hipStream_t s) {
 // ------------------------------------------------------------------------------ products
 template <int EPI> static void launch_gated_epi(const GemmArgs& g, hipStream_t s) { launch_epi<EPI, OUT_BF16, false, true>(g, s); }
 
-// operands that stand [K, rows]: the tiles of the ping-pong loop (A: those whose wave rows are whole blocks of 64)
-template <int EPI, int KROWS> static void launch_krows(const GemmArgs& g, hipStream_t s) {
-  if (g.tile_cfg == 3) launch_cfg<T2, EPI, OUT_BF16, false, true, KROWS>(g, s);
-  else if (KROWS == 2 && g.tile_cfg == 6) launch_cfg<T5, EPI, OUT_BF16, false, true, 2>(g, s);
-  else launch_cfg<T0, EPI, OUT_BF16, false, true, KROWS>(g, s);
+// operands that stand [K, rows]: the tiles of the ping-pong loop (both: those whose wave rows are whole blocks of 64)
+template <int EPI> static void launch_w_rows(const GemmArgs& g, hipStream_t s) {
+  if (g.tile_cfg == 3) launch_cfg<T2, EPI, OUT_BF16, false, true, 2>(g, s);
+  else if (g.tile_cfg == 6) launch_cfg<T5, EPI, OUT_BF16, false, true, 2>(g, s);
+  else launch_cfg<T0, EPI, OUT_BF16, false, true, 2>(g, s);
+}
+
+static void launch_both_rows(const GemmArgs& a, const GemmArgs* b, hipStream_t s) {
+  if (a.tile_cfg == 3) launch_pair<T2>(a, b, s);
+  else launch_pair<T0>(a, b, s);
 }
 
 static void launch_gated_whole(const GemmArgs& g, hipStream_t s) {
-  if (g.a_rows) launch_krows<EPI_STORE, 3>(g, s);
-  else if (g.w_rows && g.epilogue == EPI_DGATED) launch_krows<EPI_DGATED, 2>(g, s);
-  else if (g.w_rows) launch_krows<EPI_STORE, 2>(g, s);
+  if (g.a_rows) launch_both_rows(g, nullptr, s);
+  else if (g.w_rows && g.epilogue == EPI_DGATED) launch_w_rows<EPI_DGATED>(g, s);
+  else if (g.w_rows) launch_w_rows<EPI_STORE>(g, s);
   else if (g.epilogue == EPI_GATED) launch_gated_epi<EPI_GATED>(g, s);
   else if (g.epilogue == EPI_DGATED) launch_gated_epi<EPI_DGATED>(g, s);
   else launch_gated_epi<EPI_STORE>(g, s);
@@ -300,10 +305,14 @@ constexpr ProductTile kProductTiles[] = {
 
 static double rows_factor(const ProductTile& t, const GemmArgs& g) { return g.a_rows ? t.rows_both : g.w_rows ? t.rows_w : 1.0; }      // 0: the tile has no such kernel
 
-static double product_cost(const ProductTile& t, long M, long N, double K, int kind, long cus) {
-  const long tiles = ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn), slots = cus * t.blocks, full = tiles / slots, rest = tiles % slots;
+static long product_tiles(const ProductTile& t, long M, long N) { return ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn); }
+
+static double tiles_cost(const ProductTile& t, long tiles, double K, int kind, long cus) {
+  const long slots = cus * t.blocks, full = tiles / slots, rest = tiles % slots;
   return t.launch + ((double)full + (rest ? t.last0 + t.last1 * (double)rest / (double)slots : 0.0)) * (t.alpha * K / 1024.0 + t.beta[kind]);
 }
+
+static double product_cost(const ProductTile& t, long M, long N, double K, int kind, long cus) { return tiles_cost(t, product_tiles(t, M, N), K, kind, cus); }
 
 // One launch of the cheapest tile, or whole rounds of a large one and the rest of the rows in the cheapest for them:
 // 8192 x 3200 x 25 600 is 416 tiles of 256 x 256, priced two rounds (1075 us); 6080 rows in one round of 320 x 256 and 2112 in one of 256 x 128 take 980.
@@ -371,22 +380,51 @@ int launch_gemm_bf16_gated(const GemmArgs& args, hipStream_t s) {
 }
 
 // A product whose operands stand [K, rows] (g.a_rows, g.w_rows): as they stand, or turned into a_t and w_t (rows of round_up(K, 8))
-// first, which costs a pass over them at about 4.5 TB/s and a launch each.  sum_rows: see launch_gemm_bf16_gated.
-static hipError_t launch_product(GemmArgs g, void* a_t, void* w_t, hipStream_t s, int* sum_rows = nullptr) {
+// first, which costs a pass over them at about 4.5 TB/s and a launch each.
+struct Turned { GemmArgs g; bool turn; double cost; };
+static Turned plan_turned(const GemmArgs& g, void* a_t, void* w_t) {
   const long cus = num_cus();
   GemmArgs t = g;
   double turn = 0.0;
   t.K = (g.K + 7) / 8 * 8;
   if (g.a_rows) { t.A = a_t; t.lda = t.K; t.a_rows = 0; turn += 3.0 + 4.0 * g.K * (double)g.M / 4.5e6; }
   if (g.w_rows) { t.W = w_t; t.ldw = t.K; t.w_rows = 0; turn += 3.0 + 4.0 * g.K * (double)g.N / 4.5e6; }
-  if (plan_product(t, cus).cost + turn < plan_product(g, cus).cost) {
-    if (g.a_rows) if (hipError_t e = transpose(g.A, g.lda, a_t, t.lda, g.K, g.M, s)) return e;
-    if (g.w_rows) if (hipError_t e = transpose(g.W, g.ldw, w_t, t.ldw, g.K, g.N, s)) return e;
-    g = t;
-  }
-  const int rows = launch_gemm_bf16_gated(g, s);
+  turn += plan_product(t, cus).cost;
+  const double stands = plan_product(g, cus).cost;
+  return turn < stands ? Turned{t, true, turn} : Turned{g, false, stands};
+}
+
+// sum_rows: see launch_gemm_bf16_gated
+static hipError_t launch_product(const GemmArgs& g, void* a_t, void* w_t, hipStream_t s, int* sum_rows = nullptr) {
+  const Turned t = plan_turned(g, a_t, w_t);
+  if (t.turn && g.a_rows) if (hipError_t e = transpose(g.A, g.lda, a_t, t.g.lda, g.K, g.M, s)) return e;
+  if (t.turn && g.w_rows) if (hipError_t e = transpose(g.W, g.ldw, w_t, t.g.ldw, g.K, g.N, s)) return e;
+  const int rows = launch_gemm_bf16_gated(t.g, s);
   if (sum_rows) *sum_rows = rows;
   return hipSuccess;
+}
+
+// Two products of one K whose operands stand [K, rows], each wanted or not: in one launch, whose rounds they share, where that is
+// priced lower than one after the other.  The choice does not depend on which are wanted, so that a gradient has the same bits in every
+// call.
+static hipError_t launch_products(const GemmArgs& a, bool want_a, const GemmArgs& b, bool want_b, void* a_t, void* w_t, hipStream_t s) {
+  if (!want_a && !want_b) return hipSuccess;
+  const long cus = num_cus();
+  double least = plan_turned(a, a_t, w_t).cost + plan_turned(b, a_t, w_t).cost;
+  int tile = -1;
+  for (const ProductTile& t : kProductTiles) {
+    if (t.rows_both == 0.0) continue;
+    const double c = tiles_cost(t, product_tiles(t, a.M, a.N) + product_tiles(t, b.M, b.N), t.rows_both * a.K, 0, cus);
+    if (c < least) { least = c; tile = t.cfg; }
+  }
+  if (tile >= 0) {
+    GemmArgs first = want_a ? a : b;
+    first.tile_cfg = tile + 1;
+    launch_both_rows(first, want_a && want_b ? &b : nullptr, s);
+    return hipSuccess;
+  }
+  if (want_a) if (hipError_t e = launch_product(a, a_t, w_t, s)) return e;
+  return want_b ? launch_product(b, a_t, w_t, s) : hipSuccess;
 }
 
 }  // namespace epd
@@ -638,8 +676,7 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
     if (!ok(hipLaunchKernel((const void*)sum_parts_kernel, dim3(sums.blocks0 + (sums.job[1].cols + 63) / 64), dim3(256), args, 0, st))) return failed();
   }
   if (grads->dx && !ok(launch_product(dx, nullptr, ws + L.w_t, st))) return failed();
-  if (grads->gate_up_w && !ok(launch_product(dgu, ws + L.a_t, ws + L.w_t, st))) return failed();
-  if (grads->down_w && !ok(launch_product(dd, ws + L.a_t, ws + L.w_t, st))) return failed();
+  if (!ok(launch_products(dgu, grads->gate_up_w, dd, grads->down_w, ws + L.a_t, ws + L.w_t, st))) return failed();
   ok(last.now());
   return e == hipSuccess ? EPD_OK : failed();
 }

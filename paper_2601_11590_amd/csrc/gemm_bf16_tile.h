@@ -1439,6 +1439,26 @@ static int num_cus() {
   return n;
 }
 
+// Row tiles per rasterisation group of a launch.
+template <class T> static int raster_group(const GemmArgs& g, int tiles_m, int tiles_n, long blocks) {
+  if (g.group_m > 0) return std::min(g.group_m, tiles_m);
+  // keep the A panels of one group (group_m x BM rows x K) within about 2 MB of the 4 MB L2
+  const long panel = (long)T::BM * g.K * 2;
+  int group_m = (int)std::max(1L, std::min((long)tiles_m, (2L << 20) / std::max(panel, 1L)));
+  // Long K (panels beyond the cache) and a wide output: the 32 tiles an XCD runs at a time still
+  // advance through K together, so what has to stay cached is their current K window, not whole
+  // panels.  Four row tiles per group make that set 4 x 8 tiles (12 operand panels) instead of
+  // 1 x 32 (33 panels): +5 % on 32768 x 12800 x 3200 and 32768 x 9600 x 3200; narrow outputs
+  // (13 column tiles) measured best with the panel rule alone.
+  if (tiles_n >= 24) group_m = std::max(group_m, 4);
+  // Few rows against a large weight matrix (the merger projection): with row groups every
+  // XCD streams all of W.  When the whole grid runs in at most two rounds, number the tiles
+  // column by column instead, so that an XCD owns a block of columns: W is then fetched
+  // once in total and the (smaller) A once per XCD.
+  if ((long)g.N > 2L * g.M && (long)tiles_m * tiles_n <= 2 * blocks) group_m = tiles_m;
+  return std::min(group_m, tiles_m);
+}
+
 // CLAMPED: operands that may not be read past their ends take the ping-pong loop all the same, with clamps
 template <class T, int EPI, int OUT, bool GATHER, bool CLAMPED = false, int KROWS = 0>
 static void launch_cfg(const GemmArgs& g, hipStream_t s) {
@@ -1446,23 +1466,7 @@ static void launch_cfg(const GemmArgs& g, hipStream_t s) {
   const long blocks = (long)T::MINBLK * (g.compute_units > 0 ? g.compute_units : num_cus());     // of one round
   GemmArgs a = g;
   a.rot_lds = EPI == EPI_QKV && (long)tiles_m * tiles_n <= ROT_TABLE_ROUNDS * blocks;
-  if (a.group_m <= 0) {
-    // keep the A panels of one group (group_m x BM rows x K) within about 2 MB of the 4 MB L2
-    const long panel = (long)T::BM * g.K * 2;
-    a.group_m = (int)std::max(1L, std::min((long)tiles_m, (2L << 20) / std::max(panel, 1L)));
-    // Long K (panels beyond the cache) and a wide output: the 32 tiles an XCD runs at a time still
-    // advance through K together, so what has to stay cached is their current K window, not whole
-    // panels.  Four row tiles per group make that set 4 x 8 tiles (12 operand panels) instead of
-    // 1 x 32 (33 panels): +5 % on 32768 x 12800 x 3200 and 32768 x 9600 x 3200; narrow outputs
-    // (13 column tiles) measured best with the panel rule alone.
-    if (tiles_n >= 24) a.group_m = std::max(a.group_m, 4);
-    // Few rows against a large weight matrix (the merger projection): with row groups every
-    // XCD streams all of W.  When the whole grid runs in at most two rounds, number the tiles
-    // column by column instead, so that an XCD owns a block of columns: W is then fetched
-    // once in total and the (smaller) A once per XCD.
-    if ((long)g.N > 2L * g.M && (long)tiles_m * tiles_n <= 2 * blocks) a.group_m = tiles_m;
-  }
-  a.group_m = std::min(a.group_m, tiles_m);
+  a.group_m = raster_group<T>(g, tiles_m, tiles_n, blocks);
   if constexpr (CLAMPED) {
     static_assert(!GATHER, "clamped rows are dense");
     hipLaunchKernelGGL((gemm_bf16_kernel<T, EPI, OUT, false, T::PINGPONG, 2, T::PINGPONG, KROWS>), dim3(tiles_m * tiles_n), dim3(T::NT), 0, s, a);
@@ -1602,6 +1606,47 @@ static TilePlan plan_tiles(int M, int N, int K, int epi, bool may_split, long cu
     }
   }
   return best;
+}
+
+// Products whose operands both stand [K, rows]: g, and from tile `first` on a second one of the same K (the two weights'
+// gradients of a gated MLP share their rounds of blocks).
+struct GemmPair {
+  GemmArgs g;
+  const void *A, *W;
+  void* out;
+  int lda, ldw, ldo, M, N, group_m, first;
+};
+template <class T>
+__global__ __launch_bounds__(T::NT, T::MINBLK) void gemm_bf16_pair_kernel(GemmPair p) {
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS_BYTES + T::BM * 4];
+  GemmArgs g = p.g;
+  g.zeros = zero_bytes;
+  int t = xcd_remap(blockIdx.x, gridDim.x);
+  if (t >= p.first) {
+    t -= p.first;
+    g.A = p.A; g.W = p.W; g.out = p.out; g.lda = p.lda; g.ldw = p.ldw; g.ldo = p.ldo; g.M = p.M; g.N = p.N; g.group_m = p.group_m;
+  }
+  const int tiles_n = (g.N + T::BN - 1) / T::BN, tiles_m = (g.M + T::BM - 1) / T::BM;
+  int tm, tn;
+  tile_coords(t, tiles_m, tiles_n, g.group_m, tm, tn);
+  gemm_tile<T, EPI_STORE, OUT_BF16, false, false, true, true, 3>(g, tm * T::BM, tn * T::BN, lds);
+}
+
+template <class T> static void launch_pair(const GemmArgs& a, const GemmArgs* b, hipStream_t s) {
+  static_assert(T::PINGPONG, "reads transposed");
+  const long blocks = (long)T::MINBLK * num_cus();
+  auto tiles = [](int n, int b) { return (n + b - 1) / b; };
+  GemmPair p{};
+  p.g = a;
+  p.g.group_m = raster_group<T>(a, tiles(a.M, T::BM), tiles(a.N, T::BN), blocks);
+  p.first = tiles(a.M, T::BM) * tiles(a.N, T::BN);
+  int all = p.first;
+  if (b) {
+    p.A = b->A; p.W = b->W; p.out = b->out; p.lda = b->lda; p.ldw = b->ldw; p.ldo = b->ldo; p.M = b->M; p.N = b->N;
+    p.group_m = raster_group<T>(*b, tiles(b->M, T::BM), tiles(b->N, T::BN), blocks);
+    all += tiles(b->M, T::BM) * tiles(b->N, T::BN);
+  }
+  hipLaunchKernelGGL(gemm_bf16_pair_kernel<T>, dim3(all), dim3(T::NT), 0, s, p);
 }
 
 template <int EPI, int OUT, bool GATHER, bool CLAMPED = false>
