@@ -24,9 +24,8 @@ namespace epd {
 // waves take K in turn, 64 at a time, each with a ring of S stages of its own in LDS, which direct loads of 8 rows x 128 bytes
 // fill and nobody else reads, so no wave waits for another until their sums meet, in the order of the waves.
 //   What it replaced loaded the operands of the matrix instructions straight to registers, 16 rows x 64 bytes an instruction: half
-// lines of twice as many rows, at 4.1 TB/s where whole lines reach 5.2 (3200 x 12 800, one token: gate and up 40.2 -> 31.7 us, down
-// 22.4 -> 16.8; 16 tokens 52 -> 33.6 and 32 -> 20.7; 64 tokens 90 -> 48 and 70 -> 36; a plain stream of 164 MB takes 29 ... 32 us).  The
-// GEMM's tiles take 46 and 57 us from 64 tokens down, so this one serves up to 64.
+// lines of twice as many rows, at 4.1 TB/s where whole lines reach 5.2 (3200 x 12 800, 16 tokens: gate and up 52 -> 33.6 us, down
+// 32 -> 20.7; 64 tokens 90 -> 48 and 70 -> 36).  The GEMM's tiles take 46 and 57 us from 64 tokens down, so this one serves up to 64.
 struct FewArgs {
   const void* X; const void* W; const void* bias;
   void* out;
@@ -48,7 +47,7 @@ template <int N> __device__ __forceinline__ void read_stage(bf16x8* f, uint32_t 
 }
 #undef EPD_DSR
 
-template <int NB, int NW, int S, bool GATED>
+template <int NB, int NW, int S, bool GATED, bool NT>
 __global__ __launch_bounds__(64 * NW) void few_tokens_kernel(FewArgs a) {
   constexpr int WB = GATED ? 2 : 1, STAGE = (WB + NB) * 2048, L = 2 * (WB + NB);     // blocks of 16 rows of W; bytes and loads per stage
   static_assert((S - 1) * L < 64 && S >= 2, "load counter");
@@ -74,20 +73,24 @@ __global__ __launch_bounds__(64 * NW) void few_tokens_kernel(FewArgs a) {
   const int nk = (a.K + 63) / 64;
   const bool ragged = a.K % 64 != 0;                       // K is a multiple of 8: whole chunks come from zeros
   auto issue = [&](int slot, int kt) {
-    auto one = [&](const char* base, uint32_t off, int h, char* to) {
-      const char* p = base + (size_t)kt * 128 + (size_t)off;
-      if (ragged && kt == nk - 1 && kt * 64 + k_at[h] >= a.K) p = (const char*)zero_bytes;
-      __builtin_amdgcn_global_load_lds(EPD_GPTR(p), EPD_LPTR(to), 16, 0, 0);
+    auto from = [&](const char* base, uint32_t off, int h) {
+      return ragged && kt == nk - 1 && kt * 64 + k_at[h] >= a.K ? (const char*)zero_bytes : base + (size_t)kt * 128 + (size_t)off;
     };
     char* const to = ring + slot * STAGE;
 #pragma unroll
     for (int w = 0; w < WB; ++w)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) one((const char*)a.W + ((size_t)n0 + (size_t)w * a.N) * a.K * 2, w_off[h], h, to + w * 2048 + h * 1024);
+      for (int h = 0; h < 2; ++h) {
+        const char* const p = from((const char*)a.W + ((size_t)n0 + (size_t)w * a.N) * a.K * 2, w_off[h], h);
+        __builtin_amdgcn_global_load_lds(EPD_GPTR(p), EPD_LPTR(to + w * 2048 + h * 1024), 16, 0, NT ? 2 : 0);       // 2: non-temporal
+      }
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) one((const char*)a.X, x_off[b * 2 + h], h, to + (WB + b) * 2048 + h * 1024);
+      for (int h = 0; h < 2; ++h) {
+        const char* const p = from((const char*)a.X, x_off[b * 2 + h], h);
+        __builtin_amdgcn_global_load_lds(EPD_GPTR(p), EPD_LPTR(to + (WB + b) * 2048 + h * 1024), 16, 0, 0);
+      }
   };
   f32x4 acc[WB][NB];
 #pragma unroll
@@ -167,17 +170,100 @@ __global__ __launch_bounds__(64 * NW) void few_tokens_kernel(FewArgs a) {
   }
 }
 
+// The same for one token, where matrix instructions would have 15 empty columns and X as much traffic as W: a channel's row (GATED: its
+// two rows) per wave, or per block with the K of its four waves in turn, 16 bytes a lane straight to registers.  Bound: HBM (gate and up of
+// 3200 x 12 800: 24.6 us, 6.7 TB/s; few_tokens_kernel 28.4).
+template <int SPLIT, int U, bool GATED, bool NT>
+__global__ __launch_bounds__(256) void one_token_kernel(FewArgs a) {
+  constexpr int WB = GATED ? 2 : 1;
+  __shared__ float part[4][WB];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int n = SPLIT == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  if (n >= a.N) return;                                    // SPLIT 1: whole waves, which no barrier waits for
+  const uint16_t* const X = (const uint16_t*)a.X;
+  const uint16_t* const row = (const uint16_t*)a.W + (size_t)n * a.K;
+  const size_t up = (size_t)a.N * a.K;
+  float sum[WB] = {};
+  for (int k0 = (SPLIT == 1 ? 0 : wave) * 512 + lane * 8; k0 < a.K; k0 += 512 * SPLIT * U) {
+    u32x4 w[U][WB], x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * 512 * SPLIT;                  // K is a multiple of 8
+      const bool in = k < a.K;
+      x[u] = in ? *(const u32x4*)(X + k) : u32x4{};
+#pragma unroll
+      for (int s = 0; s < WB; ++s) w[u][s] = in ? (NT ? __builtin_nontemporal_load((const u32x4*)(row + s * up + k)) : *(const u32x4*)(row + s * up + k)) : u32x4{};
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int s = 0; s < WB; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sum[s] = fmaf(__uint_as_float(w[u][s][i] << 16), __uint_as_float(x[u][i] << 16), sum[s]);
+          sum[s] = fmaf(__uint_as_float(w[u][s][i] & 0xffff0000u), __uint_as_float(x[u][i] & 0xffff0000u), sum[s]);
+        }
+  }
+#pragma unroll
+  for (int s = 0; s < WB; ++s)
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum[s] += __shfl_xor(sum[s], o);
+  if constexpr (SPLIT == 4) {
+    if (lane == 0) {
+#pragma unroll
+      for (int s = 0; s < WB; ++s) part[wave][s] = sum[s];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < WB; ++s) sum[s] = (part[0][s] + part[1][s]) + (part[2][s] + part[3][s]);
+  }
+  if (lane != 0 || (SPLIT == 4 && wave != 0)) return;
+#pragma unroll
+  for (int s = 0; s < WB; ++s)
+    if (a.bias) sum[s] += bf16_bits_to_float(((const uint16_t*)a.bias)[s * a.N + n]);
+  float o = sum[0];
+  if constexpr (GATED) {
+    const float gate = sum[0], u = sum[WB - 1];
+    if (a.keep_p) {
+      float p[4] = {}, q[4] = {};
+      q[0] = (a.act == 0 ? gate_act_d<0>(gate, p[0]) : a.act == 1 ? gate_act_d<1>(gate, p[0]) : gate_act_d<2>(gate, p[0])) * u;
+      o = p[0] * u;
+      uint2 ph, qh;
+      uint32_t low;
+      keep_channels(p, q, ph, qh, low);
+      ((uint16_t*)a.keep_p)[n] = (uint16_t)ph.x; ((uint16_t*)a.keep_q)[n] = (uint16_t)qh.x; ((uint8_t*)a.keep_low)[n] = (uint8_t)low;
+    } else {
+      o = (a.act == 0 ? gate_act<0>(gate) : a.act == 1 ? gate_act<1>(gate) : gate_act<2>(gate)) * u;
+    }
+  }
+  ((__bf16*)a.out)[n] = (__bf16)o;
+}
+
 constexpr int kFewTokens = 64;
 
-// waves per block and stages: the fastest of two to four choices each at hidden 1024, 1152, 3200 and 4096 (they lie within 10 %)
-template <bool GATED> static hipError_t launch_few(const FewArgs& a, hipStream_t s) {
+// One token: rows of up to 2048 a wave each (gate and up, K = 1024 4.9 us, a block each 5.8; K = 3200 25.7 and 24.6; down, K = 4096 4.2 and
+// 3.7, 12 800 18.2 and 15.4).  More: waves per block and stages are the fastest of two to four choices each at hidden 1024, 1152,
+// 3200 and 4096 (they lie within 10 %).
+template <bool GATED, bool NT> static hipError_t launch_few_as(const FewArgs& a, hipStream_t s) {
   void* args[] = {(void*)&a};
+  if (a.T == 1) {
+    const bool split = a.K > 2048;
+    const void* f = split ? (const void*)one_token_kernel<4, GATED ? 2 : 4, GATED, NT> : (const void*)one_token_kernel<1, 4, GATED, NT>;
+    return hipLaunchKernel(f, dim3(split ? a.N : (a.N + 3) / 4), dim3(256), args, 0, s);
+  }
   constexpr int NW1 = GATED ? 4 : 8, NW2 = GATED ? 2 : 8, S2 = GATED ? 4 : 3, NW4 = GATED ? 2 : 4;
-  const void* f = (const void*)few_tokens_kernel<4, NW4, 3, GATED>;
+  const void* f = (const void*)few_tokens_kernel<4, NW4, 3, GATED, NT>;
   int nw = NW4;
-  if (a.T <= 16) { f = (const void*)few_tokens_kernel<1, NW1, 3, GATED>; nw = NW1; }
-  else if (a.T <= 32) { f = (const void*)few_tokens_kernel<2, NW2, S2, GATED>; nw = NW2; }
+  if (a.T <= 16) { f = (const void*)few_tokens_kernel<1, NW1, 3, GATED, NT>; nw = NW1; }
+  else if (a.T <= 32) { f = (const void*)few_tokens_kernel<2, NW2, S2, GATED, NT>; nw = NW2; }
   return hipLaunchKernel(f, dim3((a.N + 15) / 16), dim3(64 * nw), args, 0, s);
+}
+
+// Weights beyond the L2s together (32 MB) are read as non-temporal, past what X stays in: 16 tokens through 3200 x 12 800, gate and
+// up 33.8 -> 30.7 us, down 20.9 -> 20.1; through 4096 x 14 336 43.7 -> 39.1 and 24.6 -> 23.1.  Smaller ones may still be there from the call before, which
+// that would undo: both of 1024 x 4096 again and again 10.0 us, non-temporal 11.3 (on other weights each time 12.3 and 11.9).
+template <bool GATED> static hipError_t launch_few(const FewArgs& a, hipStream_t s) {
+  return (size_t)(GATED ? 2 : 1) * a.N * a.K * 2 > (32u << 20) ? launch_few_as<GATED, true>(a, s) : launch_few_as<GATED, false>(a, s);
 }
 
 // ------------------------------------------------------------------------------ transpose, column sums

@@ -55,6 +55,19 @@ def test_bf16_many_tokens(T, D, F):
     check({"y": y, **op.backward(w, x, dy, saved)}, reference("swiglu", w, x, dy))
 
 
+@pytest.mark.parametrize("act,bias", [("swiglu", True), ("geglu_erf", False), ("geglu_tanh", True)])
+@pytest.mark.parametrize("T", [1, 2])
+@pytest.mark.parametrize("D,F", [(8, 4096), (2048, 2056), (2056, 2048), (4104, 72), (72, 12808), (3200, 8200), (520, 1032)])
+def test_bf16_one_and_two_tokens(T, D, F, act, bias):
+    w, x, dy = make(T, D, F, torch.bfloat16, bias, D + F)
+    op = op_for("bf16", D, F, act, T, bias)
+    y, saved = op.forward(w, x, save=True)
+    check({"y": y, **op.backward(w, x, dy, saved)}, reference(act, w, x, dy))
+    assert torch.equal(op.forward(w, x), y)
+    one = op.forward(w, x[:1].clone())
+    assert torch.equal(op.forward(w, x[:1], out=x[:1]), one) and torch.equal(x[:1], one)                 # in place
+
+
 def test_the_large_sizes_reach_every_tile():
     plans = set()
     for T, D, F in LARGE + SIZES:
