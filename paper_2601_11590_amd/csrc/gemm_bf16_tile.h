@@ -1649,6 +1649,36 @@ template <class T> static void launch_pair(const GemmArgs& a, const GemmArgs* b,
   hipLaunchKernelGGL(gemm_bf16_pair_kernel<T>, dim3(all), dim3(T::NT), 0, s, p);
 }
 
+// A product whose K is cut into parts of k_part (a multiple of 64), each a block's own: fp32 sums [part][M][N] for a kernel that adds
+// them.  KROWS: 0 or 2.
+struct GemmSplit { GemmArgs g; int k_part; };
+template <class T, int KROWS>
+__global__ __launch_bounds__(T::NT, T::MINBLK) void gemm_bf16_split_kernel(GemmSplit p) {
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS_BYTES + T::BM * 4];
+  GemmArgs g = p.g;
+  g.zeros = zero_bytes;
+  const int tiles_n = (g.N + T::BN - 1) / T::BN, tiles_m = (g.M + T::BM - 1) / T::BM;
+  const int t = xcd_remap(blockIdx.x, gridDim.x), part = t / (tiles_m * tiles_n), k0 = part * p.k_part;
+  g.A = (const __bf16*)g.A + k0;
+  g.W = (const __bf16*)g.W + (KROWS ? (size_t)k0 * g.ldw : (size_t)k0);
+  g.out = (float*)g.out + (size_t)part * g.M * g.N;
+  g.K = min(p.k_part, g.K - k0);
+  int tm, tn;
+  tile_coords(t - part * (tiles_m * tiles_n), tiles_m, tiles_n, g.group_m, tm, tn);
+  gemm_tile<T, EPI_STORE, OUT_F32, false, false, T::PINGPONG, T::PINGPONG, KROWS>(g, tm * T::BM, tn * T::BN, lds);
+}
+
+// g.out: the sums, rows of N.
+template <class T, int KROWS> static void launch_split(const GemmArgs& g, int parts, int k_part, hipStream_t s) {
+  const int tiles_m = (g.M + T::BM - 1) / T::BM, tiles_n = (g.N + T::BN - 1) / T::BN;
+  GemmSplit p{g, k_part};
+  p.g.ldo = g.N; p.g.bias = nullptr;
+  GemmArgs of_part = g;
+  of_part.K = k_part;
+  p.g.group_m = raster_group<T>(of_part, tiles_m, tiles_n, (long)T::MINBLK * num_cus());
+  hipLaunchKernelGGL((gemm_bf16_split_kernel<T, KROWS>), dim3(tiles_m * tiles_n * parts), dim3(T::NT), 0, s, p);
+}
+
 template <int EPI, int OUT, bool GATHER, bool CLAMPED = false>
 static void launch_epi(const GemmArgs& g, hipStream_t s) {
   int t = g.tile_cfg > 0 ? g.tile_cfg - 1 : -1;   // tile_cfg: set by the tuning hook of the C ABI, or by a split

@@ -24,6 +24,25 @@ def test_every_kernel_of_the_products(T, D, F):
     assert torch.equal(op.forward(w, x), y)
 
 
+# Few rows: the long products' K in parts (in each of their tiles, two to eight parts, the last one shorter or not), joined
+@pytest.mark.parametrize("T,D,F", [(65, 1024, 4096), (130, 1160, 4312), (333, 1024, 4096), (600, 2048, 6152), (784, 3200, 12808), (1024, 2056, 6144), (1500, 1024, 8192),
+                                   (3000, 1024, 4096)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_products_in_parts(T, D, F, bias):
+    w, x, dy = make(T, D, F, torch.bfloat16, bias, T)
+    op = B.GatedMLP("bf16", D, F, act="swiglu", max_tokens=T + 9, use_bias=bias, training=True)
+    op.workspace.fill_(0xFF)                                           # nothing is read that was not written
+    wide = torch.full((T, D + 24), 7.0, dtype=torch.bfloat16, device=DEV)
+    y, saved = op.forward(w, x, save=True, out=wide[:, 8:8 + D])
+    op.workspace.fill_(0xFF)
+    grads = op.backward(w, x, dy, saved)
+    check({"y": y, **grads}, reference("swiglu", w, x, dy))
+    assert torch.equal(op.backward(w, x, dy, saved, want=["dx"])["dx"], grads["dx"])
+    assert (wide[:, :8] == 7).all() and (wide[:, 8 + D:] == 7).all()
+    again = B.GatedMLP("bf16", D, F, act="swiglu", max_tokens=T, use_bias=bias)
+    assert torch.equal(again.forward(w, x), y) and torch.equal(again.forward(w, x, out=x), y)
+
+
 def some_channels(w, channels):
     F = w["down_w"].shape[1]
     both = torch.cat([channels, channels + F])
