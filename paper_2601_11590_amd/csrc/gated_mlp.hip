@@ -25,7 +25,7 @@ namespace epd {
 // fill and nobody else reads, so no wave waits for another until their sums meet, in the order of the waves.
 //   What it replaced loaded the operands of the matrix instructions straight to registers, 16 rows x 64 bytes an instruction: half
 // lines of twice as many rows, at 4.1 TB/s where whole lines reach 5.2 (3200 x 12 800, 16 tokens: gate and up 52 -> 33.6 us, down
-// 32 -> 20.7; 64 tokens 90 -> 48 and 70 -> 36).  The GEMM's tiles take 46 and 57 us from 64 tokens down, so this one serves up to 64.
+// 32 -> 20.7).  Up to how many tokens: few_up, few_down.
 struct FewArgs {
   const void* X; const void* W; const void* bias;
   void* out;
@@ -239,7 +239,13 @@ __global__ __launch_bounds__(256) void one_token_kernel(FewArgs a) {
   ((__bf16*)a.out)[n] = (__bf16)o;
 }
 
-constexpr int kFewTokens = 64;
+// Which of the two products these kernels take, the others' being the GEMM's (K in parts where that is cheaper).  Weights not in any cache, us:
+//   gate and up  1024 x 4096: 32 tokens 6.3 (GEMM 9.8), 64 8.1 (10.2);  3200 x 12 800: 16 30.9 (35.4), 32 37.1 (37.0), 33 41.6 (37.4), 64 48.6 (40.9);
+//                2048 x 6144: 33 15.7 (15.8), 64 17.2 (16.5)
+//   down         512 x 2048: 64 5.7 (6.9);  1024 x 4096: 32 7.5 (8.2), 33 8.7 (8.1);  1152 x 4304: 16 9.5 (8.8);  3200 x 12 800: 16 20.1 (21.1), 32 25.6 (22.5)
+constexpr size_t kL2s = 32u << 20;     // bytes
+bool few_up(int T, int D, int F) { return T <= 32 || (T <= 64 && (size_t)4 * D * F <= kL2s); }
+bool few_down(int T, int F) { return T <= 16 || (T <= 64 && T * F <= 1 << 17); }
 
 // One token: rows of up to 2048 a wave each (gate and up, K = 1024 4.9 us, a block each 5.8; K = 3200 25.7 and 24.6; down, K = 4096 4.2 and
 // 3.7, 12 800 18.2 and 15.4).  More: waves per block and stages are the fastest of two to four choices each at hidden 1024, 1152,
@@ -252,10 +258,11 @@ template <bool GATED, bool NT> static hipError_t launch_few_as(const FewArgs& a,
     return hipLaunchKernel(f, dim3(split ? a.N : (a.N + 3) / 4), dim3(256), args, 0, s);
   }
   constexpr int NW1 = GATED ? 4 : 8, NW2 = GATED ? 2 : 8, S2 = GATED ? 4 : 3, NW4 = GATED ? 2 : 4;
-  const void* f = (const void*)few_tokens_kernel<4, NW4, 3, GATED, NT>;
-  int nw = NW4;
+  const void* f;
+  int nw;
   if (a.T <= 16) { f = (const void*)few_tokens_kernel<1, NW1, 3, GATED, NT>; nw = NW1; }
-  else if (a.T <= 32) { f = (const void*)few_tokens_kernel<2, NW2, S2, GATED, NT>; nw = NW2; }
+  else if (a.T <= 32 || (GATED && NT)) { f = (const void*)few_tokens_kernel<2, NW2, S2, GATED, NT>; nw = NW2; }       // (see few_up)
+  else { f = (const void*)few_tokens_kernel<4, NW4, 3, GATED, NT && !GATED>; nw = NW4; }
   return hipLaunchKernel(f, dim3((a.N + 15) / 16), dim3(64 * nw), args, 0, s);
 }
 
@@ -263,7 +270,7 @@ template <bool GATED, bool NT> static hipError_t launch_few_as(const FewArgs& a,
 // up 33.8 -> 30.7 us, down 20.9 -> 20.1; through 4096 x 14 336 43.7 -> 39.1 and 24.6 -> 23.1.  Smaller ones may still be there from the call before, which
 // that would undo: both of 1024 x 4096 again and again 10.0 us, non-temporal 11.3 (on other weights each time 12.3 and 11.9).
 template <bool GATED> static hipError_t launch_few(const FewArgs& a, hipStream_t s) {
-  return (size_t)(GATED ? 2 : 1) * a.N * a.K * 2 > (32u << 20) ? launch_few_as<GATED, true>(a, s) : launch_few_as<GATED, false>(a, s);
+  return (size_t)(GATED ? 2 : 1) * a.N * a.K * 2 > kL2s ? launch_few_as<GATED, true>(a, s) : launch_few_as<GATED, false>(a, s);
 }
 
 // ------------------------------------------------------------------------------ transpose, column sums
@@ -601,8 +608,8 @@ GatedLayout gated_layout(const epd_gated_mlp_cfg& c) {
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = up(off + bytes, 256); return o; };
   L.h = take(T * F * L.es);
-  // sums of parts of K, of Y and dX (up to kFewTokens rows of Y take none)
-  L.parts = take(bf && (c.training || T > kFewTokens) ? std::min<size_t>(T * kSplits, kSplitRows) * D * 4 : 0);
+  // sums of parts of K, of Y and dX (a few rows of Y take none)
+  L.parts = take(bf && (c.training || !few_down(c.max_tokens, c.mlp_dim)) ? std::min<size_t>(T * kSplits, kSplitRows) * D * 4 : 0);
   L.dgu = L.a_t = L.w_t = L.sums_gu = L.sums_d = 0;
   if (c.training) L.dgu = take(T * 2 * F * L.es);
   if (c.training && bf) {
@@ -712,14 +719,6 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
   const Saved keep = saved_parts(c, saved, T);
   void* const H = bf && saved ? keep.h : (char*)workspace + L.h;
   hipStream_t st = (hipStream_t)stream;
-  if (bf && T <= kFewTokens) {
-    FewArgs a{x, w->gate_up_w, c.use_bias ? w->gate_up_b : nullptr, H, keep.p, keep.q, keep.low, (int)ld_x, F, T, F, D, act_code(c)};
-    hipError_t e = launch_few<true>(a, st);
-    FewArgs b{H, w->down_w, c.use_bias ? w->down_b : nullptr, y, nullptr, nullptr, nullptr, F, (int)ld_y, T, D, F, 0};
-    if (e == hipSuccess) e = launch_few<false>(b, st);
-    if (e != hipSuccess) return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e));
-    return EPD_OK;
-  }
   GemmArgs up{}, down{};
   up.A = x; up.lda = (int)ld_x; up.W = w->gate_up_w; up.ldw = D; up.bias = c.use_bias ? w->gate_up_b : nullptr;
   up.M = T; up.N = bf ? (F + 15) / 16 * 32 : 2 * F; up.K = D; up.epilogue = EPI_GATED; up.act = act_code(c);
@@ -731,9 +730,20 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
   hipError_t e;
   if (bf) {
     const LastError last;
-    launch_gemm_bf16_gated(up, st);
-    e = launch_product(down, nullptr, nullptr, (float*)((char*)workspace + L.parts), st);
-    if (e == hipSuccess) e = last.now();
+    if (few_up(T, D, F)) {
+      const FewArgs a{x, up.W, up.bias, H, keep.p, keep.q, keep.low, up.lda, F, T, F, D, up.act};
+      e = launch_few<true>(a, st);
+    } else {
+      launch_gemm_bf16_gated(up, st);
+      e = last.now();
+    }
+    if (e == hipSuccess && few_down(T, F)) {
+      const FewArgs a{H, down.W, down.bias, y, nullptr, nullptr, nullptr, F, down.ldo, T, D, F, 0};
+      e = launch_few<false>(a, st);
+    } else if (e == hipSuccess) {
+      e = launch_product(down, nullptr, nullptr, (float*)((char*)workspace + L.parts), st);
+      if (e == hipSuccess) e = last.now();
+    }
   } else {
     F32Group a{}, b{};
     a.n = b.n = 1;

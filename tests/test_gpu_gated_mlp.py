@@ -68,6 +68,19 @@ def test_bf16_one_and_two_tokens(T, D, F, act, bias):
     assert torch.equal(op.forward(w, x[:1], out=x[:1]), one) and torch.equal(x[:1], one)                 # in place
 
 
+@pytest.mark.parametrize("T", [16, 17, 32, 33, 64])
+@pytest.mark.parametrize("D,F,act,bias", [(512, 2048, "swiglu", True), (1024, 4096, "geglu_tanh", False), (1152, 4304, "geglu_erf", True), (2056, 4104, "swiglu", True),
+                                          (8200, 2048, "swiglu", False)])
+def test_bf16_few_tokens(T, D, F, act, bias):
+    # where one or both products change from the kernels for few tokens to the tiles
+    w, x, dy = make(T, D, F, torch.bfloat16, bias, D + F)
+    op = op_for("bf16", D, F, act, T, bias)
+    y, saved = op.forward(w, x, save=True)
+    check({"y": y, **op.backward(w, x, dy, saved)}, reference(act, w, x, dy))
+    assert torch.equal(op_for("bf16", D, F, act, T, bias, training=False).forward(w, x), y)
+    assert torch.equal(op_for("bf16", D, F, act, 4 * T, bias).forward(w, x), y)
+
+
 def test_the_large_sizes_reach_every_tile():
     plans = set()
     for T, D, F in LARGE + SIZES:
