@@ -160,8 +160,9 @@ struct F32Group {
   GemmArgs g[3];
   F32Sum sum[2];
   int n, first[4];      // products; first is set by the launcher
-  long t16;             // 16 x 16 tiles and longest K of the products that the tile is chosen by (count_f32): a call's products
-  int k;                //   whether wanted or not, so that a gradient has the same bits in every call
+  long t16;             // 16 x 16 tiles, operations and longest K of the products that the tile is chosen by (count_f32): a call's
+  double flops;         //   products whether wanted or not, so that a gradient has the same bits in every call
+  int k, products;
 };
 void count_f32(F32Group& a, int M, int N, int K);
 hipError_t launch_gemm_f32_group(F32Group& a, hipStream_t s);

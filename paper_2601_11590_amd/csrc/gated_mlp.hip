@@ -344,7 +344,7 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(SumPartsArgs a) {
 
 // out[m][c] = sum_p in[p][m][c] + bias[c], parts of a cut K in their order.  Bound: the caches they are still in, and HBM.
 struct JoinArgs { const float* in; const __bf16* bias; __bf16* out; int parts, M, N, ldo; };
-constexpr int kSplits = 8, kSplitRows = 8192;       // parts, and their rows together
+constexpr int kSplits = 8, kSplitRows = 8192, kPartK = 256;       // parts, their rows together, and the shortest part
 __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
   const int i = blockIdx.x * 256 + threadIdx.x, row = i / (a.N / 8), c = (i - row * (a.N / 8)) * 8;
   if (row >= a.M) return;
@@ -522,7 +522,7 @@ static SplitPlan plan_split(const GemmArgs& g, long cus) {
   for (const ProductTile& t : kProductTiles) {
     const double f = rows_factor(t, g);
     if ((t.cfg != 0 && t.cfg != 2 && t.cfg != 7) || f == 0.0) continue;      // (the others' best lie within 1 % of these)
-    for (int n = 2; n <= kSplits && (int64_t)n * g.M <= kSplitRows && g.K / n >= 256; ++n) {
+    for (int n = 2; n <= kSplits && (int64_t)n * g.M <= kSplitRows && g.K / n >= kPartK; ++n) {
       const int k_part = (g.K + 64 * n - 1) / (64 * n) * 64, parts = (g.K + k_part - 1) / k_part;
       const double c = 0.95 * tiles_cost(t, product_tiles(t, g.M, g.N) * parts, f * k_part, 0, cus) + 3.0 + (4.0 * parts + 2.0) * g.M * (double)g.N / 4e6;
       if (c < plan.cost) plan = {t.cfg, parts, k_part, c};
@@ -608,8 +608,9 @@ GatedLayout gated_layout(const epd_gated_mlp_cfg& c) {
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = up(off + bytes, 256); return o; };
   L.h = take(T * F * L.es);
-  // sums of parts of K, of Y and dX (a few rows of Y take none)
-  L.parts = take(bf && (c.training || !few_down(c.max_tokens, c.mlp_dim)) ? std::min<size_t>(T * kSplits, kSplitRows) * D * 4 : 0);
+  // sums of parts of K, of Y and dX (a few rows of Y take none, nor a short K)
+  const bool parts = (c.training && 2 * c.mlp_dim >= 2 * kPartK) || (!few_down(c.max_tokens, c.mlp_dim) && c.mlp_dim >= 2 * kPartK);
+  L.parts = take(bf && parts ? std::min<size_t>(T * kSplits, kSplitRows) * D * 4 : 0);
   L.dgu = L.a_t = L.w_t = L.sums_gu = L.sums_d = 0;
   if (c.training) L.dgu = take(T * 2 * F * L.es);
   if (c.training && bf) {

@@ -12,6 +12,7 @@
 #include "epd_internal.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace epd {
 
@@ -40,6 +41,69 @@ __device__ __forceinline__ float gate_f32(float g, int act, float& d) {
   const float p = 1.0f / (1.0f + expf(-g));
   d = p * (1.0f + g * (1.0f - p));
   return g * p;
+}
+
+// The sums of a block in LDS to where they go.
+template <int BT, int LD, int COPIES, int NT, bool OPS>
+__device__ __forceinline__ void f32_epilogue(const GemmArgs& g, const int m0, const int n0, float (*acc_lds)[BT][LD]) {
+  // epilogue: a thread takes 4 consecutive columns (whole rotary pairs) of a row
+  const float* bias = (const float*)g.bias;
+  float* out = (float*)g.out;
+  for (int e = threadIdx.x; e < BT * BT / 4; e += NT) {
+    const int r = e / (BT / 4), c = (e - r * (BT / 4)) * 4;
+    const int m = m0 + r, n = n0 + c;
+    if (m >= g.M || n >= g.N) continue;
+    f32x4 v = *(const f32x4*)&acc_lds[0][r][c];
+#pragma unroll
+    for (int w = 1; w < COPIES; ++w) v += *(const f32x4*)&acc_lds[w][r][c];
+    const int left = min(4, g.N - n);
+    if (OPS && g.epilogue != EPI_STORE) {
+      float* const gu = (float*)g.gu + (size_t)m * g.ldgu;
+      if (g.epilogue == EPI_GATED) {
+        for (int j = 0; j < left; j += 2) {
+          const int ch = (n + j) >> 1;
+          const float gate = v[j] + (bias ? bias[ch] : 0.f), up = v[j + 1] + (bias ? bias[g.gate_rows + ch] : 0.f);
+          float d;
+          out[(size_t)m * g.ldo + ch] = gate_f32(gate, g.act, d) * up;
+          if (g.gu) { gu[ch] = gate; gu[g.gate_rows + ch] = up; }
+        }
+      } else {
+        float* const dgu = (float*)g.dgu + (size_t)m * g.lddgu;
+        for (int j = 0; j < left; ++j) {
+          float d;
+          const float up = gu[g.gate_rows + n + j], a = gate_f32(gu[n + j], g.act, d);
+          dgu[n + j] = v[j] * up * d;
+          dgu[g.gate_rows + n + j] = v[j] * a;
+          out[(size_t)m * g.ldo + n + j] = a * up;
+        }
+      }
+      continue;
+    }
+    if (bias)
+      for (int j = 0; j < left; ++j) v[j] += bias[n + j];
+    if (g.epilogue == EPI_QKV && g.rot) {
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        if (n + j + 1 < g.N && n + j < g.qk_cols) {          // even column; pair = (n + j, n + j + 1)
+          const float2 cs = g.rot[(size_t)m * g.rot_pairs + (((n + j) % g.head_dim) >> 1)];
+          const float a = v[j], b = v[j + 1];
+          v[j] = a * cs.x - b * cs.y;
+          v[j + 1] = a * cs.y + b * cs.x;
+        }
+      }
+    }
+    if (g.epilogue == EPI_GELU) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = gelu_f32(v[j], g.act);
+    }
+    float* dst = g.epilogue == EPI_RESIDUAL ? g.resid + (size_t)m * g.ldr + n : out + (size_t)m * g.ldo + n;
+    if (left == 4 && ((size_t)dst & 15) == 0) {
+      if (g.epilogue == EPI_RESIDUAL) v += *(const f32x4*)dst;
+      *(f32x4*)dst = v;
+    } else {
+      for (int j = 0; j < left; ++j) dst[j] = g.epilogue == EPI_RESIDUAL ? dst[j] + v[j] : v[j];
+    }
+  }
 }
 
 // A block of NW waves.  SPLIT: all of them share one 16 T x 16 T tile and take its K in turn, 32 at a
@@ -162,64 +226,153 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int m0, c
       *(f32x4*)&acc_lds[SPLIT ? wave : 0][wm + j * 16 + l16][wn + i * 16 + g4 * 4] = acc[i][j];
   __syncthreads();
 
-  // epilogue: a thread takes 4 consecutive columns (whole rotary pairs) of a row
-  const float* bias = (const float*)g.bias;
-  float* out = (float*)g.out;
-  for (int e = tid; e < BT * BT / 4; e += 64 * NW) {
-    const int r = e / (BT / 4), c = (e - r * (BT / 4)) * 4;
-    const int m = m0 + r, n = n0 + c;
-    if (m >= g.M || n >= g.N) continue;
-    f32x4 v = *(const f32x4*)&acc_lds[0][r][c];
+  f32_epilogue<BT, F32Tile<T, NW, SPLIT>::LD, COPIES, 64 * NW, OPS>(g, m0, n0, acc_lds);
+}
+
+// 64 x 64 tiles of the gated MLP's products (OPS of gemm_f32_tile) with both operands through LDS, 32 k a step and the next two steps' in
+// registers meanwhile; four waves of 32 x 32.  Rows are padded to 36 floats: the 16 rows of a fragment's 16-byte reads lie in different banks.
+// Bound: the fp32 matrix instructions, two thirds of whose rate long calls reach.
+struct F32Lds { static constexpr int BT = 64, BK = 32, LDK = BK + 4, LD = BT + 4, FLOATS = 4 * BT * LDK; };
+
+// An operand's rows along k: a thread has 4 k of rows tid / 8 and 32 further; across (element k of row r at k * ld + r): 4 rows of k = tid / 16
+// and 16 further.  Rows beyond the matrix repeat its last one: they only feed sums that are never stored.
+template <bool ACROSS> struct F32Operand {
+  const float* at[2];
+  size_t step;                         // floats from one k to the next
+  int last;                            // across: of the thread's 4 rows the last one that exists, 0 at least
+  __device__ __forceinline__ F32Operand(const void* base, int ld, int r0, int rows, int gate_rows) {
+    const int tid = threadIdx.x;
+    if constexpr (ACROSS) {
+      const int r = min(r0 + (tid & 15) * 4, rows - 1);
+      step = ld; last = min(3, rows - 1 - r);
 #pragma unroll
-    for (int w = 1; w < COPIES; ++w) v += *(const f32x4*)&acc_lds[w][r][c];
-    const int left = min(4, g.N - n);
-    if (OPS && g.epilogue != EPI_STORE) {
-      float* const gu = (float*)g.gu + (size_t)m * g.ldgu;
-      if (g.epilogue == EPI_GATED) {
-        for (int j = 0; j < left; j += 2) {
-          const int ch = (n + j) >> 1;
-          const float gate = v[j] + (bias ? bias[ch] : 0.f), up = v[j + 1] + (bias ? bias[g.gate_rows + ch] : 0.f);
-          float d;
-          out[(size_t)m * g.ldo + ch] = gate_f32(gate, g.act, d) * up;
-          if (g.gu) { gu[ch] = gate; gu[g.gate_rows + ch] = up; }
-        }
-      } else {
-        float* const dgu = (float*)g.dgu + (size_t)m * g.lddgu;
-        for (int j = 0; j < left; ++j) {
-          float d;
-          const float up = gu[g.gate_rows + n + j], a = gate_f32(gu[n + j], g.act, d);
-          dgu[n + j] = v[j] * up * d;
-          dgu[g.gate_rows + n + j] = v[j] * a;
-          out[(size_t)m * g.ldo + n + j] = a * up;
-        }
-      }
-      continue;
-    }
-    if (bias)
-      for (int j = 0; j < left; ++j) v[j] += bias[n + j];
-    if (g.epilogue == EPI_QKV && g.rot) {
-#pragma unroll
-      for (int j = 0; j < 4; j += 2) {
-        if (n + j + 1 < g.N && n + j < g.qk_cols) {          // even column; pair = (n + j, n + j + 1)
-          const float2 cs = g.rot[(size_t)m * g.rot_pairs + (((n + j) % g.head_dim) >> 1)];
-          const float a = v[j], b = v[j + 1];
-          v[j] = a * cs.x - b * cs.y;
-          v[j + 1] = a * cs.y + b * cs.x;
-        }
-      }
-    }
-    if (g.epilogue == EPI_GELU) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = gelu_f32(v[j], g.act);
-    }
-    float* dst = g.epilogue == EPI_RESIDUAL ? g.resid + (size_t)m * g.ldr + n : out + (size_t)m * g.ldo + n;
-    if (left == 4 && ((size_t)dst & 15) == 0) {
-      if (g.epilogue == EPI_RESIDUAL) v += *(const f32x4*)dst;
-      *(f32x4*)dst = v;
+      for (int i = 0; i < 2; ++i) at[i] = (const float*)base + r + (size_t)((tid >> 4) + i * 16) * ld;
     } else {
-      for (int j = 0; j < left; ++j) dst[j] = g.epilogue == EPI_RESIDUAL ? dst[j] + v[j] : v[j];
+      step = 1; last = 3;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        int r = min(r0 + (tid >> 3) + i * 32, rows - 1);
+        if (gate_rows) r = (r >> 1) + (r & 1) * gate_rows;
+        at[i] = (const float*)base + (size_t)r * ld + (tid & 7) * 4;
+      }
     }
   }
+  // a whole step; EDGE: the tile has rows beyond the matrix (across)
+  template <bool EDGE> __device__ __forceinline__ void load(f32x4* v, int k0) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float* const p = at[i] + (size_t)k0 * step;
+      if constexpr (ACROSS && EDGE) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[i][c] = p[min(c, last)];
+      } else {
+        v[i] = *(const f32x4_any*)p;
+      }
+    }
+  }
+  // the last step of a K that is no multiple of 32: zeros from K on
+  __device__ __forceinline__ void load_rest(f32x4* v, int k0, int K) const {
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k = k0 + (ACROSS ? (tid >> 4) + i * 16 : (tid & 7) * 4);
+      const float* const p = at[i] + (size_t)k0 * step;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[i][c] = (ACROSS ? k : k + c) < K ? p[ACROSS ? min(c, last) : c] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void put(const f32x4* v, float* t) const {
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (ACROSS) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) t[((tid & 15) * 4 + c) * F32Lds::LDK + (tid >> 4) + i * 16] = v[i][c];
+      } else {
+        *(f32x4*)&t[((tid >> 3) + i * 32) * F32Lds::LDK + (tid & 7) * 4] = v[i];
+      }
+    }
+  }
+};
+
+template <bool AK, bool WK, bool EDGE>
+__device__ __forceinline__ void gemm_f32_lds_loop(const GemmArgs& g, const int m0, const int n0, float* const lds, f32x4 (*acc)[2]) {
+  constexpr int BT = F32Lds::BT, BK = F32Lds::BK, LDK = F32Lds::LDK;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g4 = lane >> 4, wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
+  float* const tile[2] = {lds, lds + 2 * BT * LDK};          // A, W: two stages each
+  const F32Operand<AK> A(g.A, g.lda, m0, g.M, 0);
+  const F32Operand<WK> W(g.W, g.ldw, n0, g.N, g.epilogue == EPI_GATED ? g.gate_rows : 0);
+  auto multiply = [&](int s) {
+    const float* const ta = tile[0] + s * BT * LDK + (wm + l16) * LDK + g4 * 4;
+    const float* const tw = tile[1] + s * BT * LDK + (wn + l16) * LDK + g4 * 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4 fa[2], fw[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) { fa[j] = *(const f32x4*)(ta + j * 16 * LDK + h * 16); fw[j] = *(const f32x4*)(tw + j * 16 * LDK + h * 16); }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[i][c], fa[j][c], acc[i][j], 0, 0, 0);
+    }
+  };
+  const int whole = g.K / BK;
+  if (whole) {
+    // loads beyond the last whole step repeat it, so that every step issues as many and waits for the older ones only
+    auto load = [&](f32x4* a, f32x4* w, int i) { const int k0 = min(i, whole - 1) * BK; A.template load<EDGE>(a, k0); W.template load<EDGE>(w, k0); };
+    f32x4 va[2][2], vw[2][2];
+    load(va[1], vw[1], 0);
+    load(va[0], vw[0], 1);
+    A.put(va[1], tile[0]); W.put(vw[1], tile[1]);
+    load(va[1], vw[1], 2);
+    auto step = [&](auto STAGE, int i) {                     // stage s and register set s
+      constexpr int s = decltype(STAGE)::value;
+      __syncthreads();                                       // stage s is written; stage s ^ 1 has been read
+      multiply(s);
+      A.put(va[s], tile[0] + (s ^ 1) * BT * LDK); W.put(vw[s], tile[1] + (s ^ 1) * BT * LDK);
+      load(va[s], vw[s], i + 3);
+    };
+    for (int i = 0; i < whole; i += 2) {
+      step(std::integral_constant<int, 0>{}, i);
+      if (i + 1 >= whole) break;
+      step(std::integral_constant<int, 1>{}, i + 1);
+    }
+  }
+  if (whole * BK < g.K) {
+    f32x4 a[2], w[2];
+    A.load_rest(a, whole * BK, g.K); W.load_rest(w, whole * BK, g.K);
+    __syncthreads();                                         // both stages have been read
+    A.put(a, tile[0]); W.put(w, tile[1]);
+    __syncthreads();
+    multiply(0);
+  }
+}
+
+__device__ __forceinline__ void gemm_f32_lds_tile(const GemmArgs& g, const int m0, const int n0, float* const lds) {
+  constexpr int BT = F32Lds::BT;
+  f32x4 acc[2][2];                                           // [n][m]: a lane holds 4 consecutive n of one m
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const bool edge = m0 + BT > g.M || n0 + BT > g.N;
+  if (!g.w_rows) gemm_f32_lds_loop<false, false, false>(g, m0, n0, lds, acc);
+  else if (!g.a_rows && !edge) gemm_f32_lds_loop<false, true, false>(g, m0, n0, lds, acc);
+  else if (!g.a_rows) gemm_f32_lds_loop<false, true, true>(g, m0, n0, lds, acc);
+  else if (!edge) gemm_f32_lds_loop<true, true, false>(g, m0, n0, lds, acc);
+  else gemm_f32_lds_loop<true, true, true>(g, m0, n0, lds, acc);
+  __syncthreads();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
+  auto* const out = (float (*)[BT][F32Lds::LD])lds;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) *(f32x4*)&out[0][(wave >> 1) * 32 + j * 16 + l16][(wave & 1) * 32 + i * 16 + g4 * 4] = acc[i][j];
+  __syncthreads();
+  f32_epilogue<BT, F32Lds::LD, 1, 256, true>(g, m0, n0, out);
 }
 
 template <int T, int NW, bool SPLIT, bool VEC>
@@ -232,18 +385,15 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_kernel(GemmArgs g) {
 // Up to three products and two sets of column sums in one launch: products of the sizes this path serves leave most of the
 // chip idle, and what is left of a launch is its latency (8 ... 14 us each, the backward pass of 257 tokens through 256 x 1024
 // was 12 launches and 79 us).  Blocks first[i] .. first[i + 1] - 1 make product i; then 16 columns of a sum each, 16 rows at a time.
-template <int T, int NW, bool SPLIT, bool VEC>
-__global__ __launch_bounds__(64 * NW) void gemm_f32_group_kernel(F32Group a) {
-  using F = F32Tile<T, NW, SPLIT>;
-  __shared__ __attribute__((aligned(16))) float acc_lds[F::COPIES][F::BT][F::LD];
-  int b = blockIdx.x, i = 0;
+// The product that block b is of, and its number there; the group's sums follow as product a.n.
+__device__ __forceinline__ int group_member(const F32Group& a, int& b) {
+  int i = 0;
   while (i < a.n && b >= a.first[i + 1]) ++i;
   b -= a.first[i];
-  if (i < a.n) {
-    const int tiles_n = (a.g[i].N + F::BT - 1) / F::BT, tm = b / tiles_n;
-    gemm_f32_tile<T, NW, SPLIT, VEC, true>(a.g[i], tm * F::BT, (b - tm * tiles_n) * F::BT, acc_lds);
-    return;
-  }
+  return i;
+}
+
+template <int NW> __device__ __forceinline__ void group_sums(const F32Group& a, int b, float* const part) {      // part: [RG][16]
   const int blocks0 = (a.sum[0].cols + 15) / 16;
   const F32Sum& s = a.sum[b >= blocks0];
   if (b >= blocks0) b -= blocks0;
@@ -254,7 +404,6 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_group_kernel(F32Group a) {
 #pragma unroll 8
     for (int r = r0; r < s.rows; r += RG) v += s.in[(size_t)r * s.ld + c];
   }
-  float* const part = &acc_lds[0][0][0];                     // [RG][16]
   part[threadIdx.x] = v;
   __syncthreads();
   if (threadIdx.x < 16 && c < s.cols) {
@@ -263,34 +412,67 @@ __global__ __launch_bounds__(64 * NW) void gemm_f32_group_kernel(F32Group a) {
   }
 }
 
-template <int T, int NW, bool SPLIT> static hipError_t launch_group_f32(F32Group& a, hipStream_t s) {
+template <int T, int NW, bool SPLIT, bool VEC>
+__global__ __launch_bounds__(64 * NW) void gemm_f32_group_kernel(F32Group a) {
   using F = F32Tile<T, NW, SPLIT>;
-  static_assert(sizeof(float) * F::COPIES * F::BT * F::LD >= 64 * NW * sizeof(float), "partial sums");
-  bool vec = true;
+  __shared__ __attribute__((aligned(16))) float acc_lds[F::COPIES][F::BT][F::LD];
+  static_assert(sizeof(acc_lds) >= 64 * NW * sizeof(float), "partial sums");
+  int b = blockIdx.x;
+  const int i = group_member(a, b);
+  if (i == a.n) { group_sums<NW>(a, b, &acc_lds[0][0][0]); return; }
+  const int tiles_n = (a.g[i].N + F::BT - 1) / F::BT, tm = b / tiles_n;
+  gemm_f32_tile<T, NW, SPLIT, VEC, true>(a.g[i], tm * F::BT, (b - tm * tiles_n) * F::BT, acc_lds);
+}
+
+__global__ __launch_bounds__(256, 4) void gemm_f32_lds_group_kernel(F32Group a) {
+  __shared__ __attribute__((aligned(16))) float lds[F32Lds::FLOATS];
+  int b = blockIdx.x;
+  const int i = group_member(a, b);
+  if (i == a.n) { group_sums<4>(a, b, lds); return; }
+  const int tiles_n = (a.g[i].N + F32Lds::BT - 1) / F32Lds::BT, tm = b / tiles_n;
+  gemm_f32_lds_tile(a.g[i], tm * F32Lds::BT, (b - tm * tiles_n) * F32Lds::BT, lds);
+}
+
+static int group_blocks(F32Group& a, int bt) {
   a.first[0] = 0;
+  for (int i = 0; i < a.n; ++i) a.first[i + 1] = a.first[i] + ((a.g[i].M + bt - 1) / bt) * ((a.g[i].N + bt - 1) / bt);
+  return a.first[a.n] + (a.sum[0].cols + 15) / 16 + (a.sum[1].cols + 15) / 16;
+}
+
+template <int T, int NW> static hipError_t launch_group_f32(F32Group& a, hipStream_t s) {
+  bool vec = true;
   for (int i = 0; i < a.n; ++i) {
     const GemmArgs& g = a.g[i];
-    a.first[i + 1] = a.first[i] + ((g.M + F::BT - 1) / F::BT) * ((g.N + F::BT - 1) / F::BT);
     vec = vec && (g.a_rows || (g.K % 4 == 0 && g.lda % 4 == 0 && (size_t)g.A % 16 == 0)) && (g.w_rows || (g.K % 4 == 0 && g.ldw % 4 == 0 && (size_t)g.W % 16 == 0));
   }
-  const int blocks = a.first[a.n] + (a.sum[0].cols + 15) / 16 + (a.sum[1].cols + 15) / 16;
   void* args[] = {(void*)&a};
-  return hipLaunchKernel(vec ? (const void*)gemm_f32_group_kernel<T, NW, SPLIT, true> : (const void*)gemm_f32_group_kernel<T, NW, SPLIT, false>, dim3(blocks), dim3(64 * NW), args, 0, s);
+  const int blocks = group_blocks(a, F32Tile<T, NW, true>::BT);
+  return hipLaunchKernel(vec ? (const void*)gemm_f32_group_kernel<T, NW, true, true> : (const void*)gemm_f32_group_kernel<T, NW, true, false>, dim3(blocks), dim3(64 * NW), args, 0, s);
+}
+
+static hipError_t launch_lds_group_f32(F32Group& a, hipStream_t s) {
+  void* args[] = {(void*)&a};
+  const int blocks = group_blocks(a, F32Lds::BT);
+  return hipLaunchKernel((const void*)gemm_f32_lds_group_kernel, dim3(blocks), dim3(256), args, 0, s);
 }
 
 void count_f32(F32Group& a, int M, int N, int K) {
   a.t16 += (long)((M + 15) / 16) * ((N + 15) / 16);
   a.k = std::max(a.k, K);
+  a.flops += 2.0 * M * N * K;
+  ++a.products;
 }
 
-// K over eight waves: 16 x 16 tiles while they are few, or while one of the products is a few tiles of a long K (the backward
-// pass of 257 tokens, 256 x 1024: 23 us; 27 in 32 x 32 tiles, 34 with K over four waves), else 32 x 32 (1000 tokens,
-// 512 x 2048: 202 us backward; 240 in 16 x 16, 305 in 64 x 64 blocks); 64 x 64 blocks of four wave tiles where there are many tiles of
-// a short K (2048 tokens, gate and up of 512 x 2048: 177 us, 191 in 32 x 32).
+// Tiles through LDS where their work is long against the longest chain of steps (0.75 us each: 32 k): 1024 x 4096, 512 tokens forward 250 -> 170 us and
+// backward 474 -> 318, 2048 tokens 957 -> 470 (109 TFLOP/s) and 1941 -> 1010; 512 x 2048 backward, 1000 tokens 256 -> 210, 512 tokens 133, but 142
+// through LDS; 64 x 256, 8192 tokens 118, but 258.  One long product alone pays sooner, its chains share the units with nothing: down of 1000 x
+// 512 x 2048 71 -> 50.  Below that, K over eight waves: 16 x 16 tiles while they are few, or while one of the
+// products is a few tiles of a long K (the backward pass of 257 tokens, 256 x 1024: 23 us; 27 in 32 x 32 tiles, 34 with K over four waves),
+// else 32 x 32.
 hipError_t launch_gemm_f32_group(F32Group& a, hipStream_t s) {
-  if (a.t16 <= 1024 || (a.k >= 1024 && a.t16 <= 3500)) return launch_group_f32<1, 8, true>(a, s);
-  if (a.t16 >= 20000 && a.k <= 512) return launch_group_f32<2, 4, false>(a, s);
-  return launch_group_f32<2, 8, true>(a, s);
+  if (a.flops >= (a.products == 1 && a.k >= 1024 ? 1e6 : 1.4e6) * a.k) return launch_lds_group_f32(a, s);
+  if (a.t16 <= 1024 || (a.k >= 1024 && a.t16 <= 3500)) return launch_group_f32<1, 8>(a, s);
+  return launch_group_f32<2, 8>(a, s);
 }
 
 template <int T, int NW, bool SPLIT> static void launch_tile_f32(const GemmArgs& g, hipStream_t s) {

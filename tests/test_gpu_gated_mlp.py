@@ -42,6 +42,20 @@ def test_f32_training_step(T, D, F, act, bias):
     assert torch.equal(op.forward(w, x), y)
 
 
+# tiles through LDS for some or all products: whole and ragged K, edges across and along, a K below one step, rows apart
+@pytest.mark.parametrize("T,D,F", [(700, 1024, 1030), (1111, 517, 643), (2049, 350, 1030), (40_000, 20, 30), (1024, 512, 2048), (3000, 255, 129), (6001, 128, 64)])
+def test_f32_many_tokens(T, D, F):
+    w, x, dy = make(T, D, F, torch.float32, True, T)
+    op = op_for("f32", D, F, "geglu_erf", T, True)
+    wide = torch.full((T, D + 3), 5.0, device=DEV)
+    y, saved = op.forward(w, x, save=True, out=wide[:, 1:1 + D])
+    grads = op.backward(w, x, dy, saved)
+    check({"y": y, **grads}, reference("geglu_erf", w, x, dy))
+    assert torch.equal(op.forward(w, x), y) and (wide[:, 0] == 5).all() and (wide[:, 1 + D:] == 5).all()
+    for n in ("dx", "down_w"):
+        assert torch.equal(op.backward(w, x, dy, saved, want=[n])[n], grads[n])
+
+
 # sizes whose first product is planned in each of the large tiles, with rows behind whole tiles, channels that no tile
 # divides and inner dimensions that are and are not whole K steps
 LARGE = [(2049, 1024, 1024), (3000, 1152, 4304), (5003, 1160, 2056), (6273, 320, 1288), (9001, 256, 2560), (12545, 64, 136)]
