@@ -94,3 +94,48 @@ def test_rotation_of_more_than_2_31_elements(dtype, pairing, T, H, d, pairs):
     op.apply([y], pos, inverse=True, out=[y])                          # back, from rows rounded once: checked below in float64
     rows = torch.unique(torch.cat([torch.randint(0, T, (100,), generator=torch.Generator().manual_seed(7)), torch.arange(3), torch.arange(T - 3, T)])).to(DEV)
     check_rope(y[rows], x[rows], pos[:, rows], pairs, "sections", "axis", pairing, inverse=True)
+
+
+@pytest.mark.parametrize("T,D,F", [(2001, 1024, 2048), (130, 1024, 4096), (5000, 328, 1288)])
+def test_a_gradient_alone_has_the_bits_of_the_whole_call(T, D, F):
+    w, x, dy = make(T, D, F, torch.bfloat16, True, T)
+    op = B.GatedMLP("bf16", D, F, max_tokens=T, use_bias=True, training=True)
+    _, saved = op.forward(w, x, save=True)
+    whole = op.backward(w, x, dy, saved)
+    for want in ([n] for n in whole):
+        assert torch.equal(op.backward(w, x, dy, saved, want=want)[want[0]], whole[want[0]]), want
+    some = op.backward(w, x, dy, saved, want=["down_w", "dx"])
+    assert torch.equal(some["down_w"], whole["down_w"]) and torch.equal(some["dx"], whole["dx"])
+
+
+@pytest.mark.parametrize("dtype,T,D,F", [("bf16", 130, 1024, 4096), ("bf16", 1, 2056, 4104), ("bf16", 40, 512, 2048), ("f32", 1024, 256, 1024)])
+def test_two_objects_in_graphs_on_two_streams(dtype, T, D, F):
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    w, x, dy = make(T, D, F, t, True, 8)
+    ops = [B.GatedMLP(dtype, D, F, act="geglu_erf", max_tokens=T, use_bias=True, training=True) for _ in range(2)]
+
+    def step(op):
+        y, saved = op.forward(w, x, save=True)
+        return {"y": y, **op.backward(w, x, dy, saved)}
+
+    step(ops[0])
+    torch.cuda.synchronize()
+    graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in ops]
+    for op in ops:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(step(op))
+        graphs.append(graph)
+    for seed in (30, 31, 32):
+        _, x1, dy1 = make(T, D, F, t, True, seed)
+        x.copy_(x1)
+        dy.copy_(dy1)
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        eager = step(B.GatedMLP(dtype, D, F, act="geglu_erf", max_tokens=T, use_bias=True, training=True))
+        torch.cuda.synchronize()
+        for got in outs:
+            assert all(torch.equal(got[n], eager[n]) for n in eager)
