@@ -326,20 +326,24 @@ __global__ __launch_bounds__(256) void part_sums_kernel(PartSums a) {
 }
 
 struct SumParts { const float* in; __bf16* out; int parts, cols; };
-struct SumPartsArgs { SumParts job[2]; int blocks0; };                            // blocks of 64 columns: those of job 0, then of job 1
+struct SumPartsArgs { SumParts job[2]; int blocks0; };                            // blocks of 16 columns: those of job 0, then of job 1
 __global__ __launch_bounds__(256) void sum_parts_kernel(SumPartsArgs a) {
-  __shared__ float part[4][64];
+  __shared__ float part[16][16];
   const bool second = (int)blockIdx.x >= a.blocks0;
   const SumParts& s = a.job[second];
-  const int c = ((int)blockIdx.x - (second ? a.blocks0 : 0)) * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
+  const int l = threadIdx.x & 15, c = ((int)blockIdx.x - (second ? a.blocks0 : 0)) * 16 + l, g = threadIdx.x >> 4;
   float v = 0.f;
   if (c < s.cols) {
 #pragma unroll 8
-    for (int p = g; p < s.parts; p += 4) v += s.in[(size_t)p * s.cols + c];
+    for (int p = g; p < s.parts; p += 16) v += s.in[(size_t)p * s.cols + c];
   }
-  part[g][threadIdx.x & 63] = v;
+  part[g][l] = v;
   __syncthreads();
-  if (g == 0 && c < s.cols) s.out[c] = (__bf16)((part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]));
+  if (g == 0 && c < s.cols) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v += part[i][l];
+    s.out[c] = (__bf16)v;
+  }
 }
 
 // out[m][c] = sum_p in[p][m][c] + bias[c], parts of a cut K in their order.  Bound: the caches they are still in, and HBM.
@@ -596,8 +600,8 @@ struct GatedLayout {
   size_t h, parts, dgu, a_t, w_t, sums_gu, sums_d, total;
 };
 
-constexpr int kParts = 512;             // partial sums of dY at most, of 64 rows or more each
-int part_rows(int tokens) { return std::max(64, (tokens + kParts - 1) / kParts); }
+constexpr int kParts = 512, kPartRows = 16;            // partial sums of dY at most, of 16 rows or more each (6272 x 1024 in 64 rows each: 10 us, not 5)
+int part_rows(int tokens) { return std::max(kPartRows, (tokens + kParts - 1) / kParts); }
 
 GatedLayout gated_layout(const epd_gated_mlp_cfg& c) {
   GatedLayout L;
@@ -618,7 +622,7 @@ GatedLayout gated_layout(const epd_gated_mlp_cfg& c) {
     L.a_t = take(std::max(2 * F, D) * Tp * L.es);                                   // (dG | dU)^T, dY^T
     L.w_t = take(std::max(std::max(D, F) * Tp, 2 * F * D) * L.es);                  // X^T, H^T, Wd^T, Wgu^T
     L.sums_gu = take(c.use_bias ? (up(T, 64) / 32 + 2) * 2 * F * 4 : 0);            // two rows per tile of 64 rows or more; a cut launch has a tile more
-    L.sums_d = take(c.use_bias ? std::min<size_t>(kParts, (T + 63) / 64) * D * 4 : 0);
+    L.sums_d = take(c.use_bias ? std::min<size_t>(kParts, (T + kPartRows - 1) / kPartRows) * D * 4 : 0);
   }
   L.total = off;
   return L;
@@ -834,9 +838,9 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
     sums.job[1] = SumParts{p.out, (__bf16*)grads->down_b, parts, iD};
   }
   if (sums.job[0].cols || sums.job[1].cols) {
-    sums.blocks0 = (sums.job[0].cols + 63) / 64;
+    sums.blocks0 = (sums.job[0].cols + 15) / 16;
     void* args[] = {(void*)&sums};
-    if (!ok(hipLaunchKernel((const void*)sum_parts_kernel, dim3(sums.blocks0 + (sums.job[1].cols + 63) / 64), dim3(256), args, 0, st))) return failed();
+    if (!ok(hipLaunchKernel((const void*)sum_parts_kernel, dim3(sums.blocks0 + (sums.job[1].cols + 15) / 16), dim3(256), args, 0, st))) return failed();
   }
   if (grads->dx && !ok(launch_product(dx, nullptr, ws + L.w_t, (float*)(ws + L.parts), st))) return failed();
   if (!ok(launch_products(dgu, grads->gate_up_w, dd, grads->down_w, ws + L.a_t, ws + L.w_t, st))) return failed();
