@@ -600,7 +600,10 @@ def epd_rope_tokens(span_thw: np.ndarray) -> int:
 def epd_rope_positions(span_thw: np.ndarray, cu_spans: np.ndarray, start: Optional[np.ndarray], t_step: int, positions: int,
                        position_stride: int, stream: int) -> np.ndarray:
     """Returns the next position of every sequence, int32 [num_sequences]."""
-    span, cu = _spans(span_thw, cu_spans)
+    return _positions(*_spans(span_thw, cu_spans), start, t_step, positions, position_stride, stream)
+
+
+def _positions(span: np.ndarray, cu: np.ndarray, start, t_step: int, positions: int, position_stride: int, stream: int) -> np.ndarray:
     n = len(cu) - 1
     if start is not None:
         start = np.ascontiguousarray(start, dtype=np.int32)
@@ -621,7 +624,7 @@ def _spans(span_thw, cu_spans):
         span_thw = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
     if type(cu_spans) is not np.ndarray or cu_spans.dtype != np.int32 or not cu_spans.flags.c_contiguous:
         cu_spans = np.ascontiguousarray(cu_spans, dtype=np.int32)
-    if cu_spans.ndim != 1 or len(cu_spans) < 1 or int(cu_spans.max()) > len(span_thw):
+    if cu_spans.ndim != 1 or len(cu_spans) < 1 or int(cu_spans[-1]) > len(span_thw):      # the library refuses cu_spans that decrease
         raise ValueError("cu_spans must be [num_sequences + 1] and end within the spans")
     return span_thw, cu_spans
 
@@ -652,7 +655,7 @@ def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str 
         out = torch.empty((3, tokens), dtype=torch.int32, device=dev)
     if not out.is_cuda or out.dtype != torch.int32 or out.dim() != 2 or out.shape[0] != 3 or out.shape[1] < tokens or (out.shape[1] and out.stride(1) != 1):
         raise ValueError("out must be a device int32 [3, >= tokens] whose rows are contiguous")
-    return out, _on(dev.index, epd_rope_positions, span, cu, start, t_step, out.data_ptr() or 256, out.stride(0))      # no tokens: nothing is written
+    return out, _on(dev.index, _positions, span, cu, start, t_step, out.data_ptr() or 256, out.stride(0))      # no tokens: nothing is written
 
 
 class Rope:

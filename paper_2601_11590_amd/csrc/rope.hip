@@ -321,6 +321,8 @@ epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, 
   if (num_sequences < 0) return op_fail(EPD_ERR_SHAPE, "epd_rope_positions: num_sequences %d", num_sequences);
   if (t_step < 0) return op_fail(EPD_ERR_INVALID_ARG, "epd_rope_positions: t_step %d", t_step);
   if (cu_spans[0] != 0) return op_fail(EPD_ERR_SHAPE, "epd_rope_positions: cu_spans must start at 0");
+  for (int s = 0; s < num_sequences; ++s)                  // first: the spans end at the last of cu_spans
+    if (cu_spans[s + 1] < cu_spans[s]) return op_fail(EPD_ERR_SHAPE, "epd_rope_positions: cu_spans decreases at %d", s);
   // everything is checked before the first launch: two walks over the spans
   for (int pass = 0; pass < 2; ++pass) {
     int64_t tok = 0, sent = 0;
@@ -337,7 +339,6 @@ epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, 
       return e;
     };
     for (int s = 0; s < num_sequences; ++s) {
-      if (!pass && cu_spans[s + 1] < cu_spans[s]) return op_fail(EPD_ERR_SHAPE, "epd_rope_positions: cu_spans decreases at %d", s);
       int64_t pos = start ? start[s] : 0;
       for (int i = cu_spans[s]; i < cu_spans[s + 1]; ++i) {
         const int64_t t = span_thw[3 * (int64_t)i], h = span_thw[3 * (int64_t)i + 1], w = span_thw[3 * (int64_t)i + 2];

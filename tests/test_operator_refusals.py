@@ -128,6 +128,7 @@ def pos(spans, cu, start=None, t_step=1, positions=0x1000, stride=1 << 40):
     (dict(spans=[(1, -2, -2)], cu=[0, 1]), "span 0"),
     (dict(spans=[(3, 0, 0)], cu=[1, 1]), "start at 0"),
     (dict(spans=[(3, 0, 0), (3, 0, 0)], cu=[0, 2, 1]), "decreases"),
+    (dict(spans=[(3, 0, 0)], cu=[0, 1 << 30, 1]), "decreases"),        # before a span beyond the last is read
     (dict(spans=[(2, 65536, 65536)], cu=[0, 1]), "too many tokens"),
     (dict(spans=[(2 ** 31 - 1, 0, 0), (1, 0, 0)], cu=[0, 1, 2]), "more than"),
     (dict(spans=[(3, 0, 0)], cu=[0, 1], start=[2 ** 31 - 3]), "position"),
