@@ -12,9 +12,9 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 
 
-# Together these reach each tile with each epilogue (plain, gated, gated and kept, backward), operands as they stand and turned,
-# read along their rows and across them, in one launch and cut into two.
-@pytest.mark.parametrize("T,D,F", [(530, 4624, 1928), (2091, 824, 10000), (4692, 1192, 1872), (7259, 1168, 3344), (9754, 792, 1880), (13071, 1648, 280),
+# Together with those in parts below and the smaller ones of test_gpu_gated_mlp.py these reach each tile with each epilogue (plain, gated, gated
+# and kept, backward), operands as they stand and turned, read along their rows and across them, in one launch and cut into two.
+@pytest.mark.parametrize("T,D,F", [(530, 4624, 1928), (585, 1112, 10104), (2091, 824, 10000), (4692, 1192, 1872), (7259, 1168, 3344), (9754, 792, 1880), (13071, 1648, 280),
                                    (13600, 1792, 1304), (20118, 848, 72)])
 def test_every_kernel_of_the_products(T, D, F):
     w, x, dy = make(T, D, F, torch.bfloat16, True, T)
