@@ -293,6 +293,11 @@ epd_status epd::op_fail(epd_status status, const char* format, ...) {
   return status;
 }
 
+epd_status epd::op_launch_failed(const char* who, hipError_t e) {
+  (void)hipGetLastError();
+  return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e));
+}
+
 extern "C" {
 
 const char* epd_op_last_error(void) { return g_op_error; }
@@ -515,7 +520,7 @@ epd_status epd_encode(epd_handle h, const void* packed_patches, const int32_t* c
     g.tile_cfg = h->tile_cfg;
     g.compute_units = h->compute_units;
     if (!bf) launch_gemm_f32(g, st);
-    else if (g.epilogue == EPI_GATED) launch_gemm_bf16_gated(g, st);
+    else if (g.epilogue == EPI_GATED) (void)launch_gemm_bf16_gated(g, st, nullptr);      // a failure is the runtime's last error, as those of the others
     else launch_gemm_bf16(g, st);
   };
   auto norm = [&](const void* gma, const void* bta, void* dst) {

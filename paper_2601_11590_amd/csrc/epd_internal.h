@@ -168,7 +168,7 @@ void count_f32(F32Group& a, int M, int N, int K);
 hipError_t launch_gemm_f32_group(F32Group& a, hipStream_t s);
 bool launch_attn_f32(const AttnArgs& a, hipStream_t s);   // false: head_dim not covered
 void launch_gemm_bf16(const GemmArgs& g, hipStream_t s);
-int launch_gemm_bf16_gated(const GemmArgs& g, hipStream_t s);   // EPI_STORE (bf16 out), EPI_GATED, EPI_DGATED; zeros, overread_* are not used
+hipError_t launch_gemm_bf16_gated(const GemmArgs& g, hipStream_t s, int* filled);   // EPI_STORE (bf16 out), EPI_GATED, EPI_DGATED; zeros, overread_* are not used
 // How launch_gemm_bf16 would tile g on a chip of compute_units units (<= 0: the current device's;
 // host only, launches nothing): the tile of the first or only launch, and the rows that launch
 // covers when the rest is left to a second launch of smaller tiles (0 = one launch covers all).

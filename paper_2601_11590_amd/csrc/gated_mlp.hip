@@ -382,27 +382,35 @@ static hipError_t clear(bool bf16, void* p, int64_t n, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------------------ products
-template <int EPI> static void launch_gated_epi(const GemmArgs& g, hipStream_t s) { launch_epi<EPI, OUT_BF16, false, true>(g, s); }
+template <int EPI> static hipError_t launch_gated_epi(const GemmArgs& g, hipStream_t s) {
+  switch (g.tile_cfg - 1) {
+    case 0: return launch_clamped<T0, EPI>(g, s);
+    case 2: return launch_clamped<T2, EPI>(g, s);
+    case 5: return launch_clamped<T5, EPI>(g, s);
+    case 7: return launch_clamped<T7, EPI>(g, s);
+    case 8: return launch_clamped<T8, EPI>(g, s);
+    default: return launch_clamped<T4, EPI>(g, s);
+  }
+}
 
 // operands that stand [K, rows]: the tiles of the ping-pong loop (both: those whose wave rows are whole blocks of 64)
-template <int EPI> static void launch_w_rows(const GemmArgs& g, hipStream_t s) {
-  if (g.tile_cfg == 3) launch_cfg<T2, EPI, OUT_BF16, false, true, 2>(g, s);
-  else if (g.tile_cfg == 6) launch_cfg<T5, EPI, OUT_BF16, false, true, 2>(g, s);
-  else launch_cfg<T0, EPI, OUT_BF16, false, true, 2>(g, s);
+template <int EPI> static hipError_t launch_w_rows(const GemmArgs& g, hipStream_t s) {
+  if (g.tile_cfg == 3) return launch_clamped<T2, EPI, 2>(g, s);
+  if (g.tile_cfg == 6) return launch_clamped<T5, EPI, 2>(g, s);
+  return launch_clamped<T0, EPI, 2>(g, s);
 }
 
-static void launch_both_rows(const GemmArgs& a, const GemmArgs* b, hipStream_t s) {
-  if (a.tile_cfg == 3) launch_pair<T2>(a, b, s);
-  else launch_pair<T0>(a, b, s);
+static hipError_t launch_both_rows(const GemmArgs& a, const GemmArgs* b, hipStream_t s) {
+  return a.tile_cfg == 3 ? launch_pair<T2>(a, b, s) : launch_pair<T0>(a, b, s);
 }
 
-static void launch_gated_whole(const GemmArgs& g, hipStream_t s) {
-  if (g.a_rows) launch_both_rows(g, nullptr, s);
-  else if (g.w_rows && g.epilogue == EPI_DGATED) launch_w_rows<EPI_DGATED>(g, s);
-  else if (g.w_rows) launch_w_rows<EPI_STORE>(g, s);
-  else if (g.epilogue == EPI_GATED) launch_gated_epi<EPI_GATED>(g, s);
-  else if (g.epilogue == EPI_DGATED) launch_gated_epi<EPI_DGATED>(g, s);
-  else launch_gated_epi<EPI_STORE>(g, s);
+static hipError_t launch_gated_whole(const GemmArgs& g, hipStream_t s) {
+  if (g.a_rows) return launch_both_rows(g, nullptr, s);
+  if (g.w_rows && g.epilogue == EPI_DGATED) return launch_w_rows<EPI_DGATED>(g, s);
+  if (g.w_rows) return launch_w_rows<EPI_STORE>(g, s);
+  if (g.epilogue == EPI_GATED) return launch_gated_epi<EPI_GATED>(g, s);
+  if (g.epilogue == EPI_DGATED) return launch_gated_epi<EPI_DGATED>(g, s);
+  return launch_gated_epi<EPI_STORE>(g, s);
 }
 
 // Time of a launch of these products in us: per round of blocks alpha * K / 1024 + beta[epilogue] (the last round, of a
@@ -470,10 +478,10 @@ static TilePlan plan_product(const GemmArgs& g, long cus) {
 
 static int tile_rows(int tile) { return tile == 5 ? 320 : tile == 4 ? 128 : tile >= 7 ? 64 : 256; }
 
-// EPI_STORE, EPI_GATED or EPI_DGATED with operands that are not read past their ends.  Returns the rows of g.sums that the
+// EPI_STORE, EPI_GATED or EPI_DGATED with operands that are not read past their ends.  filled: the rows of g.sums that the
 // launches fill (two per tile along M).
-int launch_gemm_bf16_gated(const GemmArgs& args, hipStream_t s) {
-  if (args.M <= 0 || args.N <= 0) return 0;
+hipError_t launch_gemm_bf16_gated(const GemmArgs& args, hipStream_t s, int* filled) {
+  if (args.M <= 0 || args.N <= 0) return hipSuccess;
   GemmArgs g = args;
   TilePlan plan = {0, 0, 0.0, 0};
   if (g.tile_cfg == 0) {
@@ -481,7 +489,10 @@ int launch_gemm_bf16_gated(const GemmArgs& args, hipStream_t s) {
     g.tile_cfg = plan.tile + 1;
   }
   auto sum_rows = [](const GemmArgs& x) { return (x.M + tile_rows(x.tile_cfg - 1) - 1) / tile_rows(x.tile_cfg - 1) * 2; };
-  if (plan.body_rows <= 0) { launch_gated_whole(g, s); return sum_rows(g); }
+  if (plan.body_rows <= 0) {
+    if (filled) *filled = sum_rows(g);
+    return launch_gated_whole(g, s);
+  }
   const size_t mb = plan.body_rows;
   GemmArgs body = g, tail = g;
   body.M = (int)mb;
@@ -496,9 +507,9 @@ int launch_gemm_bf16_gated(const GemmArgs& args, hipStream_t s) {
   }
   if (g.dgu) tail.dgu = (__bf16*)g.dgu + mb * g.lddgu;
   if (g.stats_in) tail.stats_in = g.stats_in + mb * g.stats_n;
-  launch_gated_whole(body, s);
-  launch_gated_whole(tail, s);
-  return sum_rows(body) + sum_rows(tail);
+  if (filled) *filled = sum_rows(body) + sum_rows(tail);
+  if (hipError_t e = launch_gated_whole(body, s)) return e;
+  return launch_gated_whole(tail, s);
 }
 
 // A product whose operands stand [K, rows] (g.a_rows, g.w_rows): as they stand, or turned into a_t and w_t (rows of round_up(K, 8))
@@ -538,14 +549,11 @@ static SplitPlan plan_split(const GemmArgs& g, long cus) {
 static hipError_t launch_parts(const GemmArgs& g, const SplitPlan& p, float* sums, hipStream_t s) {
   GemmArgs x = g;
   x.out = sums;
-  if (g.w_rows) {
-    if (p.tile == 2) launch_split<T2, 2>(x, p.parts, p.k_part, s);
-    else launch_split<T0, 2>(x, p.parts, p.k_part, s);
-  } else {
-    if (p.tile == 7) launch_split<T7, 0>(x, p.parts, p.k_part, s);
-    else if (p.tile == 2) launch_split<T2, 0>(x, p.parts, p.k_part, s);
-    else launch_split<T0, 0>(x, p.parts, p.k_part, s);
-  }
+  hipError_t e;
+  if (g.w_rows) e = p.tile == 2 ? launch_split<T2, 2>(x, p.parts, p.k_part, s) : launch_split<T0, 2>(x, p.parts, p.k_part, s);
+  else if (p.tile == 7) e = launch_split<T7, 0>(x, p.parts, p.k_part, s);
+  else e = p.tile == 2 ? launch_split<T2, 0>(x, p.parts, p.k_part, s) : launch_split<T0, 0>(x, p.parts, p.k_part, s);
+  if (e != hipSuccess) return e;
   JoinArgs j{sums, (const __bf16*)g.bias, (__bf16*)g.out, p.parts, g.M, g.N, g.ldo};
   void* args[] = {(void*)&j};
   return hipLaunchKernel((const void*)join_kernel, dim3((g.M * (g.N / 8) + 255) / 256), dim3(256), args, 0, s);
@@ -560,9 +568,7 @@ static hipError_t launch_product(const GemmArgs& g, void* a_t, void* w_t, float*
   }
   if (t.turn && g.a_rows) if (hipError_t e = transpose(g.A, g.lda, a_t, t.g.lda, g.K, g.M, s)) return e;
   if (t.turn && g.w_rows) if (hipError_t e = transpose(g.W, g.ldw, w_t, t.g.ldw, g.K, g.N, s)) return e;
-  const int rows = launch_gemm_bf16_gated(t.g, s);
-  if (sum_rows) *sum_rows = rows;
-  return hipSuccess;
+  return launch_gemm_bf16_gated(t.g, s, sum_rows);
 }
 
 // Two products of one K whose operands stand [K, rows], each wanted or not: in one launch, whose rounds they share, where that is
@@ -581,8 +587,7 @@ static hipError_t launch_products(const GemmArgs& a, bool want_a, const GemmArgs
   if (tile >= 0) {
     GemmArgs first = want_a ? a : b;
     first.tile_cfg = tile + 1;
-    launch_both_rows(first, want_a && want_b ? &b : nullptr, s);
-    return hipSuccess;
+    return launch_both_rows(first, want_a && want_b ? &b : nullptr, s);
   }
   if (want_a) if (hipError_t e = launch_product(a, a_t, w_t, nullptr, s)) return e;
   return want_b ? launch_product(b, a_t, w_t, nullptr, s) : hipSuccess;
@@ -682,18 +687,6 @@ epd_status check_call(const char* who, const epd_gated_mlp_cfg* c, const epd_gat
 
 int act_code(const epd_gated_mlp_cfg& c) { return c.act == EPD_SWIGLU ? 2 : c.act == EPD_GEGLU_TANH ? 1 : 0; }
 
-// Launches of the GEMM families report through the runtime's last error, which may hold one that the program left
-// there: only a new one counts, and the program's stays.
-struct LastError {
-  const hipError_t before = hipPeekAtLastError();
-  hipError_t now() const {
-    const hipError_t e = hipPeekAtLastError();
-    if (e == before) return hipSuccess;
-    (void)hipGetLastError();
-    return e;
-  }
-};
-
 }  // namespace
 
 extern "C" {
@@ -734,20 +727,17 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
   down.M = T; down.N = D; down.K = F; down.epilogue = EPI_STORE; down.out = y; down.ldo = (int)ld_y;
   hipError_t e;
   if (bf) {
-    const LastError last;
     if (few_up(T, D, F)) {
       const FewArgs a{x, up.W, up.bias, H, keep.p, keep.q, keep.low, up.lda, F, T, F, D, up.act};
       e = launch_few<true>(a, st);
     } else {
-      launch_gemm_bf16_gated(up, st);
-      e = last.now();
+      e = launch_gemm_bf16_gated(up, st, nullptr);
     }
     if (e == hipSuccess && few_down(T, F)) {
       const FewArgs a{H, down.W, down.bias, y, nullptr, nullptr, nullptr, F, down.ldo, T, D, F, 0};
       e = launch_few<false>(a, st);
     } else if (e == hipSuccess) {
       e = launch_product(down, nullptr, nullptr, (float*)((char*)workspace + L.parts), st);
-      if (e == hipSuccess) e = last.now();
     }
   } else {
     F32Group a{}, b{};
@@ -758,8 +748,7 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
     e = launch_gemm_f32_group(a, st);
     if (e == hipSuccess) e = launch_gemm_f32_group(b, st);
   }
-  if (e != hipSuccess) return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e));
-  return EPD_OK;
+  return e == hipSuccess ? EPD_OK : op_launch_failed(who, e);
 }
 
 epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weights* w, const void* x, int64_t ld_x, const void* dy, int64_t ld_dy,
@@ -777,7 +766,7 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
   hipStream_t st = (hipStream_t)stream;
   hipError_t e = hipSuccess;
   auto ok = [&](hipError_t r) { if (e == hipSuccess) e = r; return e == hipSuccess; };
-  auto failed = [&]() { return op_fail(EPD_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(e)); };
+  auto failed = [&]() { return op_launch_failed(who, e); };
   if (tokens == 0) {                     // sums over no token
     if (grads->gate_up_w) ok(clear(bf, grads->gate_up_w, 2 * F * D, st));
     if (grads->down_w && e == hipSuccess) ok(clear(bf, grads->down_w, D * F, st));
@@ -822,7 +811,6 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
     if ((b.n || b.sum[0].cols || b.sum[1].cols) && !ok(launch_gemm_f32_group(b, st))) return failed();
     return EPD_OK;
   }
-  const LastError last;
   SumPartsArgs sums{};
   if (want_h) {
     if (grads->gate_up_b) dh.sums = (float*)(ws + L.sums_gu);
@@ -844,8 +832,7 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
   }
   if (grads->dx && !ok(launch_product(dx, nullptr, ws + L.w_t, (float*)(ws + L.parts), st))) return failed();
   if (!ok(launch_products(dgu, grads->gate_up_w, dd, grads->down_w, ws + L.a_t, ws + L.w_t, st))) return failed();
-  ok(last.now());
-  return e == hipSuccess ? EPD_OK : failed();
+  return EPD_OK;
 }
 
 }  // extern "C"

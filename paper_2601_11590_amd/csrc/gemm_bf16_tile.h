@@ -1460,19 +1460,13 @@ template <class T> static int raster_group(const GemmArgs& g, int tiles_m, int t
   return std::min(group_m, tiles_m);
 }
 
-// CLAMPED: operands that may not be read past their ends take the ping-pong loop all the same, with clamps
-template <class T, int EPI, int OUT, bool GATHER, bool CLAMPED = false, int KROWS = 0>
+template <class T, int EPI, int OUT, bool GATHER>
 static void launch_cfg(const GemmArgs& g, hipStream_t s) {
   const int tiles_m = (g.M + T::BM - 1) / T::BM, tiles_n = (g.N + T::BN - 1) / T::BN;
   const long blocks = (long)T::MINBLK * (g.compute_units > 0 ? g.compute_units : num_cus());     // of one round
   GemmArgs a = g;
   a.rot_lds = EPI == EPI_QKV && (long)tiles_m * tiles_n <= ROT_TABLE_ROUNDS * blocks;
   a.group_m = raster_group<T>(g, tiles_m, tiles_n, blocks);
-  if constexpr (CLAMPED) {
-    static_assert(!GATHER, "clamped rows are dense");
-    hipLaunchKernelGGL((gemm_bf16_kernel<T, EPI, OUT, false, T::PINGPONG, 2, T::PINGPONG, KROWS>), dim3(tiles_m * tiles_n), dim3(T::NT), 0, s, a);
-    return;
-  } else {
   if constexpr (!GATHER) {
     if (g.overread_a && g.overread_w && g.K % T::BK == 0) {
       if (EPI == EPI_RESIDUAL && g.name_tag == 1)
@@ -1489,7 +1483,16 @@ static void launch_cfg(const GemmArgs& g, hipStream_t s) {
     }
   }
   hipLaunchKernelGGL((gemm_bf16_kernel<T, EPI, OUT, GATHER, false, 0>), dim3(tiles_m * tiles_n), dim3(T::NT), 0, s, a);
-  }
+}
+
+// Products of the gated MLP: operands that may not be read past their ends take the ping-pong loop all the same, with clamps.  These
+// launches return their own status: the runtime's last error may hold one of the program's.
+template <class T, int EPI, int KROWS = 0> static hipError_t launch_clamped(const GemmArgs& g, hipStream_t s) {
+  const int tiles_m = (g.M + T::BM - 1) / T::BM, tiles_n = (g.N + T::BN - 1) / T::BN;
+  GemmArgs a = g;
+  a.group_m = raster_group<T>(g, tiles_m, tiles_n, (long)T::MINBLK * (g.compute_units > 0 ? g.compute_units : num_cus()));
+  void* args[] = {(void*)&a};
+  return hipLaunchKernel((const void*)gemm_bf16_kernel<T, EPI, OUT_BF16, false, T::PINGPONG, 2, T::PINGPONG, KROWS>, dim3(tiles_m * tiles_n), dim3(T::NT), args, 0, s);
 }
 
 // 256 x 128 serves QKV where 2 * hidden is not a multiple of 256, and narrow outputs (plan_tiles).  Ping-pong loop: 1385
@@ -1633,7 +1636,7 @@ __global__ __launch_bounds__(T::NT, T::MINBLK) void gemm_bf16_pair_kernel(GemmPa
   gemm_tile<T, EPI_STORE, OUT_BF16, false, false, true, true, 3>(g, tm * T::BM, tn * T::BN, lds);
 }
 
-template <class T> static void launch_pair(const GemmArgs& a, const GemmArgs* b, hipStream_t s) {
+template <class T> static hipError_t launch_pair(const GemmArgs& a, const GemmArgs* b, hipStream_t s) {
   static_assert(T::PINGPONG, "reads transposed");
   const long blocks = (long)T::MINBLK * num_cus();
   auto tiles = [](int n, int b) { return (n + b - 1) / b; };
@@ -1647,7 +1650,8 @@ template <class T> static void launch_pair(const GemmArgs& a, const GemmArgs* b,
     p.group_m = raster_group<T>(*b, tiles(b->M, T::BM), tiles(b->N, T::BN), blocks);
     all += tiles(b->M, T::BM) * tiles(b->N, T::BN);
   }
-  hipLaunchKernelGGL(gemm_bf16_pair_kernel<T>, dim3(all), dim3(T::NT), 0, s, p);
+  void* args[] = {(void*)&p};
+  return hipLaunchKernel((const void*)gemm_bf16_pair_kernel<T>, dim3(all), dim3(T::NT), args, 0, s);
 }
 
 // A product whose K is cut into parts of k_part (a multiple of 64), each a block's own: fp32 sums [part][M][N] for a kernel that adds
@@ -1670,28 +1674,29 @@ __global__ __launch_bounds__(T::NT, T::MINBLK) void gemm_bf16_split_kernel(GemmS
 }
 
 // g.out: the sums, rows of N.
-template <class T, int KROWS> static void launch_split(const GemmArgs& g, int parts, int k_part, hipStream_t s) {
+template <class T, int KROWS> static hipError_t launch_split(const GemmArgs& g, int parts, int k_part, hipStream_t s) {
   const int tiles_m = (g.M + T::BM - 1) / T::BM, tiles_n = (g.N + T::BN - 1) / T::BN;
   GemmSplit p{g, k_part};
   p.g.ldo = g.N; p.g.bias = nullptr;
   GemmArgs of_part = g;
   of_part.K = k_part;
   p.g.group_m = raster_group<T>(of_part, tiles_m, tiles_n, (long)T::MINBLK * num_cus());
-  hipLaunchKernelGGL((gemm_bf16_split_kernel<T, KROWS>), dim3(tiles_m * tiles_n * parts), dim3(T::NT), 0, s, p);
+  void* args[] = {(void*)&p};
+  return hipLaunchKernel((const void*)gemm_bf16_split_kernel<T, KROWS>, dim3(tiles_m * tiles_n * parts), dim3(T::NT), args, 0, s);
 }
 
-template <int EPI, int OUT, bool GATHER, bool CLAMPED = false>
+template <int EPI, int OUT, bool GATHER>
 static void launch_epi(const GemmArgs& g, hipStream_t s) {
   int t = g.tile_cfg > 0 ? g.tile_cfg - 1 : -1;   // tile_cfg: set by the tuning hook of the C ABI, or by a split
   if (!gemm_bf16_tile_known(t)) t = plan_tiles(g.M, g.N, g.K, g.epilogue, false, g.compute_units > 0 ? g.compute_units : num_cus()).tile;
   if (EPI == EPI_QKV && (t == 0 || t == 5) && g.qk_cols % 256 != 0) t = 2;
   switch (t) {
-    case 0: launch_cfg<T0, EPI, OUT, GATHER, CLAMPED>(g, s); break;
-    case 2: launch_cfg<T2, EPI, OUT, GATHER, CLAMPED>(g, s); break;
-    case 5: launch_cfg<T5, EPI, OUT, GATHER, CLAMPED>(g, s); break;
-    case 7: launch_cfg<T7, EPI, OUT, GATHER, CLAMPED>(g, s); break;
-    case 8: launch_cfg<T8, EPI, OUT, GATHER, CLAMPED>(g, s); break;
-    default: launch_cfg<T4, EPI, OUT, GATHER, CLAMPED>(g, s); break;
+    case 0: launch_cfg<T0, EPI, OUT, GATHER>(g, s); break;
+    case 2: launch_cfg<T2, EPI, OUT, GATHER>(g, s); break;
+    case 5: launch_cfg<T5, EPI, OUT, GATHER>(g, s); break;
+    case 7: launch_cfg<T7, EPI, OUT, GATHER>(g, s); break;
+    case 8: launch_cfg<T8, EPI, OUT, GATHER>(g, s); break;
+    default: launch_cfg<T4, EPI, OUT, GATHER>(g, s); break;
   }
 }
 

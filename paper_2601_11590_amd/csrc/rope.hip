@@ -300,7 +300,7 @@ epd_status epd_rope_apply(const epd_rope_cfg* c, const epd_rope_tensor* tensors,
       part.t[i].out = (char*)a.t[i].out + tok0 * a.t[i].out_token * (int64_t)es;
     }
     if (hipError_t e = launch_rope(part, bf, vec, adjacent, dim3(n, shares), (hipStream_t)stream))
-      return op_fail(EPD_ERR_HIP, "epd_rope_apply: kernel launch failed: %s", hipGetErrorString(e));
+      return op_launch_failed("epd_rope_apply", e);
   }
   return EPD_OK;
 }
@@ -350,7 +350,7 @@ epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, 
         const int64_t ahead = text ? t : std::max((int64_t)t_step * (t - 1) + 1, std::max(h, w));
         if (pass && count) {
           if (a.n == kPosSpans)
-            if (hipError_t e = flush()) return op_fail(EPD_ERR_HIP, "epd_rope_positions: kernel launch failed: %s", hipGetErrorString(e));
+            if (hipError_t e = flush()) return op_launch_failed("epd_rope_positions", e);
           a.span[a.n++] = PosSpan{(int32_t)(tok - sent), (int32_t)pos, (int32_t)h, (int32_t)w};
         }
         tok += count;
@@ -363,7 +363,7 @@ epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, 
     if (!pass) {
       if (position_stride < tok) return op_fail(EPD_ERR_SHAPE, "epd_rope_positions: position_stride %lld < %lld tokens", (long long)position_stride, (long long)tok);
     } else if (hipError_t e = flush()) {
-      return op_fail(EPD_ERR_HIP, "epd_rope_positions: kernel launch failed: %s", hipGetErrorString(e));
+      return op_launch_failed("epd_rope_positions", e);
     }
   }
   return EPD_OK;

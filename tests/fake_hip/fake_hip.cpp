@@ -113,6 +113,7 @@ int hipStreamSynchronize(void*) {
 }
 int hipStreamIsCapturing(void*, int* status) { CALL(); *status = (int)g_set[kCapture]; return 0; }
 int hipGetLastError() { CALL(); const int e = (int)g_set[kLastError]; g_set[kLastError] = 0; return e; }
+int hipPeekAtLastError() { CALL(); return (int)g_set[kLastError]; }
 const char* hipGetErrorString(int e) { static char b[32]; std::snprintf(b, sizeof b, "fake error %d", e); return b; }
 int hipHostMalloc(void** p, size_t n, unsigned flags) { CALL(); g_set[kHostFlags] = flags; *p = std::calloc(n, 1); return 0; }
 int hipHostFree(void* p) { CALL(); std::free(p); return 0; }
