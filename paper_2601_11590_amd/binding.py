@@ -771,7 +771,7 @@ class GatedMLP:
         ld, one = t.stride()
         if one != 1 and t.numel() and self.hidden > 1:
             raise ValueError("the rows of %s must be contiguous" % name)
-        return t.data_ptr(), max(ld, self.hidden) if shape[0] < 2 else ld      # one row: its stride means nothing
+        return t.data_ptr(), self.hidden if shape[0] < 2 else ld      # one row: its stride means nothing
 
     def _call(self, call, *args) -> None:
         def on(*a):

@@ -665,7 +665,9 @@ epd_status check_cfg(const char* who, const epd_gated_mlp_cfg* c) {
   return EPD_OK;
 }
 
-epd_status check_rows(const char* who, const char* name, const epd_gated_mlp_cfg& c, const void* p, int64_t ld) {
+// Rows of X, Y or a gradient; what the row of a single token would be apart from the next is not looked at.
+epd_status check_rows(const char* who, const char* name, const epd_gated_mlp_cfg& c, const void* p, int64_t& ld, int tokens) {
+  if (tokens == 1) ld = c.hidden;
   if (!p) return op_fail(EPD_ERR_INVALID_ARG, "%s: %s is NULL", who, name);
   if (ld < c.hidden || ld >= kMaxTokens) return op_fail(EPD_ERR_SHAPE, "%s: rows of %s are %lld apart: hidden %d .. 2^22 - 1", who, name, (long long)ld, c.hidden);
   if (c.dtype == EPD_BF16 ? ((uintptr_t)p % 16 || ld % 8) : (uintptr_t)p % 4)
@@ -708,8 +710,8 @@ epd_status epd_gated_mlp(const epd_gated_mlp_cfg* cfg, const epd_gated_mlp_weigh
   if (epd_status s = check_call(who, cfg, w, tokens, workspace, workspace_bytes)) return s;
   if (tokens == 0) return EPD_OK;
   const epd_gated_mlp_cfg& c = *cfg;
-  if (epd_status s = check_rows(who, "x", c, x, ld_x)) return s;
-  if (epd_status s = check_rows(who, "y", c, y, ld_y)) return s;
+  if (epd_status s = check_rows(who, "x", c, x, ld_x, tokens)) return s;
+  if (epd_status s = check_rows(who, "y", c, y, ld_y, tokens)) return s;
   if ((uintptr_t)saved % (c.dtype == EPD_BF16 ? 16 : 4)) return op_fail(EPD_ERR_UNSUPPORTED, "%s: saved must be aligned to 16 bytes (bf16) or 4 (fp32)", who);
   const GatedLayout L = gated_layout(c);
   const bool bf = c.dtype == EPD_BF16;
@@ -774,10 +776,11 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
     if (grads->down_b && e == hipSuccess) ok(clear(bf, grads->down_b, D, st));
     return e == hipSuccess ? EPD_OK : failed();
   }
-  if (epd_status s = check_rows(who, "x", c, x, ld_x)) return s;
-  if (epd_status s = check_rows(who, "dy", c, dy, ld_dy)) return s;
+  if (epd_status s = check_rows(who, "x", c, x, ld_x, tokens)) return s;
+  if (epd_status s = check_rows(who, "dy", c, dy, ld_dy, tokens)) return s;
   if (!saved) return op_fail(EPD_ERR_INVALID_ARG, "%s: saved is NULL", who);
-  if (grads->dx) if (epd_status s = check_rows(who, "dx", c, grads->dx, grads->ld_dx)) return s;
+  int64_t ld_dx = grads->ld_dx;
+  if (grads->dx) if (epd_status s = check_rows(who, "dx", c, grads->dx, ld_dx, tokens)) return s;
   const GatedLayout L = gated_layout(c);
   char* const ws = (char*)workspace;
   const int T = tokens, iD = c.hidden, iF = c.mlp_dim;
@@ -790,7 +793,7 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
   if (bf) { dh.keep_p = keep.p; dh.keep_q = keep.q; dh.keep_low = keep.low; }
   else { dh.gu = (void*)saved; dh.ldgu = 2 * iF; dh.out = ws + L.h; dh.ldo = iF; }
   // dX = (dG | dU) Wgu,  dWgu = (dG | dU)^T X,  dWd = dY^T H
-  dx.A = ws + L.dgu; dx.lda = 2 * iF; dx.M = T; dx.N = iD; dx.K = 2 * iF; dx.epilogue = EPI_STORE; dx.out = grads->dx; dx.ldo = (int)grads->ld_dx;
+  dx.A = ws + L.dgu; dx.lda = 2 * iF; dx.M = T; dx.N = iD; dx.K = 2 * iF; dx.epilogue = EPI_STORE; dx.out = grads->dx; dx.ldo = (int)ld_dx;
   dgu.M = 2 * iF; dgu.N = iD; dgu.epilogue = EPI_STORE; dgu.out = grads->gate_up_w; dgu.ldo = iD;
   dd.M = iD; dd.N = iF; dd.epilogue = EPI_STORE; dd.out = grads->down_w; dd.ldo = iF;
   dh.W = w->down_w; dh.ldw = iF; dh.w_rows = 1;
