@@ -293,7 +293,8 @@ typedef struct {
   const void* in;       /* device; element e of head h of token t at in[t * in_token + h * in_head + e] */
   void* out;            /* device; the same with out_*.  May be `in` (then with the same strides)   */
   int64_t in_token, in_head, out_token, out_head; /* strides in elements, 0 .. 2^40; rows of `out` are
-                           apart, `in` may repeat rows (stride 0)                                   */
+                           apart, `in` may repeat rows (stride 0); those of a single token or head
+                           are not looked at                                                        */
   int32_t heads;        /* 0 .. 256                                                                 */
 } epd_rope_tensor;
 

@@ -653,7 +653,7 @@ def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str 
         dev = torch.device(dev.type, torch.cuda.current_device())
     if out is None:
         out = torch.empty((3, tokens), dtype=torch.int32, device=dev)
-    if not out.is_cuda or out.dtype != torch.int32 or out.dim() != 2 or out.shape[0] != 3 or out.shape[1] < tokens or (out.shape[1] and out.stride(1) != 1):
+    if not out.is_cuda or out.dtype != torch.int32 or out.dim() != 2 or out.shape[0] != 3 or out.shape[1] < tokens or (out.shape[1] > 1 and out.stride(1) != 1):
         raise ValueError("out must be a device int32 [3, >= tokens] whose rows are contiguous")
     return out, _on(dev.index, _positions, span, cu, start, t_step, out.data_ptr() or 256, out.stride(0))      # no tokens: nothing is written
 

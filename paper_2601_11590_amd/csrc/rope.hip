@@ -248,12 +248,16 @@ epd_status epd_rope_apply(const epd_rope_cfg* c, const epd_rope_tensor* tensors,
   auto fits = [&](int64_t v) { while (vec > 1 && v % vec) vec /= 2; };
   fits(c->head_dim);
   fits(adjacent ? 2 * pairs : pairs);
+  epd_rope_tensor of[kRopeTensors];
   for (int i = 0; i < num_tensors; ++i) {
-    const epd_rope_tensor& x = tensors[i];
+    epd_rope_tensor& x = of[i];
+    x = tensors[i];
     if (x.heads < 0 || x.heads > kRopeHeads) return op_fail(EPD_ERR_UNSUPPORTED, "epd_rope_apply: tensor %d has %d heads: 0 .. %d", i, x.heads, kRopeHeads);
     if (x.heads == 0 || tokens == 0) continue;
     if (!x.in || !x.out) return op_fail(EPD_ERR_INVALID_ARG, "epd_rope_apply: tensor %d: a required pointer is NULL", i);
     if (((uintptr_t)x.in | (uintptr_t)x.out) % es) return op_fail(EPD_ERR_INVALID_ARG, "epd_rope_apply: tensor %d is not aligned to its elements", i);
+    if (tokens == 1) x.in_token = x.out_token = 0;         // there is no next row
+    if (x.heads == 1) x.in_head = x.out_head = 0;
     constexpr int64_t kMaxStride = 1ll << 40;
     for (int64_t v : {x.in_token, x.in_head, x.out_token, x.out_head})
       if (v < 0 || v > kMaxStride) return op_fail(EPD_ERR_SHAPE, "epd_rope_apply: tensor %d has a stride of %lld", i, (long long)v);
@@ -273,7 +277,7 @@ epd_status epd_rope_apply(const epd_rope_cfg* c, const epd_rope_tensor* tensors,
   a.inv_pairs = inv(pairs);
   int most = 1;
   for (int i = 0; i < num_tensors; ++i) {
-    const epd_rope_tensor& x = tensors[i];
+    const epd_rope_tensor& x = of[i];
     if (!x.heads) continue;
     RopeTensor& d = a.t[a.n++];
     d.in = x.in; d.out = x.out; d.heads = x.heads;
