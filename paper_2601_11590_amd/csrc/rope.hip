@@ -337,7 +337,7 @@ epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, 
       if (a.n && tok > sent) {
         a.out = positions + sent; a.tokens = (int)(tok - sent);
         void* args[] = {(void*)&a};
-        e = hipLaunchKernel((const void*)rope_positions_kernel, dim3((a.tokens + 255) / 256), dim3(256), args, 0, (hipStream_t)stream);
+        e = hipLaunchKernel((const void*)rope_positions_kernel, dim3((a.tokens - 1) / 256 + 1), dim3(256), args, 0, (hipStream_t)stream);
       }
       a.n = 0; sent = tok;
       return e;

@@ -74,6 +74,19 @@ def a_failed_launch_is_reported(fake, lib):
     fake.fake_set(LAST_ERROR, 0)
 
 
+def sequences_of_2_31_tokens(fake, lib):
+    """Positions of as many tokens as the entry takes: a thread each."""
+    most = 2 ** 31 - 1
+    for tokens in (most, most - 1, most - 254, most - 255, most - 256):
+        fake.fake_forget()
+        assert positions(lib, [(tokens - 10, 0, 0), (10, 0, 0)], [0, 1, 2]) == OK
+        ((_, grid, block),) = launches(fake)
+        assert (grid, block) == ((-(-tokens // 256), 1, 1), (256, 1, 1)), (tokens, grid)
+    fake.fake_forget()
+    assert rotate(lib, most) == OK
+    assert all(g * b < 2 ** 32 for l in launches(fake) for g, b in zip(l[1], l[2]))
+
+
 if __name__ == "__main__":
     loaded = load(sys.argv[1], sys.argv[2])
     globals()[sys.argv[3]](*loaded, *(json.loads(a) for a in sys.argv[4:]))

@@ -28,3 +28,7 @@ def run(tmp_path_factory):
 
 def test_a_failed_launch_is_reported(run):
     run("a_failed_launch_is_reported")
+
+
+def test_sequences_of_2_31_tokens(run):
+    run("sequences_of_2_31_tokens")
