@@ -160,7 +160,7 @@ struct F32Group {
   GemmArgs g[3];
   F32Sum sum[2];
   int n, first[4];      // products; first is set by the launcher
-  long t16;             // 16 x 16 tiles, operations and longest K of the products that the tile is chosen by (count_f32): a call's
+  long t16, t32;        // 16 x 16 and 32 x 32 tiles, operations and longest K of the products that the tile is chosen by (count_f32): a call's
   double flops;         //   products whether wanted or not, so that a gradient has the same bits in every call
   int k, products;
 };

@@ -458,6 +458,7 @@ static hipError_t launch_lds_group_f32(F32Group& a, hipStream_t s) {
 
 void count_f32(F32Group& a, int M, int N, int K) {
   a.t16 += (long)((M + 15) / 16) * ((N + 15) / 16);
+  a.t32 += (long)((M + 31) / 32) * ((N + 31) / 32);
   a.k = std::max(a.k, K);
   a.flops += 2.0 * M * N * K;
   ++a.products;
@@ -468,8 +469,9 @@ void count_f32(F32Group& a, int M, int N, int K) {
 // through LDS; 64 x 256, 8192 tokens 118, but 258.  One long product alone pays sooner, its chains share the units with nothing: down of 1000 x
 // 512 x 2048 71 -> 50.  Below that, K over eight waves: 16 x 16 tiles while they are few, or while one of the
 // products is a few tiles of a long K (the backward pass of 257 tokens, 256 x 1024: 23 us; 27 in 32 x 32 tiles, 34 with K over four waves),
-// else 32 x 32.
+// else 32 x 32.  A launch has fewer than 2^32 threads: 512 for each 32 x 32 tile, and for 16 columns of a sum (2 F + D of them, below 2^19).
 hipError_t launch_gemm_f32_group(F32Group& a, hipStream_t s) {
+  if (a.t32 >= (1l << 23) - (1l << 15)) return launch_lds_group_f32(a, s);
   if (a.flops >= (a.products == 1 && a.k >= 1024 ? 1e6 : 1.4e6) * a.k) return launch_lds_group_f32(a, s);
   if (a.t16 <= 1024 || (a.k >= 1024 && a.t16 <= 3500)) return launch_group_f32<1, 8>(a, s);
   return launch_group_f32<2, 8>(a, s);

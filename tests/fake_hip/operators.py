@@ -87,6 +87,26 @@ def sequences_of_2_31_tokens(fake, lib):
     assert all(g * b < 2 ** 32 for l in launches(fake) for g, b in zip(l[1], l[2]))
 
 
+def launches_stay_within_the_thread_limit(fake, lib):
+    """Every call that the entries take is launched, in fewer than 2^32 threads along each axis of a grid."""
+    most, threads = {"bf16": 1 << 36, "f32": 1 << 33}, 0
+    for dtype in most:
+        for D in (8, 64, 2040, 2047, 2048, 8184, 65536):
+            for F in (8, 16, 64, 128, 2048, 8192, 131072):
+                if D * F >= 1 << 30 or (dtype == "bf16" and (D % 8 or F % 8)):
+                    continue
+                T = min((1 << 22) - 1, (most[dtype] - 1) // max(D, F))
+                c = mlp_cfg(dtype, T, D, F)
+                assert lib.epd_gated_mlp_workspace_bytes(C.byref(c)) > 0, (dtype, T, D, F)
+                for call in (forward, backward):
+                    fake.fake_forget()
+                    assert call(lib, c, T) == OK, (call, dtype, T, D, F)
+                    for name, grid, block in launches(fake):
+                        assert all(0 < g * b < 2 ** 32 for g, b in zip(grid, block)) and grid[1] < 65536, (dtype, T, D, F, name, grid, block)
+                        threads = max(threads, grid[0] * block[0])
+    assert threads > 1 << 30
+
+
 if __name__ == "__main__":
     loaded = load(sys.argv[1], sys.argv[2])
     globals()[sys.argv[3]](*loaded, *(json.loads(a) for a in sys.argv[4:]))

@@ -32,3 +32,7 @@ def test_a_failed_launch_is_reported(run):
 
 def test_sequences_of_2_31_tokens(run):
     run("sequences_of_2_31_tokens")
+
+
+def test_launches_stay_within_the_thread_limit(run):
+    run("launches_stay_within_the_thread_limit")
