@@ -97,7 +97,8 @@ typedef struct {
   int32_t in_channels, patch, temporal_patch;
   int32_t norm;         /* epd_norm                                                            */
   float norm_eps;
-  int32_t act;          /* epd_act                                                             */
+  int32_t act;          /* epd_act; gated: hidden * mlp_dim < 2^30, mlp_dim <= 131072 and
+                           max_tokens * mlp_dim < 2^36 (fp32: 2^33), EPD_ERR_UNSUPPORTED beyond */
   int32_t use_bias;     /* 1: every linear has a bias vector                                   */
   int32_t rope;         /* epd_rope                                                            */
   float rope_base;
@@ -333,11 +334,11 @@ epd_status epd_rope_positions(const int32_t* span_thw, const int32_t* cu_spans, 
 typedef struct {
   uint32_t struct_size; /* sizeof(epd_gated_mlp_cfg)                                                */
   int32_t dtype;        /* epd_dtype of X, Y, weights, gradients                                    */
-  int32_t hidden;       /* D; bf16: a multiple of 8                                                 */
-  int32_t mlp_dim;      /* F; bf16: a multiple of 8; D * F < 2^30                                   */
+  int32_t hidden;       /* D <= 65536; bf16: a multiple of 8                                        */
+  int32_t mlp_dim;      /* F <= 131072; bf16: a multiple of 8; D * F < 2^30                         */
   int32_t act;          /* EPD_SWIGLU, EPD_GEGLU_ERF or EPD_GEGLU_TANH                              */
   int32_t use_bias;     /* 1: both linears have a bias                                              */
-  int32_t max_tokens;   /* largest `tokens` of any call; < 2^22                                     */
+  int32_t max_tokens;   /* largest `tokens` of any call; < 2^22; times D and F < 2^36 (fp32: 2^33)  */
   int32_t training;     /* 1: the workspace also serves epd_gated_mlp_backward                      */
 } epd_gated_mlp_cfg;
 typedef struct {        /* device, dense; bf16: 16-byte aligned                                     */

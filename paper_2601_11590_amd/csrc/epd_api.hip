@@ -198,6 +198,15 @@ epd_status validate_cfg(const epd_encode_cfg* c, bool need_buffers, std::string&
     err = "head_dim * (max_tokens + 128 * max_segments) too large (bf16: must stay below 2^31)";
     return EPD_ERR_UNSUPPORTED;
   }
+  // the tiles of a gated product reach the up rows of W from its gate rows by 32-bit byte offsets, and a launch has fewer than 2^32 threads
+  if (gated(*c)) {
+    const int64_t D = c->hidden, F = c->mlp_dim;
+    if (D * F >= 1ll << 30 || F > kGatedMlpDim) {
+      err = fmt("gated: hidden %d * mlp_dim %d too large (below 2^30, mlp_dim at most %d)", c->hidden, c->mlp_dim, kGatedMlpDim);
+      return EPD_ERR_UNSUPPORTED;
+    }
+    if (c->max_tokens * F >= kGatedElements[c->dtype]) { err = "gated: max_tokens * mlp_dim too large (below 2^36, fp32 2^33)"; return EPD_ERR_UNSUPPORTED; }
+  }
   if (!need_buffers) return EPD_OK;
   const epd_weights* w = c->weights;
   if (!w) { err = "cfg.weights is NULL"; return EPD_ERR_INVALID_ARG; }

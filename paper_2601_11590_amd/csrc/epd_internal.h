@@ -154,6 +154,10 @@ void launch_plan(PlanArgs& p, hipStream_t s);
 void launch_norm(const float* x, const void* gamma, const void* beta, void* out, int T, int D,
                  float eps, bool rms, bool bf16, hipStream_t s);
 void launch_gemm_f32(const GemmArgs& g, hipStream_t s);
+// sizes of a gated MLP: mlp_dim, and tokens * mlp_dim or hidden by epd_dtype (a launch has fewer than 2^32 threads: fp32 tiles of 64 x 64, bf16
+// of 128 x 128 and 256 threads)
+constexpr int kGatedMlpDim = 131072;
+constexpr int64_t kGatedElements[2] = {1ll << 33, 1ll << 36};
 // fp32 products of the gated MLP (EPI_STORE without bias or with, EPI_GATED, EPI_DGATED) and column sums, in one launch
 struct F32Sum { const float* in; float* out; int rows, cols, ld; };      // cols = 0: none
 struct F32Group {

@@ -657,10 +657,9 @@ epd_status check_cfg(const char* who, const epd_gated_mlp_cfg* c) {
   if (c->act != EPD_SWIGLU && c->act != EPD_GEGLU_ERF && c->act != EPD_GEGLU_TANH) return op_fail(EPD_ERR_INVALID_ARG, "%s: act %d is not a gated activation", who, c->act);
   if (c->hidden <= 0 || c->mlp_dim <= 0 || c->max_tokens <= 0) return op_fail(EPD_ERR_INVALID_ARG, "%s: a size is not positive", who);
   if (c->dtype == EPD_BF16 && (c->hidden % 8 || c->mlp_dim % 8)) return op_fail(EPD_ERR_UNSUPPORTED, "%s: bf16: hidden and mlp_dim must be multiples of 8", who);
-  if (c->hidden > 65536 || c->mlp_dim > 131072 || (int64_t)c->hidden * c->mlp_dim >= (1ll << 30))
-    return op_fail(EPD_ERR_UNSUPPORTED, "%s: hidden %d, mlp_dim %d: at most 65536, 131072 and 2^30 together", who, c->hidden, c->mlp_dim);
-  // (a launch has fewer than 2^32 threads: tiles of 128 x 128 and 256 threads, fp32 64 x 64)
-  if (c->max_tokens >= kMaxTokens || (int64_t)c->max_tokens * std::max(c->mlp_dim, c->hidden) >= (c->dtype == EPD_BF16 ? 1ll << 36 : 1ll << 33))
+  if (c->hidden > 65536 || c->mlp_dim > kGatedMlpDim || (int64_t)c->hidden * c->mlp_dim >= (1ll << 30))
+    return op_fail(EPD_ERR_UNSUPPORTED, "%s: hidden %d, mlp_dim %d: at most 65536, %d and 2^30 together", who, c->hidden, c->mlp_dim, kGatedMlpDim);
+  if (c->max_tokens >= kMaxTokens || (int64_t)c->max_tokens * std::max(c->mlp_dim, c->hidden) >= kGatedElements[c->dtype])
     return op_fail(EPD_ERR_UNSUPPORTED, "%s: max_tokens %d too large", who, c->max_tokens);
   return EPD_OK;
 }

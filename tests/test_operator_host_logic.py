@@ -36,3 +36,21 @@ def test_sequences_of_2_31_tokens(run):
 
 def test_launches_stay_within_the_thread_limit(run):
     run("launches_stay_within_the_thread_limit")
+
+
+def test_gated_encoders_have_the_limits_of_the_operator():
+    from paper_2601_11590_amd import binding as B, workloads as W
+
+    def size(act, hidden, mlp_dim, max_tokens=64, dtype="bf16"):
+        cfg = W.EncoderConfig(name="t", dtype=dtype, num_layers=1, hidden=hidden, num_heads=hidden // 64, head_dim=64, mlp_dim=mlp_dim, patch=4,
+                              temporal_patch=1, norm="layernorm", rope="2d", rope_pairs=(0, 16, 16), out_dim=64)
+        return B.epd_encode_workspace_bytes(B.make_cfg(cfg.replace(act=act), max_tokens, 4, 4))
+
+    for act in W.GATED_ACTS:
+        # below 2^30 weights a half, as the operator: with 2^31 the up rows would lie 2^32 bytes from the gate rows, past the tiles' offsets
+        assert size(act, 8192, 131064) > 0 and size(act, 8192, 131072) == 0 and size(act, 8192, 262144) == 0
+        assert size(act, 64, 131072) > 0 and size(act, 64, 131080) == 0
+        assert size(act, 64, 64, (1 << 24) - 1) > 0
+        # 2^33 gates in fp32: a launch of 64 x 64 tiles has a thread for 16 of both halves
+        assert size(act, 64, 1024, (1 << 23) - 1, "f32") > 0 and size(act, 64, 1024, 1 << 23, "f32") == 0
+    assert size("gelu_erf", 8192, 262144) > 0 and size("gelu_erf", 64, 1024, 1 << 23, "f32") > 0      # as before
