@@ -590,7 +590,7 @@ def epd_rope_apply(cfg: epd_rope_cfg, tensors, positions: int, position_stride: 
 
 def epd_rope_tokens(span_thw: np.ndarray) -> int:
     """Tokens of all spans."""
-    span = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
+    span = _int32(span_thw, "span_thw").reshape(-1, 3)
     tokens = lib.epd_rope_tokens(_address(span), len(span))
     if tokens < 0:
         raise EpdError(EPD_ERR_SHAPE, epd_op_last_error())
@@ -605,8 +605,10 @@ def epd_rope_positions(span_thw: np.ndarray, cu_spans: np.ndarray, start: Option
 
 def _positions(span: np.ndarray, cu: np.ndarray, start, t_step: int, positions: int, position_stride: int, stream: int) -> np.ndarray:
     n = len(cu) - 1
+    if not -1 << 31 <= t_step < 1 << 31:
+        raise ValueError("t_step must be an int32")
     if start is not None:
-        start = np.ascontiguousarray(start, dtype=np.int32)
+        start = _int32(start, "start")
         if start.shape != (n,):
             raise ValueError("start must be [num_sequences]")
     after = np.empty(n, dtype=np.int32)
@@ -619,11 +621,22 @@ def _address(a: np.ndarray) -> int:
     return a.__array_interface__["data"][0]       # (a.ctypes.data makes an object for it)
 
 
+def _int32(a, name: str) -> np.ndarray:
+    """``a`` as a contiguous int32 array: itself where it is one, else its values, which have to be such."""
+    if type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous:
+        return a
+    a = np.asarray(a)
+    if a.size and a.dtype != np.int32:
+        lo, hi = a.min(), a.max()
+        if not (lo >= -2 ** 31 and hi < 2 ** 31) or (a.dtype.kind not in "iu" and not (a == np.trunc(a)).all()):
+            raise ValueError("%s must hold 32-bit integers" % name)
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
 def _spans(span_thw, cu_spans):
-    if type(span_thw) is not np.ndarray or span_thw.dtype != np.int32 or span_thw.ndim != 2 or span_thw.shape[1] != 3 or not span_thw.flags.c_contiguous:
-        span_thw = np.ascontiguousarray(span_thw, dtype=np.int32).reshape(-1, 3)
-    if type(cu_spans) is not np.ndarray or cu_spans.dtype != np.int32 or not cu_spans.flags.c_contiguous:
-        cu_spans = np.ascontiguousarray(cu_spans, dtype=np.int32)
+    span_thw, cu_spans = _int32(span_thw, "span_thw"), _int32(cu_spans, "cu_spans")
+    if span_thw.ndim != 2 or span_thw.shape[1] != 3:
+        span_thw = span_thw.reshape(-1, 3)
     if cu_spans.ndim != 1 or len(cu_spans) < 1 or int(cu_spans[-1]) > len(span_thw):      # the library refuses cu_spans that decrease
         raise ValueError("cu_spans must be [num_sequences + 1] and end within the spans")
     return span_thw, cu_spans
@@ -685,6 +698,8 @@ class Rope:
         if dev < 0 or positions.dtype != torch.int32 or len(axes) != 2 or axes[0] != self.axes or (axes[1] > 1 and positions.stride(1) != 1):
             raise ValueError("positions must be a device int32 [%d, tokens] whose rows are contiguous" % self.axes)
         T, d = axes[1], self.head_dim
+        if T >= 1 << 31:
+            raise ValueError("at most 2^31 - 1 tokens")
 
         def strides(v, shape):
             if v.get_device() != dev or v.dtype != self.dtype or v.shape != shape or len(shape) != 3 or shape[0] != T or shape[2] != d:
@@ -705,7 +720,7 @@ class Rope:
             else:
                 y, so = out[i], strides(out[i], shape)
             made.append(y)
-            arr[i] = (x.data_ptr(), y.data_ptr(), *si, *so, shape[1])
+            arr[i] = (x.data_ptr(), y.data_ptr(), *si, *so, min(shape[1], 1 << 30))      # (the library takes 256 heads at most)
         _on(dev, epd_rope_apply, self.cfg, arr, positions.data_ptr() or 256, positions.stride(0), T, inverse)
         return made
 
@@ -771,6 +786,8 @@ class GatedMLP:
         ld, one = t.stride()
         if one != 1 and t.numel() and self.hidden > 1:
             raise ValueError("the rows of %s must be contiguous" % name)
+        if shape[0] > self.cfg.max_tokens:
+            raise EpdError(EPD_ERR_SHAPE, "%s has %d rows: 0 .. max_tokens %d" % (name, shape[0], self.cfg.max_tokens))
         return t.data_ptr(), self.hidden if shape[0] < 2 else ld      # one row: its stride means nothing
 
     def _call(self, call, *args) -> None:
