@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <iterator>
 #include <map>
 #include <string>
 #include <vector>
@@ -77,6 +78,10 @@ const char* fake_launch(int i, uint32_t* sizes) {
   std::memcpy(sizes, v, sizeof v);
   return l.name.c_str();
 }
+
+// kernels of the loaded libraries
+int fake_kernels() { return (int)g_names.size(); }
+const char* fake_kernel(int i) { auto it = g_names.begin(); std::advance(it, i); return it->second.c_str(); }
 
 #define CALL() (++g_calls[__func__])
 

@@ -3,6 +3,8 @@ file> [<JSON>]."""
 
 import ctypes as C
 import json
+import random
+import re
 import sys
 
 from driver import ERR_HIP, LAST_ERROR, LAUNCH_STATUS, OK, binding, launches, load
@@ -34,10 +36,10 @@ def backward(lib, cfg, T, want=("dx", "gate_up_w", "gate_up_b", "down_w", "down_
     return lib.epd_gated_mlp_backward(C.byref(cfg), C.byref(mlp_weights()), X, cfg.hidden, DY, cfg.hidden, T, SAVED, C.byref(g), WORKSPACE, 1 << 60, None)
 
 
-def rotate(lib, T):
+def rotate(lib, T, dtype="bf16", pairing="half", heads=(4,), d=64, pairs=(8, 12, 12)):
     B = binding()
-    arr = (B.epd_rope_tensor * 1)((X, Y, 256, 64, 256, 64, 4))
-    return lib.epd_rope_apply(C.byref(B.Rope("bf16", 64, (8, 12, 12)).cfg), arr, 1, 0x1000, T, T, 0, None)
+    arr = (B.epd_rope_tensor * len(heads))(*((X + (i << 36), Y + (i << 36), h * d, d, h * d, d, h) for i, h in enumerate(heads)))
+    return lib.epd_rope_apply(C.byref(B.Rope(dtype, d, pairs, pairing=pairing).cfg), arr, len(heads), 0x1000, T, T, 0, None)
 
 
 def positions(lib, spans, cu):
@@ -105,6 +107,98 @@ def launches_stay_within_the_thread_limit(fake, lib):
                         assert all(0 < g * b < 2 ** 32 for g, b in zip(grid, block)) and grid[1] < 65536, (dtype, T, D, F, name, grid, block)
                         threads = max(threads, grid[0] * block[0])
     assert threads > 1 << 30
+
+
+# ------------------------------------------------------------------ what the sizes of the GPU tests reach
+
+def kernels(fake):
+    """The library's kernels that only the operators launch."""
+    fake.fake_kernel.restype = C.c_char_p
+    names = [fake.fake_kernel(i).decode() for i in range(fake.fake_kernels())]
+    own = ["gemm_bf16_pair", "gemm_bf16_split", "few_tokens", "one_token", "transpose_bf16", "part_sums", "sum_parts", "join_kernel", "gemm_f32_group",
+           "gemm_f32_lds_group", "rope_kernel", "rope_positions"]
+    return {n for n in names if any(o in n for o in own) or tag(n) == 2}
+
+
+GEMM = r"gemm_bf16_(kernel|pair_kernel|split_kernel)INS_4TileILi(\d+)ELi(\d+)E.*?EE"
+
+
+def tag(name):
+    m = re.search(GEMM + r"Li\d+ELi\d+ELb[01]ELb[01]ELi(\d)E", name)
+    return int(m[4]) if m and m[1] == "kernel" else -1
+
+
+def product(launched, M, N):
+    """How a product of M x N was made: by a kernel for few tokens, in K parts (of which tile and how many), else whole or cut in two, and
+    whether operands were turned first."""
+    turned = [l for l in launched if "transpose" in l[0]]
+    rest = [l for l in launched if "transpose" not in l[0]]
+    for few in ("few_tokens", "one_token"):
+        if few in rest[0][0]:
+            assert len(rest) == 1
+            return (few,)
+    m = re.search(GEMM, rest[0][0])
+    tile = (int(m[2]), int(m[3]))
+    if m[1] == "split_kernel":
+        assert len(rest) == 2 and "join_kernel" in rest[1][0] and not turned
+        return ("parts", tile, rest[0][1][0] // (-(-M // tile[0]) * -(-N // tile[1])))
+    assert len(rest) <= 2
+    return ("cut" if len(rest) == 2 else "whole", "turned" if turned else "as they stand")
+
+
+def plans(fake, lib, T, D, F):
+    """Every product of a bf16 training step, and how it was made."""
+    c, out = mlp_cfg("bf16", T, D, F), set()
+
+    def launched(call, *args):
+        fake.fake_forget()
+        assert call(lib, c, T, *args) == OK, (T, D, F)
+        return launches(fake)
+
+    is_epilogue = lambda l, e: re.search(GEMM + "Li%dE" % e, l[0])
+    for save in (False, True):
+        l = launched(forward, save)
+        up = max(1, sum(1 for x in l if is_epilogue(x, 4)))
+        out |= {("up", save, *product(l[:up], T, 2 * F)), ("down", *product(l[up:], T, D))}
+    l = launched(backward, ("dx",))
+    first = max(i for i, x in enumerate(l) if is_epilogue(x, 5)) + 1
+    out |= {("dh", *product(l[:first], T, F)), ("dx", *product(l[first:], T, D))}
+    both = launched(backward, ("gate_up_w", "down_w"))[first:]
+    alone = [launched(backward, ("gate_up_w",))[first:], launched(backward, ("down_w",))]
+    if len(both) == 1 and "pair" in both[0][0]:
+        assert all(len(a) == 1 and a[0][0] == both[0][0] for a in alone)
+        out.add(("weights together", re.search(GEMM, both[0][0]).groups()[1:]))
+    else:
+        out |= {("gate_up_w", *product(alone[0], 2 * F, D)), ("down_w", *product(alone[1], D, F))}
+    return out
+
+
+def the_gpu_tests_reach_every_kernel_and_plan(fake, lib, mlp, rope):
+    """mlp: [dtype, T, D, F]; rope: [dtype, pairing, T, hq, hk, d, pairs] of the GPU tests."""
+    seen, reached = set(), set()
+    for dtype, T, D, F in mlp:
+        c = mlp_cfg(dtype, T, D, F)
+        for call in (lambda: forward(lib, c, T), lambda: forward(lib, c, T, save=False), lambda: backward(lib, c, T)):
+            fake.fake_forget()
+            assert call() == OK, (dtype, T, D, F)
+            seen |= {l[0] for l in launches(fake)}
+        if dtype == "bf16":
+            reached |= plans(fake, lib, T, D, F)
+    fake.fake_forget()
+    for dtype, pairing, T, hq, hk, d, pairs in rope:
+        assert rotate(lib, T, dtype, pairing, (hq, hk), d, pairs) == OK
+    assert positions(lib, [(3, 0, 0)], [0, 1]) == OK
+    seen |= {l[0] for l in launches(fake)}
+    own = kernels(fake)
+    assert len(own) > 60 and own <= seen, sorted(own - seen)
+    # ... and every plan that any of 20 000 other sizes has
+    rng, missing = random.Random(1), {}
+    for _ in range(20000):
+        T, D, F = round(2 ** rng.uniform(0, 16)), max(1, round(2 ** rng.uniform(0, 10.5))) * 8, max(1, round(2 ** rng.uniform(0, 12))) * 8
+        if D * F < 1 << 29:
+            for p in plans(fake, lib, T, D, F) - reached:
+                missing.setdefault(p, []).append((T * D * F, T, D, F))
+    assert not missing, {p: min(s)[1:] for p, s in missing.items()}
 
 
 if __name__ == "__main__":

@@ -54,3 +54,20 @@ def test_gated_encoders_have_the_limits_of_the_operator():
         # 2^33 gates in fp32: a launch of 64 x 64 tiles has a thread for 16 of both halves
         assert size(act, 64, 1024, (1 << 23) - 1, "f32") > 0 and size(act, 64, 1024, 1 << 23, "f32") == 0
     assert size("gelu_erf", 8192, 262144) > 0 and size("gelu_erf", 64, 1024, 1 << 23, "f32") > 0      # as before
+
+
+def test_the_gpu_tests_reach_every_kernel_and_plan(run):
+    import test_gpu_gated_mlp as G
+    import test_gpu_operator_plans as P
+    import test_gpu_operators_large as L
+    import test_gpu_rope as R
+
+    def sizes(test, names):
+        return next(m.args[1] for m in test.pytestmark if m.name == "parametrize" and m.args[0] == names)
+
+    mlp = [("bf16", *s) for s in G.SIZES + G.LARGE + P.PLANS + sizes(L.test_every_kernel_of_the_products, "T,D,F") + sizes(L.test_products_in_parts, "T,D,F")]
+    mlp += [("f32", *s) for t in (G.test_f32_training_step, G.test_f32_many_tokens) for s in sizes(t, "T,D,F")]
+    mlp += [("bf16", T, D, F) for T in (1, 2) for D, F in sizes(G.test_bf16_one_and_two_tokens, "D,F")]
+    mlp += [("bf16", T, D, F) for T in sizes(G.test_bf16_few_tokens, "T") for D, F, _, _ in sizes(G.test_bf16_few_tokens, "D,F,act,bias")]
+    rope = [(t, p, *s) for t in ("bf16", "f32") for p in ("half", "adjacent") for s in sizes(R.test_rotation_and_inverse, "T,hq,hk,d,pairs") + P.ROPE_PLANS]
+    run("the_gpu_tests_reach_every_kernel_and_plan", mlp, rope)
