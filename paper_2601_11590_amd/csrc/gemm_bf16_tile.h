@@ -88,8 +88,8 @@ __device__ __forceinline__ void rotate_pair(float& a, float& b, float cos, float
 
 // Gate of a gated MLP: act(g) and act'(g).  SiLU: p = sigmoid(g), g p and p (1 + g (1 - p)).  GELU (erf): g Phi(g) and
 // Phi(g) + g phi(g), Phi from the tail; beyond 7.5
-// the tail's factor is held too (gelu_erf_fast lets it grow: -3e6 at -1e20), so a NaN, which fminf makes 7.5, comes through the
-// other term, whose maximum keeps it (fmaxf would not).  GELU (tanh): with s = sigmoid(2 u(g)), g s and
+// the tail's factor is held too (gelu_erf_fast lets it grow: -3e6 at -1e20), so a NaN, which fminf makes 7.5, and -infinity, which the
+// formula makes 0 * infinity, come through the other term (fmaxf would lose both).  GELU (tanh): with s = sigmoid(2 u(g)), g s and
 // s + g s (1 - s) 2 u'(g), u spelled the same in both, so that H has the same bits whether P and Q are kept or not.  ACT:
 // GemmArgs::act.
 __device__ __forceinline__ float gelu_tanh_tail(float g, float z) {         // 1 - s;  z = g^2, held to 1e30
@@ -98,14 +98,14 @@ __device__ __forceinline__ float gelu_tanh_tail(float g, float z) {         // 1
 template <int ACT> __device__ __forceinline__ float gate_act(float g) {
   if constexpr (ACT == 0) {
     const float a = fminf(fabsf(g), 7.5f);
-    return fmaf(-a, gauss_tail(a), __builtin_elementwise_maximum(g, 0.f));
+    return fmaf(-a, gauss_tail(a), g > 0.f ? g : 0.f * g);
   } else if constexpr (ACT == 1) return g * (1.0f - gelu_tanh_tail(g, fminf(g * g, 1e30f)));
   else return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g));
 }
 template <int ACT> __device__ __forceinline__ float gate_act_d(float g, float& a) {
   if constexpr (ACT == 0) {
     const float m = fminf(fabsf(g), 7.5f), e = gauss_tail(m);
-    a = fmaf(-m, e, __builtin_elementwise_maximum(g, 0.f));
+    a = fmaf(-m, e, g > 0.f ? g : 0.f * g);
     return fmaf(g, 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752044448170368f * g * g), g >= 0.f ? 1.0f - e : e);
   } else if constexpr (ACT == 1) {
     const float z = fminf(g * g, 1e30f);               // beyond, s (1 - s) is 0: no 0 * infinity

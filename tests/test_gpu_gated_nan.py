@@ -51,6 +51,21 @@ def test_a_gate_of_nan(how, dtype, T, act):
 
 
 @pytest.mark.parametrize("act", W.GATED_ACTS)
+@pytest.mark.parametrize("dtype,T", [("bf16", 1), ("bf16", 9), ("bf16", 300), ("f32", 40)])
+def test_a_gate_of_infinity(dtype, T, act):
+    # act(g) = g * (0 .. 1) of the formulas: -infinity * 0 is NaN, +infinity stays
+    D, F = 128, 264
+    w, x, _ = make(T, D, F, DT[dtype], True, T)
+    op = B.GatedMLP(dtype, D, F, act=act, max_tokens=T, use_bias=True, training=True)
+    for value in (-float("inf"), float("inf")):
+        w["gate_up_b"][37] = value
+        y, _ = op.forward(w, x, save=True)
+        assert (torch.isnan(y) if value < 0 else ~torch.isfinite(y)).all(), value
+        y = op.forward(w, x)
+        assert (torch.isnan(y) if value < 0 else ~torch.isfinite(y)).all(), value
+
+
+@pytest.mark.parametrize("act", W.GATED_ACTS)
 @pytest.mark.parametrize("dtype,tile", [("f32", -1)] + [("bf16", t) for t in (0, 2, 4, 5, 7, 8)])
 def test_a_gate_of_nan_in_the_encoder(dtype, tile, act):
     cfg = W.EncoderConfig(name="nan", dtype=dtype, num_layers=1, hidden=256, num_heads=4, head_dim=64, mlp_dim=264, patch=4, temporal_patch=1,
