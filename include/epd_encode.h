@@ -264,8 +264,9 @@ epd_status epd_encode_cached(epd_handle h, epd_store_handle s, uint64_t model_sa
  * call names its sizes, buffers and stream, allocates nothing, waits for nothing and may be captured
  * into a graph.  Calls share nothing, so they may be made from several threads and streams; where a call takes
  * a workspace, that is its own until its kernels have run.  Buffers and stream belong to the
- * current device.  Outputs must not overlap inputs unless it is said that they may.  Results are
- * deterministic.  On an error nothing is launched (EPD_ERR_HIP: nothing further). */
+ * current device.  Outputs must not overlap inputs unless it is said that they may, nor each other.  Results are
+ * deterministic.  Launches are planned for all units of the device; on a CU-masked stream (epd_encode_set_compute_units) they
+ * are right and slower than they could be.  On an error nothing is launched (EPD_ERR_HIP: nothing further). */
 
 /* Message of the last failure of such a call on this thread.  Never NULL. */
 const char* epd_op_last_error(void);

@@ -674,7 +674,8 @@ def rope_positions(span_thw, cu_spans, start=None, t_step: int = 1, device: str 
 
 
 class Rope:
-    """Rotation of q / k rows by positions on several axes (``epd_rope_apply``)."""
+    """Rotation of q / k rows by positions on several axes (``epd_rope_apply``).  Not seen by autograd: results carry no gradient, the
+    backward pass is ``apply(..., inverse=True)`` on the gradients of the outputs."""
 
     def __init__(self, dtype: str, head_dim: int, pairs: Sequence[int], layout: str = "sections", ladder: str = "axis", pairing: str = "half",
                  base: float = 10000.0):
@@ -748,7 +749,8 @@ def epd_gated_mlp_backward(cfg: epd_gated_mlp_cfg, weights: epd_gated_mlp_weight
 
 class GatedMLP:
     """Y = (act(X Wg^T) * (X Wu^T)) Wd^T with optional biases, and its backward pass.  Owns the workspace of its calls, so one call at
-    a time: calls on other streams have to be ordered by the caller, as do replays of graphs that captured calls of one object.
+    a time: calls on other streams have to be ordered by the caller, as do replays of graphs that captured calls of one object, which
+    has to outlive them.  Not seen by autograd, whatever requires gradients: ``forward`` returns values only, the backward pass is ``backward``.
     Weights are passed with every call, as a dict of gate_up_w [2F, D] (gate rows, then up rows), down_w [D, F] and, with biases,
     gate_up_b [2F], down_b [D]."""
 

@@ -24,8 +24,7 @@ namespace epd {
 // waves take K in turn, 64 at a time, each with a ring of S stages of its own in LDS, which direct loads of 8 rows x 128 bytes
 // fill and nobody else reads, so no wave waits for another until their sums meet, in the order of the waves.
 //   What it replaced loaded the operands of the matrix instructions straight to registers, 16 rows x 64 bytes an instruction: half
-// lines of twice as many rows, at 4.1 TB/s where whole lines reach 5.2 (3200 x 12 800, 16 tokens: gate and up 52 -> 33.6 us, down
-// 32 -> 20.7).  Up to how many tokens: few_up, few_down.
+// lines of twice as many rows (3200 x 12 800, 16 tokens: gate and up 52 -> 33.6 us, 3.2 -> 4.9 TB/s, down 32 -> 20.7, 2.6 -> 4.0).  Up to how many tokens: few_up, few_down.
 struct FewArgs {
   const void* X; const void* W; const void* bias;
   void* out;
@@ -172,7 +171,8 @@ __global__ __launch_bounds__(64 * NW) void few_tokens_kernel(FewArgs a) {
 
 // The same for one token, where matrix instructions would have 15 empty columns and X as much traffic as W: a channel's row (GATED: its
 // two rows) per wave, or per block with the K of its four waves in turn, 16 bytes a lane straight to registers.  Bound: HBM (gate and up of
-// 3200 x 12 800: 24.6 us, 6.7 TB/s; few_tokens_kernel 28.4).
+// 3200 x 12 800: 24.6 us; few_tokens_kernel 28.4; both products 40.3 us, 6.1 TB/s, on other weights each time, 38.6 on the same, which the
+// last-level cache holds in part).
 template <int SPLIT, int U, bool GATED, bool NT>
 __global__ __launch_bounds__(256) void one_token_kernel(FewArgs a) {
   constexpr int WB = GATED ? 2 : 1;

@@ -11,7 +11,8 @@
 // of 128 a table in memory would save one double multiplication and a dozen fp32 ones per 100 values.)
 //
 // Angles.  In turns, r = pos * (f_p / 2 pi) in fp64, so that an int32 position far into a long context
-// keeps its phase (2^31 turns at 2^-53: 2e-7 of a turn; 1e-12 within a million tokens).  The quarter
+// keeps its phase (f_p, its quotient and the product are off by 2^-52 together or so, and 2^31 positions at f_p = 1 are 3.4e8
+// turns: 1e-7 of a turn; 4e-11 within a million tokens).  The quarter
 // turns are taken off in fp64; what is left, |x| <= pi / 4, goes through the Taylor sums of sine and
 // cosine in fp32 (next terms 1.8e-9 and 1.2e-10, below half a step of fp32).
 #include "op_error.h"
