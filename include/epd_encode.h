@@ -364,8 +364,8 @@ uint64_t epd_gated_mlp_workspace_bytes(const epd_gated_mlp_cfg* cfg);
 uint64_t epd_gated_mlp_saved_bytes(const epd_gated_mlp_cfg* cfg, int32_t tokens);
 
 /* Y = MLP(X).
- *   x, y    device [tokens, D], rows ld_x / ld_y >= D elements apart (below 2^22; bf16: multiples of 8, 16-byte
- *           aligned; tokens = 1: not looked at); y may be x (with the same rows)
+ *   x, y    device [tokens, D], 16-byte aligned in bf16, rows ld_x / ld_y elements apart: D .. 2^22 - 1, in bf16 a multiple
+ *           of 8 (ld of a single row is not looked at); y may be x (with the same rows)
  *   tokens  0 .. max_tokens; 0 launches nothing
  *   saved   device, epd_gated_mlp_saved_bytes(cfg, tokens) bytes, aligned as x, or NULL: receives what
  *           epd_gated_mlp_backward needs of this call (its layout is the library's: about 7 F bytes a token in bf16, 8 F in fp32);
