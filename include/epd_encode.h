@@ -383,6 +383,111 @@ epd_status epd_gated_mlp_backward(const epd_gated_mlp_cfg* cfg, const epd_gated_
                                   const void* saved, const epd_gated_mlp_grads* grads, void* workspace,
                                   uint64_t workspace_bytes, void* stream);
 
+/* Embeddings of sequences of text and visual tokens (V_m || V_t, section 3.1 "Prefill Stage", Eq. 2): the rows that the next stage starts
+ * from.  ids says what stands where:
+ *   0 <= id < vocab          out = table[id] * scale        (a text token)
+ *   -num_rows <= id < 0      out = rows[-1 - id]            (row -1 - id of V_m, or of any other source)
+ *   any other id             out = 0, and no gradient       (padding)
+ * fp32 arithmetic, rounded once. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(epd_embed_cfg)                                                    */
+  int32_t dtype;        /* epd_dtype of table, rows and their gradients                              */
+  int32_t out_dtype;    /* epd_dtype of out and dout: dtype, or EPD_F32                              */
+  int32_t vocab;        /* rows of the table, 1 .. 2^30                                              */
+  int32_t hidden;       /* 1 .. 65536                                                                */
+  int32_t max_tokens;   /* largest `tokens` of any call, 1 .. 2^24                                   */
+  float scale;          /* finite                                                                    */
+} epd_embed_cfg;
+
+/* table device [vocab, hidden] and rows device [num_rows, hidden] (NULL where num_rows = 0; num_rows <= 2^30), dense; ids device int32 [tokens];
+ * out device [tokens, hidden], rows ld_out elements apart (that of a single row is not looked at).  tokens = 0 launches nothing. */
+epd_status epd_embed(const epd_embed_cfg* cfg, const void* table, const void* rows, int32_t num_rows, const int32_t* ids, int32_t tokens,
+                     void* out, int64_t ld_out, void* stream);
+
+/* Bytes of device workspace (256-byte aligned) that epd_embed_backward needs; 0 when cfg is invalid. */
+uint64_t epd_embed_workspace_bytes(const epd_embed_cfg* cfg);
+
+/* Gradients of sum(out * dout) by the table ([vocab, hidden]) and by the rows ([num_rows, hidden]), dense; NULL = not wanted.  Every row is
+ * written, rows of no token as zeros.  The tokens of a row are added in fp32, in an order that their places alone decide. */
+epd_status epd_embed_backward(const epd_embed_cfg* cfg, const int32_t* ids, int32_t tokens, const void* dout, int64_t ld_dout, int32_t num_rows,
+                              void* dtable, void* drows, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* The residual's addition and RMS norm:  s = x + residual,  y = s / sqrt(mean(s^2) + eps) * gain, in fp32; s is rounded where it is
+ * kept (sum) and not before y is made of it.  q: y in 8 bits, as epd_quant_rows makes them of y before any rounding.  Mean squares
+ * beyond fp32 give zeros. */
+typedef struct {
+  uint32_t struct_size;   /* sizeof(epd_add_norm_cfg)                                                */
+  int32_t dtype;          /* epd_dtype of x, gain, y and their gradients                             */
+  int32_t residual_dtype; /* epd_dtype of residual, sum and their gradients: dtype, or EPD_F32       */
+  int32_t hidden;         /* 1 .. 65536                                                              */
+  int32_t max_tokens;     /* largest `tokens` of any call                                            */
+  float eps;              /* >= 0                                                                    */
+} epd_add_norm_cfg;
+typedef struct {          /* device, [tokens, hidden]; rows ld_* elements apart (that of a single row is not looked at) */
+  const void* x;          /* NULL: s = residual                                                      */
+  const void* residual;   /* NULL: s = x                                                             */
+  void* sum;              /* s, NULL = not wanted; may be residual                                   */
+  void* y;                /* NULL = not wanted; may be x                                             */
+  void* q;                /* int8, NULL = not wanted                                                 */
+  float* scale;           /* [tokens], with q                                                        */
+  int64_t ld_x, ld_residual, ld_sum, ld_y, ld_q;
+} epd_add_norm_rows;
+typedef struct {          /* as above                                                                */
+  const void* sum;        /* the s that the forward call kept                                        */
+  const void* dy;
+  const void* dsum;       /* gradient by sum of what else took it, NULL = none                       */
+  void* dx;               /* dtype; NULL = not wanted; may be dy                                     */
+  void* dresidual;        /* residual_dtype, the same values; NULL = not wanted; may be dsum         */
+  void* gain;             /* [hidden], dtype; NULL = not wanted                                      */
+  int64_t ld_sum, ld_dy, ld_dsum, ld_dx, ld_dresidual;
+} epd_add_norm_grads;
+
+/* tokens = 0 launches nothing. */
+epd_status epd_add_norm(const epd_add_norm_cfg* cfg, const epd_add_norm_rows* rows, const void* gain, int32_t tokens, void* stream);
+
+/* Bytes of device workspace (256-byte aligned) that epd_add_norm_backward needs for the gradient of gain; 0 when cfg is invalid. */
+uint64_t epd_add_norm_workspace_bytes(const epd_add_norm_cfg* cfg);
+
+/* Gradients of sum(y * dy) + sum(s * dsum) by x (and the residual) and by gain, at `sum`.  The workspace is not looked at where the
+ * gradient of gain is not wanted; tokens = 0 clears it. */
+epd_status epd_add_norm_backward(const epd_add_norm_cfg* cfg, const epd_add_norm_grads* grads, const void* gain, int32_t tokens,
+                                 void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Rows in 8 bits:  m = max(max |x|, 2^-100),  q = x * (127 / m) rounded to the nearest even,  scale = m / 127;  x ~ q * scale.  A row with
+ * a NaN or an infinity has q = 0 and scale NaN, so that every product with it is NaN.  x device [rows, cols] of `dtype`, q device int8
+ * [rows, cols], rows ld_x / ld_q elements apart (that of a single row is not looked at); scale device [rows]; cols 1 .. 65536.  rows = 0
+ * launches nothing. */
+epd_status epd_quant_rows(int32_t dtype, const void* x, int64_t ld_x, int32_t rows, int32_t cols, void* q, int64_t ld_q, float* scale, void* stream);
+
+/* out = q * scale of the row, rounded once to `dtype`. */
+epd_status epd_dequant_rows(const void* q, int64_t ld_q, const float* scale, int32_t rows, int32_t cols, int32_t dtype, void* out, int64_t ld_out,
+                            void* stream);
+
+/* Product of rows in 8 bits:  y[t][n] = (sum_k x[t][k] w[n][k]) * x_scale[t] * scale[n] (+ bias[n]);  the sum is exact (int32), the rest
+ * fp32, rounded once.  An operator of serving: integers have no gradient. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(epd_int8_linear_cfg)                                               */
+  int32_t in_features;  /* K, a multiple of 16, <= 131056                                            */
+  int32_t out_features; /* N, a multiple of 8, <= 2^20; K * N < 2^32                                 */
+  int32_t out_dtype;    /* epd_dtype of y                                                            */
+  int32_t use_bias;     /* 1: bias is added                                                          */
+  int32_t max_tokens;   /* largest `tokens` of any call, < 2^22; times N < 2^36                      */
+} epd_int8_linear_cfg;
+typedef struct {        /* device, dense                                                             */
+  const void* w;        /* int8 [N, K], 16-byte aligned                                              */
+  const float* scale;   /* [N]; 16-byte aligned                                                      */
+  const float* bias;    /* [N], 16-byte aligned; ignored when use_bias == 0                          */
+} epd_int8_linear_weights;
+
+/* Bytes of device workspace (256-byte aligned) that a call with `cfg` needs; 0 when cfg is invalid. */
+uint64_t epd_int8_linear_workspace_bytes(const epd_int8_linear_cfg* cfg);
+
+/* x device int8 [tokens, K], 16-byte aligned, rows ld_x apart: a multiple of 16, K .. 2^22 - 16; x_scale device [tokens]; y device [tokens, N], 16-byte
+ * aligned, rows ld_y elements apart: a multiple of 8, N .. 2^22 - 8 (the ld of a single row is not looked at).  tokens = 0 launches nothing.
+ * Nothing in the workspace is kept from one call to the next. */
+epd_status epd_int8_linear(const epd_int8_linear_cfg* cfg, const epd_int8_linear_weights* weights, const void* x, int64_t ld_x, const float* x_scale,
+                           int32_t tokens, void* y, int64_t ld_y, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* Release host-side state (events, pinned staging).  The workspace stays the caller's. */
 epd_status epd_encode_destroy(epd_handle h);
 

@@ -87,6 +87,35 @@ class epd_gated_mlp_grads(C.Structure):
     _fields_ = [("dx", C.c_void_p), ("ld_dx", C.c_int64)] + [(n, C.c_void_p) for n in _GATED_FIELDS]
 
 
+class epd_embed_cfg(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("vocab", C.c_int32), ("hidden", C.c_int32),
+                ("max_tokens", C.c_int32), ("scale", C.c_float)]
+
+
+class epd_add_norm_cfg(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("residual_dtype", C.c_int32), ("hidden", C.c_int32), ("max_tokens", C.c_int32),
+                ("eps", C.c_float)]
+
+
+class epd_add_norm_rows(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("x", "residual", "sum", "y", "q", "scale")] +
+                [(n, C.c_int64) for n in ("ld_x", "ld_residual", "ld_sum", "ld_y", "ld_q")])
+
+
+class epd_add_norm_grads(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("sum", "dy", "dsum", "dx", "dresidual", "gain")] +
+                [(n, C.c_int64) for n in ("ld_sum", "ld_dy", "ld_dsum", "ld_dx", "ld_dresidual")])
+
+
+class epd_int8_linear_cfg(C.Structure):
+    _fields_ = [(n, C.c_uint32 if n == "struct_size" else C.c_int32)
+                for n in ("struct_size", "in_features", "out_features", "out_dtype", "use_bias", "max_tokens")]
+
+
+class epd_int8_linear_weights(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w", "scale", "bias")]
+
+
 EXPORTS = ["epd_encode_workspace_bytes", "epd_encode_create", "epd_encode", "epd_encode_destroy",
            "epd_encode_last_error", "epd_encode_debug_hidden", "epd_encode_set_timing", "epd_encode_set_tuning", "epd_encode_set_compute_units",
            "epd_encode_get_timing", "epd_preprocess", "epd_encode_cached", "epd_store_create",
@@ -94,6 +123,9 @@ EXPORTS = ["epd_encode_workspace_bytes", "epd_encode_create", "epd_encode", "epd
            "epd_store_stats", "epd_probe_stream_read", "epd_probe_mfma_rate", "epd_probe_gemm_plan"]
 OPERATOR_EXPORTS = ["epd_op_last_error", "epd_rope_apply", "epd_rope_tokens", "epd_rope_positions", "epd_gated_mlp_workspace_bytes", "epd_gated_mlp_saved_bytes",
                     "epd_gated_mlp", "epd_gated_mlp_backward"]    # the operators beside the encoder
+
+ENTRY_EXPORTS = ["epd_embed", "epd_embed_workspace_bytes", "epd_embed_backward", "epd_add_norm", "epd_add_norm_workspace_bytes", "epd_add_norm_backward",
+                 "epd_quant_rows", "epd_dequant_rows", "epd_int8_linear_workspace_bytes", "epd_int8_linear"]    # those at the entry of the next stage
 
 
 def _load() -> C.CDLL:
@@ -169,6 +201,19 @@ def _load() -> C.CDLL:
     lib.epd_gated_mlp_backward.restype = C.c_int
     lib.epd_gated_mlp_backward.argtypes = [C.POINTER(epd_gated_mlp_cfg), C.POINTER(epd_gated_mlp_weights), C.c_void_p, C.c_int64, C.c_void_p,
                                            C.c_int64, C.c_int32, C.c_void_p, C.POINTER(epd_gated_mlp_grads), C.c_void_p, C.c_uint64, C.c_void_p]
+    V, I32, I64, U64 = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64
+    for name, cfg in (("embed", epd_embed_cfg), ("add_norm", epd_add_norm_cfg), ("int8_linear", epd_int8_linear_cfg)):
+        f = getattr(lib, "epd_%s_workspace_bytes" % name)
+        f.restype, f.argtypes = U64, [C.POINTER(cfg)]
+    for name, args in {"epd_embed": [C.POINTER(epd_embed_cfg), V, V, I32, V, I32, V, I64, V],
+                       "epd_embed_backward": [C.POINTER(epd_embed_cfg), V, I32, V, I64, I32, V, V, V, U64, V],
+                       "epd_add_norm": [C.POINTER(epd_add_norm_cfg), C.POINTER(epd_add_norm_rows), V, I32, V],
+                       "epd_add_norm_backward": [C.POINTER(epd_add_norm_cfg), C.POINTER(epd_add_norm_grads), V, I32, V, U64, V],
+                       "epd_quant_rows": [I32, V, I64, I32, I32, V, I64, V, V],
+                       "epd_dequant_rows": [V, I64, V, I32, I32, I32, V, I64, V],
+                       "epd_int8_linear": [C.POINTER(epd_int8_linear_cfg), C.POINTER(epd_int8_linear_weights), V, I64, V, I32, V, I64, V, U64, V]}.items():
+        f = getattr(lib, name)
+        f.restype, f.argtypes = C.c_int, args
     return lib
 
 
@@ -826,6 +871,294 @@ class GatedMLP:
             setattr(grads, n, out[n].data_ptr())
         grads.ld_dx = self.hidden
         self._call(epd_gated_mlp_backward, self.cfg, self._weights(weights), px, ld_x, pdy, ld_dy, T, saved.data_ptr(), grads, self._base, self.workspace_bytes)
+        return out
+
+
+def epd_embed(cfg: epd_embed_cfg, table: int, rows: Optional[int], num_rows: int, ids: int, tokens: int, out: int, ld_out: int, stream: int) -> None:
+    _op_check(lib.epd_embed(cfg, table, rows, num_rows, ids, tokens, out, ld_out, stream))
+
+
+def epd_embed_workspace_bytes(cfg: epd_embed_cfg) -> int:
+    return int(lib.epd_embed_workspace_bytes(cfg))
+
+
+def epd_embed_backward(cfg: epd_embed_cfg, ids: int, tokens: int, dout: int, ld_dout: int, num_rows: int, dtable: Optional[int], drows: Optional[int],
+                       workspace: int, workspace_bytes: int, stream: int) -> None:
+    _op_check(lib.epd_embed_backward(cfg, ids, tokens, dout, ld_dout, num_rows, dtable, drows, workspace, workspace_bytes, stream))
+
+
+def epd_add_norm(cfg: epd_add_norm_cfg, rows: epd_add_norm_rows, gain: Optional[int], tokens: int, stream: int) -> None:
+    _op_check(lib.epd_add_norm(cfg, rows, gain, tokens, stream))
+
+
+def epd_add_norm_workspace_bytes(cfg: epd_add_norm_cfg) -> int:
+    return int(lib.epd_add_norm_workspace_bytes(cfg))
+
+
+def epd_add_norm_backward(cfg: epd_add_norm_cfg, grads: epd_add_norm_grads, gain: int, tokens: int, workspace: Optional[int], workspace_bytes: int, stream: int) -> None:
+    _op_check(lib.epd_add_norm_backward(cfg, grads, gain, tokens, workspace, workspace_bytes, stream))
+
+
+def epd_quant_rows(dtype: int, x: int, ld_x: int, rows: int, cols: int, q: int, ld_q: int, scale: int, stream: int) -> None:
+    _op_check(lib.epd_quant_rows(dtype, x, ld_x, rows, cols, q, ld_q, scale, stream))
+
+
+def epd_dequant_rows(q: int, ld_q: int, scale: int, rows: int, cols: int, dtype: int, out: int, ld_out: int, stream: int) -> None:
+    _op_check(lib.epd_dequant_rows(q, ld_q, scale, rows, cols, dtype, out, ld_out, stream))
+
+
+def epd_int8_linear_workspace_bytes(cfg: epd_int8_linear_cfg) -> int:
+    return int(lib.epd_int8_linear_workspace_bytes(cfg))
+
+
+def epd_int8_linear(cfg: epd_int8_linear_cfg, weights: epd_int8_linear_weights, x: int, ld_x: int, x_scale: int, tokens: int, y: int, ld_y: int,
+                    workspace: int, workspace_bytes: int, stream: int) -> None:
+    _op_check(lib.epd_int8_linear(cfg, weights, x, ld_x, x_scale, tokens, y, ld_y, workspace, workspace_bytes, stream))
+
+
+_DTYPES = {"f32": EPD_F32, "bf16": EPD_BF16}
+_CODES = {torch.float32: EPD_F32, torch.bfloat16: EPD_BF16}
+
+
+def _sizes(cfg, **values) -> None:
+    """Fields of a configuration; numbers beyond 32 bits are refused, not wrapped."""
+    cfg.struct_size = C.sizeof(cfg)
+    for n, v in values.items():
+        if isinstance(v, int) and not -1 << 31 <= v < 1 << 31:
+            raise ValueError("%s must be an int32" % n)
+        setattr(cfg, n, v)
+
+
+def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: int, dtype: torch.dtype, index: int):
+    """Address of a matrix whose rows are contiguous, and what they are apart (one row: its stride means nothing)."""
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != cols or (rows is not None and shape[0] != rows) or t.dtype != dtype or t.get_device() != index:
+        raise ValueError("%s must be [%s, %d] of %s on device %d" % (name, "rows" if rows is None else rows, cols, dtype, index))
+    if shape[0] < 2:
+        ld, one = cols, t.stride(1)
+    else:
+        ld, one = t.stride()
+    if one != 1 and cols > 1 and shape[0]:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    return t.data_ptr() or 256, ld       # no rows: nothing is read or written
+
+
+def _dense(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int) -> int:
+    if t.shape != shape or t.dtype != dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s %s on device %d" % (name, list(shape), dtype, index))
+    return t.data_ptr() or 256
+
+
+class _Operator:
+    """Device of an operator's object and the workspace that its calls share: one call at a time."""
+
+    def _own(self, nbytes: Optional[int], device: str) -> None:
+        if nbytes == 0:
+            raise EpdError(EPD_ERR_INVALID_ARG, epd_op_last_error())
+        dev = torch.device(device)
+        self.device = torch.device(dev.type, torch.cuda.current_device()) if dev.index is None else dev
+        self._index = self.device.index
+        self.workspace, self._base, self.workspace_bytes = None, None, 0
+        if nbytes is not None:
+            self.workspace_bytes = nbytes
+            self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+            self._base = (self.workspace.data_ptr() + 255) // 256 * 256
+            self._stream = torch.cuda.current_stream(self.device).cuda_stream       # on which the workspace may be handed on
+
+    def _with_workspace(self, call, *args) -> None:
+        def on(*a):
+            if a[-1] != self._stream:         # the allocator may not hand the workspace on before this stream is through
+                self.workspace.record_stream(torch.cuda.current_stream(self.device))
+            call(*a[:-1], self._base, self.workspace_bytes, a[-1])
+        _on(self._index, on, *args)
+
+
+class Embedding(_Operator):
+    """Rows of sequences of text and visual tokens (``epd_embed``) and the gradients of both.  ids: int32, a row of the table (scaled),
+    -1 - j for row j of ``rows``, anything else for zeros.  Not seen by autograd.  With ``training`` it owns the workspace of
+    ``backward``: one such call at a time; calls on other streams have to be ordered by the caller, as do replays of graphs that
+    captured calls of one object, which has to outlive them."""
+
+    def __init__(self, dtype: str, vocab: int, hidden: int, out: Optional[str] = None, scale: float = 1.0, max_tokens: int = 1, training: bool = False,
+                 device: str = "cuda:0"):
+        c = self.cfg = epd_embed_cfg()
+        _sizes(c, dtype=_DTYPES[dtype], out_dtype=_DTYPES[out or dtype], vocab=vocab, hidden=hidden, max_tokens=max_tokens, scale=scale)
+        self.vocab, self.hidden, self.dtype, self.out_dtype, self.training = vocab, hidden, torch_dtype(dtype), torch_dtype(out or dtype), training
+        nbytes = epd_embed_workspace_bytes(c)
+        self._own(nbytes if training or nbytes == 0 else None, device)
+
+    def _ids(self, ids: torch.Tensor):
+        if ids.dim() != 1 or ids.dtype != torch.int32 or ids.get_device() != self._index or not ids.is_contiguous():
+            raise ValueError("ids must be a contiguous int32 [tokens] on %s" % self.device)
+        T = ids.shape[0]
+        if T > self.cfg.max_tokens:
+            raise EpdError(EPD_ERR_SHAPE, "%d ids: 0 .. max_tokens %d" % (T, self.cfg.max_tokens))
+        return ids.data_ptr() or 256, T
+
+    def forward(self, table: torch.Tensor, ids: torch.Tensor, rows: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Returns [tokens, hidden]: ``out``, whose rows may be any stride apart, or a new tensor."""
+        pids, T = self._ids(ids)
+        ptable = _dense(table, "table", (self.vocab, self.hidden), self.dtype, self._index)
+        R = 0 if rows is None else rows.shape[0]
+        prows = _dense(rows, "rows", (R, self.hidden), self.dtype, self._index) if R else None
+        if out is None:
+            out = torch.empty((T, self.hidden), dtype=self.out_dtype, device=self.device)
+        py, ld = _matrix(out, "out", T, self.hidden, self.out_dtype, self._index)
+        _on(self._index, epd_embed, self.cfg, ptable, prows, R, pids, T, py, ld)
+        return out
+
+    def backward(self, ids: torch.Tensor, dout: torch.Tensor, num_rows: int = 0, want: Optional[Sequence[str]] = None) -> Dict[str, torch.Tensor]:
+        """Gradients of sum(out * dout) by the table ("table") and the ``num_rows`` rows ("rows"), every row of them; ``want`` names those
+        to compute (all)."""
+        if not self.training:
+            raise EpdError(EPD_ERR_INVALID_ARG, "the object was made without training")
+        pids, T = self._ids(ids)
+        pd, ld = _matrix(dout, "dout", T, self.hidden, self.out_dtype, self._index)
+        if not 0 <= num_rows < 1 << 31:
+            raise ValueError("num_rows must be an int32 and not negative")
+        out = {}
+        for n in (("table", "rows") if num_rows else ("table",)) if want is None else want:
+            out[n] = torch.empty(({"table": self.vocab, "rows": num_rows}[n], self.hidden), dtype=self.dtype, device=self.device)
+        t, r = out.get("table"), out.get("rows")
+        self._with_workspace(epd_embed_backward, self.cfg, pids, T, pd, ld, num_rows, None if t is None else t.data_ptr(),
+                             None if r is None else r.data_ptr() or None)
+        return out
+
+
+class AddNorm(_Operator):
+    """s = x + residual and its RMS norm y = s / sqrt(mean(s^2) + eps) * gain (``epd_add_norm``), in its own type or in 8 bits, and the
+    backward pass.  ``residual``: type of the residual stream (that of x, or "f32").  Not seen by autograd.  With ``training`` it owns the
+    workspace of ``backward``: one such call at a time; calls on other streams have to be ordered by the caller, as do replays of graphs
+    that captured calls of one object, which has to outlive them."""
+
+    def __init__(self, dtype: str, hidden: int, residual: Optional[str] = None, eps: float = 1e-6, max_tokens: int = 1, training: bool = False,
+                 device: str = "cuda:0"):
+        c = self.cfg = epd_add_norm_cfg()
+        _sizes(c, dtype=_DTYPES[dtype], residual_dtype=_DTYPES[residual or dtype], hidden=hidden, max_tokens=max_tokens, eps=eps)
+        self.hidden, self.dtype, self.residual_dtype, self.training = hidden, torch_dtype(dtype), torch_dtype(residual or dtype), training
+        self._types = {"x": self.dtype, "residual": self.residual_dtype, "sum": self.residual_dtype, "y": self.dtype, "q": torch.int8, "dy": self.dtype,
+                       "dsum": self.residual_dtype, "dx": self.dtype, "dresidual": self.residual_dtype}
+        nbytes = epd_add_norm_workspace_bytes(c)
+        self._own(nbytes if training or nbytes == 0 else None, device)
+
+    def _put(self, to, name: str, t: torch.Tensor, tokens: Optional[int]) -> None:
+        p, ld = _matrix(t, name, tokens, self.hidden, self._types[name], self._index)
+        setattr(to, name, p)
+        setattr(to, "ld_" + name, ld)
+
+    def _tokens(self, t: torch.Tensor) -> int:
+        T = t.shape[0]
+        if T > self.cfg.max_tokens:
+            raise EpdError(EPD_ERR_SHAPE, "%d rows: 0 .. max_tokens %d" % (T, self.cfg.max_tokens))
+        return T
+
+    def _outputs(self, to, want, out, T: int) -> Dict[str, torch.Tensor]:
+        made = {}
+        for n in want:
+            t = out.get(n) if out else None
+            made[n] = t = torch.empty((T, self.hidden), dtype=self._types[n], device=self.device) if t is None else t
+            self._put(to, n, t, T)
+        return made
+
+    def forward(self, gain: Optional[torch.Tensor], x: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, want: Sequence[str] = ("sum", "y"),
+                out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+        """x, residual: [tokens, hidden], rows any stride apart; one of them may be None.  ``want``: any of "sum", "y" and "q", which comes
+        with "scale" (``quant_rows``).  ``out`` may name tensors for the outputs; sum may be ``residual``, y may be ``x``."""
+        r = epd_add_norm_rows()
+        some = x if x is not None else residual
+        if some is None:
+            raise ValueError("neither x nor residual")
+        T = self._tokens(some)
+        if x is not None:
+            self._put(r, "x", x, T)
+        if residual is not None:
+            self._put(r, "residual", residual, T)
+        made = self._outputs(r, want, out, T)
+        if "q" in made:
+            s = out.get("scale") if out else None
+            made["scale"] = s = torch.empty(T, dtype=torch.float32, device=self.device) if s is None else s
+            r.scale = _dense(s, "scale", (T,), torch.float32, self._index)
+        pg = None if gain is None else _dense(gain, "gain", (self.hidden,), self.dtype, self._index)
+        _on(self._index, epd_add_norm, self.cfg, r, pg, T)
+        return made
+
+    def backward(self, gain: torch.Tensor, sum: torch.Tensor, dy: torch.Tensor, dsum: Optional[torch.Tensor] = None, want: Optional[Sequence[str]] = None,
+                 out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+        """Gradients of sum(y * dy) + sum(s * dsum) at the kept ``sum``: "dx" (in the type of x), "dresidual" (the same values in that of
+        the residual) and "gain".  ``want`` names those to compute (all; dresidual only where its type is another); ``out`` may name
+        tensors for them; dx may be ``dy``, dresidual may be ``dsum``."""
+        if not self.training:
+            raise EpdError(EPD_ERR_INVALID_ARG, "the object was made without training")
+        if want is None:
+            want = ("dx", "gain") if self.dtype == self.residual_dtype else ("dx", "dresidual", "gain")
+        g, T = epd_add_norm_grads(), self._tokens(sum)
+        self._put(g, "sum", sum, T)
+        self._put(g, "dy", dy, T)
+        if dsum is not None:
+            self._put(g, "dsum", dsum, T)
+        made = self._outputs(g, [n for n in want if n != "gain"], out, T)
+        if "gain" in want:
+            t = out.get("gain") if out else None
+            made["gain"] = t = torch.empty(self.hidden, dtype=self.dtype, device=self.device) if t is None else t
+            g.gain = _dense(t, "gain", (self.hidden,), self.dtype, self._index)
+        self._with_workspace(epd_add_norm_backward, self.cfg, g, _dense(gain, "gain", (self.hidden,), self.dtype, self._index), T)
+        return made
+
+
+def quant_rows(x: torch.Tensor, out: Optional[torch.Tensor] = None):
+    """Rows in 8 bits (``epd_quant_rows``): (q int8, scale fp32 [rows]) with x ~ q * scale; rows any stride apart."""
+    index, shape = x.get_device(), x.shape
+    if index < 0 or len(shape) != 2 or x.dtype not in _CODES or shape[0] >= 1 << 31 or shape[1] >= 1 << 31:
+        raise ValueError("x must be a device matrix of float32 or bfloat16")
+    px, ld_x = _matrix(x, "x", shape[0], shape[1], x.dtype, index)
+    q = torch.empty(shape, dtype=torch.int8, device=x.device) if out is None else out
+    pq, ld_q = _matrix(q, "out", shape[0], shape[1], torch.int8, index)
+    scale = torch.empty(shape[0], dtype=torch.float32, device=x.device)
+    _on(index, epd_quant_rows, _CODES[x.dtype], px, ld_x, shape[0], shape[1], pq, ld_q, scale.data_ptr() or 256)
+    return q, scale
+
+
+def dequant_rows(q: torch.Tensor, scale: torch.Tensor, dtype: str = "bf16", out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q * scale of its row (``epd_dequant_rows``)."""
+    index, shape, kind = q.get_device(), q.shape, torch_dtype(dtype)
+    if index < 0 or len(shape) != 2 or shape[0] >= 1 << 31 or shape[1] >= 1 << 31:
+        raise ValueError("q must be a device matrix of int8")
+    pq, ld_q = _matrix(q, "q", shape[0], shape[1], torch.int8, index)
+    ps = _dense(scale, "scale", (shape[0],), torch.float32, index)
+    if out is None:
+        out = torch.empty(shape, dtype=kind, device=q.device)
+    po, ld_o = _matrix(out, "out", shape[0], shape[1], kind, index)
+    _on(index, epd_dequant_rows, pq, ld_q, ps, shape[0], shape[1], _DTYPES[dtype], po, ld_o)
+    return out
+
+
+class Int8Linear(_Operator):
+    """y = (x w^T) * x_scale * scale (+ bias) of rows in 8 bits (``epd_int8_linear``, ``quant_rows``).  Owns the workspace of its calls, so
+    one call at a time: calls on other streams have to be ordered by the caller, as do replays of graphs that captured calls of one
+    object, which has to outlive them.  Weights are passed with every call, as a dict of w int8 [N, K], scale fp32 [N] and, with a bias,
+    bias fp32 [N]."""
+
+    def __init__(self, in_features: int, out_features: int, out: str = "bf16", max_tokens: int = 1, use_bias: bool = False, device: str = "cuda:0"):
+        c = self.cfg = epd_int8_linear_cfg()
+        _sizes(c, in_features=in_features, out_features=out_features, out_dtype=_DTYPES[out], use_bias=int(use_bias), max_tokens=max_tokens)
+        self.in_features, self.out_features, self.use_bias, self.out_dtype = in_features, out_features, use_bias, torch_dtype(out)
+        self._own(epd_int8_linear_workspace_bytes(c), device)
+
+    def forward(self, weights: Dict[str, torch.Tensor], x: torch.Tensor, x_scale: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x: int8 [tokens, K], rows a multiple of 16 apart; x_scale: fp32 [tokens].  Returns y [tokens, N]: ``out``, rows a multiple of 8
+        apart, or a new tensor."""
+        K, N, i = self.in_features, self.out_features, self._index
+        w = epd_int8_linear_weights(_dense(weights["w"], "w", (N, K), torch.int8, i), _dense(weights["scale"], "scale", (N,), torch.float32, i),
+                                    _dense(weights["bias"], "bias", (N,), torch.float32, i) if self.use_bias else None)
+        T = x.shape[0]
+        if T > self.cfg.max_tokens:
+            raise EpdError(EPD_ERR_SHAPE, "x has %d rows: 0 .. max_tokens %d" % (T, self.cfg.max_tokens))
+        px, ld_x = _matrix(x, "x", T, K, torch.int8, i)
+        ps = _dense(x_scale, "x_scale", (T,), torch.float32, i)
+        if out is None:
+            out = torch.empty((T, N), dtype=self.out_dtype, device=self.device)
+        py, ld_y = _matrix(out, "out", T, N, self.out_dtype, i)
+        self._with_workspace(epd_int8_linear, self.cfg, w, px, ld_x, ps, T, py, ld_y)
         return out
 
 

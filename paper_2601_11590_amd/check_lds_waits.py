@@ -225,7 +225,8 @@ def check_asm(asm: str, only: Tuple[str, ...] = ()) -> List[str]:
     return errors
 
 
-def check_sources(hipcc: str, flags, sources, only=("gemm_bf16_kernel", "gemm_bf16_pair_kernel", "gemm_bf16_split_kernel", "attn_bf16_kernel", "few_tokens_kernel")) -> None:
+def check_sources(hipcc: str, flags, sources, only=("gemm_bf16_kernel", "gemm_bf16_pair_kernel", "gemm_bf16_split_kernel", "attn_bf16_kernel", "few_tokens_kernel", "int8_gemm_kernel",
+                                               "int8_split_kernel", "int8_few_kernel")) -> None:
     """Compile each source to device assembly and run the check; raise on any finding."""
     with tempfile.TemporaryDirectory() as tmp:
         for src in sources:

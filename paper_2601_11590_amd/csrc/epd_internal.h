@@ -21,8 +21,11 @@ enum Epilogue : int {
                      // out[m][c] = act(gate_c + bias_c) * (up_c + bias_(gate_rows + c));  bf16: N = 2 *
                      // round_up(gate_rows, 16), fp32: N = 2 * gate_rows.  bf16: keep_* (if any) get P = act(G) and
                      // Q = U act'(G); fp32: gu (if any) gets G | U
-  EPI_DGATED = 5     // acc = dH[m][c], N = gate_rows; dgu[m][c] = dH Q, dgu[m][gate_rows + c] = dH P;
+  EPI_DGATED = 5,    // acc = dH[m][c], N = gate_rows; dgu[m][c] = dH Q, dgu[m][gate_rows + c] = dH P;
                      // fp32: from gu, and out[m][c] = act(G) U
+  EPI_INT8 = 6,      // A and W hold bytes, two to an element of K, lda and ldw; the sums are int32:
+                     // out[m][n] = acc * row_scales[m] * col_scales[n] + col_bias[n]
+  EPI_INT8_SUMS = 7  // the same operands; out[m][n] = acc, int32
 };
 
 struct GemmArgs {
@@ -81,6 +84,7 @@ struct GemmArgs {
   float* sums;          // EPI_DGATED, bf16 path: fp32 [rows of sums, 2 * gate_rows] or nullptr: sums of dG | dU over the rows of each wave,
   int sum_row0;         //   from row sum_row0 on, two rows per tile of the launch along M
   int a_rows, w_rows;   // products of the gated MLP: 1 = the operand stands [K, rows], lda / ldw apart (ldw is always set there)
+  const float *row_scales, *col_scales, *col_bias;   // EPI_INT8: [M], [N], [N] or nullptr
   int name_tag;         // bf16 path, EPI_RESIDUAL: 1 = the second MLP GEMM (a kernel name of its own in
                         //   profiles; the code is the same)
 };

@@ -36,6 +36,7 @@ namespace epd {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
 
 #define EPD_GPTR(p) ((const __attribute__((address_space(1))) void*)(p))
 #define EPD_LPTR(p) ((__attribute__((address_space(3))) void*)(p))
@@ -137,6 +138,15 @@ __device__ __forceinline__ void keep_channels(const float* p, const float* q, ui
 __device__ __forceinline__ float kept_channel(uint2 high, uint32_t low, int i, int shift) {       // shift: 0 for P, 4 for Q
   const uint32_t h = i < 2 ? high.x : high.y;
   return __uint_as_float((i & 1 ? h & 0xffff0000u : h << 16) | (low >> (8 * i + shift) & 15u) << 12);
+}
+
+// One matrix instruction on 16 rows of 16 bytes of K each a lane group: 32 values in bf16, or 64 in 8 bits, whose int32 sums are held as the
+// bits of floats, so that both run the same loops.
+template <bool I8> __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  if constexpr (I8)
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), __builtin_bit_cast(i32x4, c), 0, 0, 0));
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
 enum OutKind : int { OUT_BF16 = 0, OUT_F32 = 1 };
@@ -377,6 +387,8 @@ template <int NW> __device__ __forceinline__ void read_frags_tr_both(bf16x8* f, 
 // whole lines as before, eight k each, and fragments are read transposed (read_frags_tr).  A wave serves 32 lanes at
 // a time, eight k (0 .. 3 and 8 .. 11) of 32 bytes each, whose 128-byte rows fall on two halves of the banks: the 32-byte pieces of row k
 // are swapped by bits 1 and 3 of k, so that the eight lie in different banks.
+// EPI_INT8, EPI_INT8_SUMS: a row's bytes are moved as those of bf16 are, so K, lda and ldw count pairs of values; only the matrix
+// instruction and the epilogue are others.  The scales and the bias of a tile's columns lie in LDS behind the rows' scales.
 template <class T, int EPI, int OUT, bool VMODE, bool GATHER, bool FAST, bool CLAMP = false, int KROWS = 0>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const int n0, char* const lds) {
   constexpr int BM = T::BM, BN = T::BN, BK = T::BK, NT = T::NT, WM = T::WM, WN = T::WN, TM = T::TM, TN = T::TN;
@@ -390,6 +402,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // wave-uniform: keeps LDS bases scalar
   const int wm = wave / T::WAVES_N, wn = wave % T::WAVES_N;
   const int l16 = lane & 15, g4 = lane >> 4;
+  constexpr bool I8 = EPI == EPI_INT8 || EPI == EPI_INT8_SUMS;
 
   const char* zeros = (const char*)g.zeros;
   const int kcw = GATHER ? g.K / g.gather_n : g.K;
@@ -555,12 +568,20 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
   } else if (CONSUMER) {
     for (int r = tid; r < BM; r += NT) row_scale[r] = 1.0f;
   }
+  [[maybe_unused]] float* const col_scale = row_scale + BM;            // EPI_INT8: scales, then bias
+  if constexpr (EPI == EPI_INT8) {
+    for (int r = tid; r < BM; r += NT) row_scale[r] = g.row_scales[min(m0 + r, g.M - 1)];
+    for (int c = tid; c < BN; c += NT) {
+      col_scale[c] = g.col_scales[min(n0 + c, g.N - 1)];
+      col_scale[BN + c] = g.col_bias ? g.col_bias[min(n0 + c, g.N - 1)] : 0.f;
+    }
+  }
 
   // The epilogue's bias values (4 columns per 16-column block of the lane) are fetched here, so that their
   // latency passes in the shadow of the main loop; the largest tile has no registers to spare for them
   // and fetches them in the epilogue
   constexpr int TN16 = T::TN16;
-  constexpr bool BIAS_USED = !VMODE && EPI != EPI_RESIDUAL && EPI != EPI_DGATED && OUT == OUT_BF16, BIAS_PRE = BIAS_USED && BM * BN <= 256 * 256;
+  constexpr bool BIAS_USED = !VMODE && !I8 && EPI != EPI_RESIDUAL && EPI != EPI_DGATED && OUT == OUT_BF16, BIAS_PRE = BIAS_USED && BM * BN <= 256 * 256;
   [[maybe_unused]] uint2 bb[TN16];
   auto load_bias = [&]() {
 #pragma unroll
@@ -646,8 +667,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
       constexpr int t = VMODE ? i / TN16 : i % AP, w = VMODE ? i % TN16 : i / AP;
       constexpr int a16 = p * AP + t;
       f32x4& c = acc[a16 >> 1][w >> 1][(a16 & 1) * 2 + (w & 1)];
-      if constexpr (VMODE) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[sl & 1][t], fw[ks][w], c, 0, 0, 0);
-      else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[ks][w], fa[sl & 1][t], c, 0, 0, 0);
+      if constexpr (VMODE) c = mfma16<I8>(fa[sl & 1][t], fw[ks][w], c);
+      else c = mfma16<I8>(fw[ks][w], fa[sl & 1][t], c);
       if constexpr (decltype(REFILL)::value && nl > 0) {
         constexpr int b0 = l0 + nl * i / MPS, b1 = l0 + nl * (i + 1) / MPS;
         if constexpr (b1 > b0) {
@@ -904,8 +925,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
       static_for<NM>([&](auto I) {
         constexpr int i = decltype(I)::value, ks = i / (NW * NA), w = i / NA % NW, x = i % NA, a16 = p * PP::NA0 + x;
         f32x4& c = acc[a16 >> 1][w >> 1][(a16 & 1) * 2 + (w & 1)];
-        if constexpr (VMODE) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[2 * x + ks], pw[2 * w + ks], c, 0, 0, 0);
-        else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw[2 * w + ks], pa[2 * x + ks], c, 0, 0, 0);
+        if constexpr (VMODE) c = mfma16<I8>(pa[2 * x + ks], pw[2 * w + ks], c);
+        else c = mfma16<I8>(pw[2 * w + ks], pa[2 * x + ks], c);
         // units refilled in this phase, their loads spread over the instructions
         static_for<PP::NU>([&](auto U) {
           constexpr int u = decltype(U)::value, ahead = S + (p - PP::q(u) < 0 ? -1 : 0);
@@ -1231,10 +1252,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
       const __amdgpu_buffer_rsrc_t out_rows = row_window(out0 + (size_t)(m0 + wm * WM) * out_pitch, out0 ? (size_t)rows_left * out_pitch : 0);
       float* const part = (float*)(lds + T::WAVES_M * T::WAVES_N * 16 * SROW);   // [WAVES_N][BM] sums of squares per wave
       uint2 br = make_uint2(0u, 0u);
-      if (g.bias && n < g.N) br = *(const uint2*)((const uint16_t*)g.bias + n);
+      if (!I8 && g.bias && n < g.N) br = *(const uint2*)((const uint16_t*)g.bias + n);
       const float b0 = bf16_bits_to_float(br.x & 0xffff), b1 = bf16_bits_to_float(br.x >> 16);
       const float b2 = bf16_bits_to_float(br.y & 0xffff), b3 = bf16_bits_to_float(br.y >> 16);
       [[maybe_unused]] float ss = 0.f;
+      [[maybe_unused]] float4 cs, cb;
+      if constexpr (EPI == EPI_INT8) {
+        cs = *(const float4*)(col_scale + wn * WN + (lane % FC) * 4);
+        cb = *(const float4*)(col_scale + BN + wn * WN + (lane % FC) * 4);
+      }
       if constexpr (HAS_AUX && !PREF) {
 #pragma unroll
         for (int b = 0; b < AUX; ++b) load_aux(b);
@@ -1251,6 +1277,16 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
         for (int w = 0; w < TN16; ++w) {
           const int c = b * TN16 + w;                  // rows c * FR + lane / FC of the wave's tile
           const float4 e = *(const float4*)(stg + schunk(w * FR + lane / FC, lane % FC));
+          if constexpr (I8) {
+            float4 v = e;
+            if constexpr (EPI == EPI_INT8) {
+              const i32x4 i = __builtin_bit_cast(i32x4, e);
+              const float rs = row_scale[wm * WM + c * FR + lane / FC];
+              v = make_float4(fmaf((float)i[0] * rs, cs.x, cb.x), fmaf((float)i[1] * rs, cs.y, cb.y), fmaf((float)i[2] * rs, cs.z, cb.z), fmaf((float)i[3] * rs, cs.w, cb.w));
+            }
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), out_rows, out_off + (uint32_t)(c * FR) * out_pitch, 0, 0);
+            continue;
+          }
           const float v0 = e.x + b0, v1 = e.y + b1, v2 = e.z + b2, v3 = e.w + b3;
           if constexpr (EPI == EPI_RESIDUAL) {
             float4 x = aux[b % AUX][w];
@@ -1291,8 +1327,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
       const uint32_t out_pitch = (uint32_t)g.ldo * 2u, out_off = ns < g.N ? (uint32_t)(lane / CH) * out_pitch + (uint32_t)ns * 2u : OUTSIDE;
       const __amdgpu_buffer_rsrc_t out_rows = row_window(outp + (size_t)(m0 + wm * WM) * g.ldo, (size_t)rows_left * out_pitch);
       float bias[TN16][4], qs[TN16];
+      [[maybe_unused]] float4 cs[TN16];                  // EPI_INT8: scales of the lane's columns
 #pragma unroll
       for (int w = 0; w < TN16; ++w) {
+        if constexpr (I8) {
+          cs[w] = *(const float4*)(col_scale + wn * WN + w * 16 + g4 * 4);
+          const float4 b = *(const float4*)(col_scale + BN + wn * WN + w * 16 + g4 * 4);
+          bias[w][0] = b.x; bias[w][1] = b.y; bias[w][2] = b.z; bias[w][3] = b.w;
+          continue;
+        }
         bias[w][0] = bf16_bits_to_float(bb[w].x & 0xffff); bias[w][1] = bf16_bits_to_float(bb[w].x >> 16);
         bias[w][2] = bf16_bits_to_float(bb[w].y & 0xffff); bias[w][3] = bf16_bits_to_float(bb[w].y >> 16);
         // the softmax scale (in log2 units) rides on Q: one rounding of q * scale instead of
@@ -1340,11 +1383,18 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const int m0, const
 #pragma unroll
         for (int b = 0; b < TM16; ++b) {
           const int ml = wm * WM + b * 16 + l16;
-          const float rs = CONSUMER ? row_scale[ml] : 1.0f;
+          const float rs = CONSUMER || I8 ? row_scale[ml] : 1.0f;
 #pragma unroll
           for (int w = 0; w < TN16; ++w) {
             const f32x4 a = acc[b >> 1][w >> 1][(b & 1) * 2 + (w & 1)];
-            float v0 = fmaf(a[0], rs, bias[w][0]), v1 = fmaf(a[1], rs, bias[w][1]), v2 = fmaf(a[2], rs, bias[w][2]), v3 = fmaf(a[3], rs, bias[w][3]);
+            float v0, v1, v2, v3;
+            if constexpr (I8) {
+              const i32x4 i = __builtin_bit_cast(i32x4, a);
+              v0 = fmaf((float)i[0] * rs, cs[w].x, bias[w][0]); v1 = fmaf((float)i[1] * rs, cs[w].y, bias[w][1]);
+              v2 = fmaf((float)i[2] * rs, cs[w].z, bias[w][2]); v3 = fmaf((float)i[3] * rs, cs[w].w, bias[w][3]);
+            } else {
+              v0 = fmaf(a[0], rs, bias[w][0]); v1 = fmaf(a[1], rs, bias[w][1]); v2 = fmaf(a[2], rs, bias[w][2]); v3 = fmaf(a[3], rs, bias[w][3]);
+            }
             if constexpr (EPI == EPI_GELU) {
               if constexpr (variant == 0) { v0 = gelu_erf_fast(v0); v1 = gelu_erf_fast(v1); v2 = gelu_erf_fast(v2); v3 = gelu_erf_fast(v3); }
               else { v0 = gelu_tanh_fast(v0); v1 = gelu_tanh_fast(v1); v2 = gelu_tanh_fast(v2); v3 = gelu_tanh_fast(v3); }
