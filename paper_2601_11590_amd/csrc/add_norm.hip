@@ -301,9 +301,10 @@ template <class F> hipError_t by_width(int D, F&& f) {
 template <typename T, typename R, bool NORM> hipError_t launch_norm_rows(const NormArgs& all, hipStream_t s) {
   return by_width(all.D, [&](auto TPR, auto U) {
     constexpr int tpr = decltype(TPR)::value, rpb = tpr < 256 ? 256 / tpr : 1;
-    for (int64_t r = 0; r < all.rows; r += (int64_t)kMaxGrid * rpb) {
+    constexpr int64_t most = (int64_t)kMaxGrid * rpb / (tpr > 512 ? 2 : 1);      // rows of a launch
+    for (int64_t r = 0; r < all.rows; r += most) {
       NormArgs a = all;
-      a.rows = (int)std::min<int64_t>(all.rows - r, (int64_t)kMaxGrid * rpb);
+      a.rows = (int)std::min<int64_t>(all.rows - r, most);
       if (a.x) a.x = (const T*)a.x + r * a.ld_x;
       if (a.r) a.r = (const R*)a.r + r * a.ld_r;
       if (a.sum) a.sum = (R*)a.sum + r * a.ld_sum;

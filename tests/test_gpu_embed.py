@@ -68,6 +68,17 @@ def test_forward_and_gradients(dtype, out, T, V, D, R):
         assert torch.equal(op.backward(ids, dout, num_rows=R, want=[name])[name], grads[name])
 
 
+# (beyond 4096 pieces of 2048 elements a wave takes such a piece, not a quarter of it)
+@pytest.mark.parametrize("dtype,out", TYPES)
+@pytest.mark.parametrize("T,D", [(4100, 520), (2050, 2056), (4096, 2047)])
+def test_rows_of_many_tokens(dtype, out, T, D):
+    gen, V, R = generator(T + D), 100, 50
+    ids = some_ids(gen, T, V, R)
+    table, rows = randn(gen, V, D, dtype=KINDS[dtype]), randn(gen, R, D, dtype=KINDS[dtype])
+    op = B.Embedding(dtype, V, D, out=out, scale=0.3, max_tokens=T)
+    check_forward(op.forward(table, ids, rows), table, rows, ids, op.cfg.scale, V, R)
+
+
 # lists of 8192 that are merged: two, the eighth full, one more than eight; tables of one to four digits of nine bits
 @pytest.mark.parametrize("T,V,D,hot", [(8192, 500, 8, 0.0), (8193, 40000, 8, 0.9), (16384, 131072, 16, 0.1), (16385, 131072, 8, 0.5), (65536, 70, 8, 0.2),
                                        (65537, 262143, 8, 0.3), (150001, 1 << 20, 4, 0.99)])

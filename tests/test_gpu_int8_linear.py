@@ -29,9 +29,14 @@ SIZES = [(1, 16, 8), (1, 3200, 136), (1, 2064, 4096), (1, 1040, 72), (2, 32, 16)
          (63, 1152, 200), (64, 2048, 512), (65, 112, 320), (100, 640, 1032), (128, 128, 256), (129, 1136, 264), (255, 64, 520), (257, 1152, 304), (300, 4112, 64),
          (513, 528, 776), (640, 16, 640), (1000, 80, 1000), (2049, 336, 264)]
 
+# a size for every tile, whole, cut behind its whole rounds, and in parts (test_entry_host_logic.py counts them)
+PLANS = [(1, 5008, 8), (2, 16, 8328), (65, 6272, 3736), (1340, 896, 14648), (4256, 8416, 72), (5697, 14816, 392), (6160, 544, 4208), (10362, 7360, 72),
+         (16779, 5200, 80), (18230, 8336, 136), (19241, 144, 680), (25656, 16, 648), (28671, 96, 432), (32410, 3952, 648), (32554, 992, 160), (33870, 7072, 168),
+         (36136, 16, 424), (38188, 16, 8), (44024, 3008, 312), (45731, 1840, 88)]
+
 
 @pytest.mark.parametrize("out", ["bf16", "f32"])
-@pytest.mark.parametrize("T,K,N", SIZES)
+@pytest.mark.parametrize("T,K,N", SIZES + PLANS)
 def test_product(out, T, K, N):
     for bias, full in ((False, False), (True, True)):
         x, xs, w = operands(T, K, N, full=full)
