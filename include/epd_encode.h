@@ -395,7 +395,7 @@ typedef struct {
   int32_t out_dtype;    /* epd_dtype of out and dout: dtype, or EPD_F32                              */
   int32_t vocab;        /* rows of the table, 1 .. 2^30                                              */
   int32_t hidden;       /* 1 .. 65536                                                                */
-  int32_t max_tokens;   /* largest `tokens` of any call, 1 .. 2^24                                   */
+  int32_t max_tokens;   /* largest `tokens` of any call, 1 .. 2^24; times hidden <= 2^38             */
   float scale;          /* finite                                                                    */
 } epd_embed_cfg;
 

@@ -6,12 +6,12 @@
 //   grad[key] = sum of dout over the tokens of that key (* scale)
 // The tokens are sorted by key, which puts those of a row side by side; blocks then add runs of equal keys.  Nothing is added
 // atomically, so a gradient's bits depend on the ids alone.
-//   1. sort_kernel: up to 8192 tokens a block, sorted in LDS by their keys' digits, from the lowest up, keeping the order of equal ones;
+//   1. sort_kernel: up to 4096 tokens a block, sorted in LDS by their keys' digits, from the lowest up, keeping the order of equal ones;
 //      meanwhile the other blocks clear the gradients, which is most of what is written where the table is large
-//   2. merge_kernel (more than 8192 tokens): eight sorted lists into one at a time: an element's place is its own plus the numbers of
+//   2. merge_kernel (more than 4096 tokens): eight sorted lists into one at a time: an element's place is its own plus the numbers of
 //      smaller ones in the other lists
-//   3. sums_kernel: pieces of 16 or 32 sorted tokens; runs within a piece are written, the ends of others left as partial sums
-//   4. runs_kernel: runs over several pieces, so that a token that takes every other place costs no more than others
+//   3. sums_kernel: pieces of 8 to 32 sorted tokens; runs within a piece and the next are written, longer ones left as partial sums
+//   4. runs_kernel: those, so that a token that takes every other place costs no more than others
 #include "op_error.h"
 #include "rows.h"
 
@@ -23,6 +23,7 @@ namespace epd {
 namespace {
 
 constexpr int kEmbedDim = 65536, kEmbedRows = 1 << 30, kEmbedTokens = 1 << 24;
+constexpr int64_t kEmbedElements = 1ll << 38;              // of all tokens: a launch has fewer than 2^32 threads
 
 struct EmbedArgs {
   const void *table, *rows;
@@ -63,7 +64,7 @@ template <typename T, typename O, int U> __global__ __launch_bounds__(256) void 
 }
 
 // ------------------------------------------------------------------------------ sorted tokens
-constexpr int kSortList = 8192, kSortWaves = 16, kMaxDigit = 9;
+constexpr int kSortList = 4096, kSortWaves = 16, kMaxDigit = 9;
 
 struct SortArgs {
   const int32_t* ids;
@@ -72,6 +73,7 @@ struct SortArgs {
   uint32_t none;                     // the key of tokens without a gradient, behind all others: vocab + num_rows
   int passes, bits;                  // digits of a key, and their bits
   int sort_blocks;
+  uint32_t* counts;                  // two counters to clear
   void* clear[2];                    // gradients to clear, and their 16-byte pieces and bytes behind these
   int64_t pieces[2];
   int tail[2];
@@ -93,6 +95,7 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs a) {
     }
     return;
   }
+  if (blockIdx.x == 0 && tid < 2) a.counts[tid] = 0;
   const int first = (int)blockIdx.x * kSortList, n = min(kSortList, a.tokens - first);
   const int rounds = (n + 1023) / 1024, base = wave * rounds * 64;       // a wave's elements: side by side, 64 a round
   for (int r = 0; r < rounds; ++r) {
@@ -107,12 +110,15 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs a) {
     ats[0][i] = (uint16_t)i;
   }
   __syncthreads();
-  const int digits = 1 << a.bits, per = digits * kSortWaves / 1024;      // counters per thread in the scan (bits >= 6: one or more)
+  const int digits = 1 << a.bits;
   for (int p = 0; p < a.passes; ++p) {
     const int from = p & 1, shift = p * a.bits;
     for (int c = tid; c < digits * kSortWaves; c += 1024) count[c] = 0;
     __syncthreads();
-    uint32_t place[kSortList / 1024];                      // among the wave's elements of the same digit
+    // place among the wave's elements of the same digit.  The lanes of a digit find each other by ballots; LDS takes a wave's accesses in
+    // order, so all of them have read its counter before the first of them writes it
+    uint32_t place[kSortList / 1024], digit[kSortList / 1024];
+    uint32_t* const mine = count + wave * digits;
 #pragma unroll
     for (int r = 0; r < kSortList / 1024; ++r) {
       if (r >= rounds) break;
@@ -122,31 +128,39 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs a) {
         const uint64_t set = __ballot(d >> b & 1);
         same &= d >> b & 1 ? set : ~set;
       }
-      uint32_t* const c = &count[d * kSortWaves + wave];
-      const uint32_t before = *(volatile uint32_t*)c;
+      const uint32_t before = mine[d];
+      asm volatile("" ::: "memory");
+      digit[r] = d;
       place[r] = before + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-      // (LDS takes a wave's accesses in order: all lanes have read before the first of each digit writes)
-      if (__ffsll((unsigned long long)same) - 1 == lane) *(volatile uint32_t*)c = before + (uint32_t)__popcll(same);
+      if (__ffsll((unsigned long long)same) - 1 == lane) mine[d] = before + (uint32_t)__popcll(same);
+      asm volatile("" ::: "memory");
     }
     __syncthreads();
-    // exclusive sums over [digit][wave]
-    uint32_t mine = 0;
-    for (int j = 0; j < per; ++j) mine += count[tid * per + j];
-    uint32_t upto = mine;
+    // exclusive sums, digits first, waves of a digit after that: a thread per digit
+    uint32_t of[kSortWaves], all = 0;
+    if (tid < digits) {
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) { of[w] = all; all += count[w * digits + tid]; }
+    }
+    uint32_t upto = all;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) { const uint32_t v = __shfl_up(upto, o); if (lane >= o) upto += v; }
     if (lane == 63) wave_sum[wave] = upto;
     __syncthreads();
-    uint32_t sum = upto - mine;
-    for (int w = 0; w < wave; ++w) sum += wave_sum[w];
-    for (int j = 0; j < per; ++j) { const uint32_t c = count[tid * per + j]; count[tid * per + j] = sum; sum += c; }
+    if (tid < digits) {
+      uint32_t sum = upto - all;
+#pragma unroll
+      for (int w = 0; w < (1 << kMaxDigit) / 64; ++w) if (w < wave) sum += wave_sum[w];
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) count[w * digits + tid] = sum + of[w];
+    }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortList / 1024; ++r) {
       if (r >= rounds) break;
       const int i = base + r * 64 + lane;
-      const uint32_t k = keys[from][i], to = count[(k >> shift & (digits - 1)) * kSortWaves + wave] + place[r];
-      keys[from ^ 1][to] = k;
+      const uint32_t to = mine[digit[r]] + place[r];
+      keys[from ^ 1][to] = keys[from][i];
       ats[from ^ 1][to] = ats[from][i];
     }
     __syncthreads();
@@ -158,14 +172,22 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs a) {
   }
 }
 
-// Groups of up to eight sorted lists of `len` into one each; lists stand in the order of their tokens, so of equal keys those of an
-// earlier list come first.
-constexpr int kMergeLists = 8;
-struct MergeArgs { const uint32_t *key, *at; uint32_t *key_out, *at_out; int tokens, len, steps; };      // steps: 2^steps > len
+// Groups of up to eight sorted lists of `len` (a multiple of 4096) into one each; lists stand in the order of their tokens, so of equal keys
+// those of an earlier list come first.  A thread per element; every 1/128th key of the lists comes to LDS, so that only the last steps of
+// its searches wait for memory.
+constexpr int kMergeLists = 8, kSamples = 128;
+struct MergeArgs { const uint32_t *key, *at; uint32_t *key_out, *at_out; int tokens, len; };
 __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
+  __shared__ uint32_t sample[kMergeLists][kSamples];
+  const int64_t i0 = (int64_t)blockIdx.x * 256;            // a block's elements are of one list
+  const int list = (int)(i0 / a.len), first = list / kMergeLists * kMergeLists, stride = a.len / kSamples;
+  for (int s = threadIdx.x; s < kMergeLists * kSamples; s += 256) {
+    const int64_t p = (int64_t)(first + s / kSamples) * a.len + (int64_t)(s % kSamples + 1) * stride - 1;
+    sample[s / kSamples][s % kSamples] = p < a.tokens ? a.key[p] : 0xffffffffu;
+  }
+  __syncthreads();
+  const int64_t i = i0 + threadIdx.x;
   if (i >= a.tokens) return;
-  const int list = i / a.len, first = list / kMergeLists * kMergeLists;
   const uint32_t k = a.key[i];
   int below[kMergeLists], size[kMergeLists];
 #pragma unroll
@@ -174,18 +196,26 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a) {
     below[j] = 0;
     size[j] = first + j == list ? 0 : (int)max((int64_t)0, min((int64_t)a.len, a.tokens - start));
   }
-  for (int s = a.steps - 1; s >= 0; --s) {
+  auto under = [&](int j, uint32_t key) { return first + j < list ? key <= k : key < k; };
+#pragma unroll
+  for (int s = kSamples; s > 0; s /= 2)                    // in samples
+#pragma unroll
+    for (int j = 0; j < kMergeLists; ++j) {
+      const int next = below[j] + s;
+      if (next * stride <= size[j] && under(j, sample[j][next - 1])) below[j] = next;
+    }
+#pragma unroll
+  for (int j = 0; j < kMergeLists; ++j) below[j] *= stride;
+  for (int s = stride / 2; s > 0; s /= 2) {
     uint32_t probe[kMergeLists];
 #pragma unroll
     for (int j = 0; j < kMergeLists; ++j) {
-      const int next = below[j] + (1 << s);
+      const int next = below[j] + s;
       probe[j] = next <= size[j] ? a.key[(int64_t)(first + j) * a.len + next - 1] : 0xffffffffu;
     }
 #pragma unroll
-    for (int j = 0; j < kMergeLists; ++j) {
-      const int next = below[j] + (1 << s);
-      if (next <= size[j] && (first + j < list ? probe[j] <= k : probe[j] < k)) below[j] = next;
-    }
+    for (int j = 0; j < kMergeLists; ++j)
+      if (below[j] + s <= size[j] && under(j, probe[j])) below[j] += s;
   }
   int64_t to = (int64_t)first * a.len + (i - (int64_t)list * a.len);
 #pragma unroll
@@ -195,10 +225,20 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a) {
 }
 
 // ------------------------------------------------------------------------------ sums of runs
-constexpr int kPiece = 32, kFewPieces = 1024;      // tokens of a piece; half of that while the pieces are fewer than the second
-int piece_of(int tokens) { return tokens <= kFewPieces * kPiece / 2 ? kPiece / 2 : kPiece; }
+constexpr int64_t kClearAll = 48 << 20;              // bytes of the tokens' rows up to which all rows are cleared first
+constexpr int kPiece = 32, kLeastPiece = 8, kFewPieces = 1024;      // tokens of a piece, fewer while that gives no more pieces than this
+int piece_of(int tokens) {
+  int piece = kLeastPiece;
+  while (piece < kPiece && tokens > kFewPieces * piece) piece *= 2;
+  return piece;
+}
 int pieces_of(int tokens) { return (tokens + piece_of(tokens) - 1) / piece_of(tokens); }
-int most_pieces(int max_tokens) { return std::max(pieces_of(max_tokens), pieces_of(std::min(max_tokens, kFewPieces * kPiece / 2))); }
+int most_pieces(int max_tokens) { return std::max(pieces_of(max_tokens), std::min(kFewPieces, (max_tokens + kLeastPiece - 1) / kLeastPiece)); }
+
+// Runs of kManyParts pieces or more stand from the end of the list on.  Their order there is that in which blocks came by; no sum depends on it.
+constexpr int kManyParts = 33;
+struct Run { uint32_t key; int piece, parts, pad; };
+struct Runs { uint32_t count[4]; Run list[1]; };
 
 struct SumsArgs {
   const uint32_t *key, *at;
@@ -209,6 +249,9 @@ struct SumsArgs {
   int tokens, D, vocab, piece;
   uint32_t none;
   float scale;
+  Runs* runs;
+  int most_runs;                     // that the list holds
+  int slices, sum_blocks, clear_blocks, clear_rows;        // sums_kernel: blocks per piece, of sums, and those that clear `clear_rows` rows a wave
 };
 
 template <typename T> __device__ __forceinline__ T* row_of(const SumsArgs& a, uint32_t key, float& scale) {
@@ -220,45 +263,106 @@ template <typename T> __device__ __forceinline__ T* row_of(const SumsArgs& a, ui
 // (tokens whose gradient is not wanted keep their places, so that the others' sums have the same bits in every call)
 __device__ __forceinline__ bool wanted(const SumsArgs& a, uint32_t key) { return key < (uint32_t)a.vocab ? a.table != nullptr : key < a.none && a.rows != nullptr; }
 
-template <typename T, typename O> __global__ __launch_bounds__(256) void sums_kernel(SumsArgs a) {
-  __shared__ uint32_t key[kPiece + 2], at[kPiece];         // key[0]: that of the token ahead
-  const int p0 = blockIdx.x * a.piece, n = min(a.piece, a.tokens - p0);
-  if ((int)threadIdx.x < n + 2) {
-    const int p = p0 - 1 + (int)threadIdx.x;
-    key[threadIdx.x] = p >= 0 && p < a.tokens ? a.key[p] : 0xffffffffu;
-    if (threadIdx.x < n) at[threadIdx.x] = a.at[p0 + (int)threadIdx.x];
+// Rows of no token, by a wave, `clear_rows` (up to 64) at a time: its lanes look for as many rows among the sorted keys.
+template <typename T> __device__ __forceinline__ void clear_rows(const SumsArgs& a, int64_t wave) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t r0 = wave * a.clear_rows; r0 < (int64_t)a.none; r0 += 4ll * a.clear_blocks * a.clear_rows) {
+    const uint32_t key = (uint32_t)min(r0 + lane, (int64_t)a.none);
+    int lo = 0, hi = a.tokens;                             // the first token of this key or a later one
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (a.key[mid] < key) lo = mid + 1; else hi = mid;
+    }
+    uint64_t absent = __ballot(lane < a.clear_rows && key < a.none && wanted(a, key) && (lo >= a.tokens || a.key[min(lo, a.tokens - 1)] != key));
+    float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, scale;
+    for (; absent; absent &= absent - 1) {
+      T* const row = row_of<T>(a, (uint32_t)(r0 + __ffsll((unsigned long long)absent) - 1), scale);
+      for (int e = lane * 8; e < a.D; e += 512) store8(row + e, a.D - e, zero);
+    }
   }
+}
+
+// A block's runs are those that start in its piece.  One that ends in the next piece is finished here, beyond the piece's end, and
+// passed over there; one that goes on further is `long`: every block adds its own part, for runs_kernel.
+//   TINY: rows of fewer than eight elements.  Otherwise the last eight of a row stand in for the ones that would run past it, which two
+// threads then write alike, so that no load waits behind a branch (embed-grad of 32 768 x 3200 with branches: 190 us).
+template <typename T, typename O, bool TINY> __global__ __launch_bounds__(256) void sums_kernel(SumsArgs a) {
+  __shared__ uint32_t keys[3 * kPiece + 2], at[2 * kPiece];            // from the token ahead of the piece before on
+  // blocks that clear stand evenly between the others, so that reads and writes go on together
+  const int64_t all = gridDim.x;
+  const int clear = (int)((int64_t)blockIdx.x * a.clear_blocks / all);
+  if ((int)(((int64_t)blockIdx.x + 1) * a.clear_blocks / all) > clear) {
+    clear_rows<T>(a, (int64_t)clear * 4 + (threadIdx.x >> 6));
+    return;
+  }
+  const int block = (int)blockIdx.x - clear, piece = block / a.slices, slice = block - piece * a.slices;
+  const int S = a.piece, p0 = piece * S, mine = min(S, a.tokens - p0), more = min(2 * S, a.tokens - p0);
+  for (int i = threadIdx.x; i < 3 * S + 2; i += 256) {
+    const int p = p0 - S - 1 + i;
+    keys[i] = p >= 0 && p < a.tokens ? a.key[p] : 0xffffffffu;
+  }
+  if ((int)threadIdx.x < more) at[threadIdx.x] = a.at[p0 + (int)threadIdx.x];
   __syncthreads();
-  const int e = ((int)blockIdx.y * 256 + (int)threadIdx.x) * 8, left = a.D - e;
-  if (left <= 0) return;
+  const uint32_t* const key = keys + S + 1;                // of the piece's first token; [-S - 1, 2 S] are there
+  const int lane = threadIdx.x & 63;
+  const uint32_t here = lane < 2 * S ? key[lane] : 0xffffffffu;
+  const bool begun = key[-1] == key[0], goes_on = key[mine - 1] == key[mine], whole = key[mine - 1] == key[0];
+  // a run that started before: a part of a long one, or finished by the block before
+  bool from_before = begun && (key[-S - 1] == key[0] || (whole && goes_on));
+  const int first = begun && !from_before ? min(mine, __ffsll((unsigned long long)~__ballot(here == key[0])) - 1) : 0;
+  // one past the last token to add
+  int last = mine;
+  if (goes_on && !(begun && whole) && key[2 * S] != key[mine - 1]) last += __ffsll((unsigned long long)~(__ballot(here == key[mine - 1]) >> mine)) - 1;
+  // a long run that starts here is listed by one wave, which finds its last piece: every lane looks at one of 64 places
+  if (goes_on && !(begun && whole) && key[2 * S] == key[mine - 1] && slice == 0 && threadIdx.x < 64) {
+    const uint32_t k = key[mine - 1];
+    const int pieces = (a.tokens + S - 1) / S;
+    int to = piece + 2, end = pieces;
+    while (end - to > 1) {
+      const int step = (end - to + 63) / 64, p = to + lane * step;
+      to += (__popcll(__ballot(p < end && a.key[(int64_t)min(p, end - 1) * S] == k)) - 1) * step;
+      end = min(end, to + step);
+    }
+    if (lane == 0 && wanted(a, k)) {
+      const bool many = to - piece + 1 >= kManyParts;
+      const int i = (int)atomicAdd(&a.runs->count[many], 1u);
+      a.runs->list[many ? a.most_runs - 1 - i : i] = Run{k, piece, to - piece + 1, 0};
+    }
+  }
+  // (the ballots above need every lane)
+  if (first >= last || (!a.table && key[last - 1] < (uint32_t)a.vocab) || (!a.rows && key[first] >= (uint32_t)a.vocab)) return;
+  int e = (slice * 256 + (int)threadIdx.x) * 8;
+  if (e >= a.D) return;
+  const int left = TINY ? a.D : 8;
+  if constexpr (!TINY) e = min(e, a.D - 8);
   float sum[8];
-  bool from_before = key[0] == key[1];
 #pragma unroll
   for (int i = 0; i < 8; ++i) sum[i] = 0.f;
   constexpr int BATCH = 8;
-  for (int b = 0; b < n; b += BATCH) {
+  for (int b = first; b < last; b += BATCH) {
+    if (key[b] >= a.none) return;                          // and all behind it
     float v[BATCH][8];
 #pragma unroll
-    for (int j = 0; j < BATCH; ++j)
-      if (b + j < n && wanted(a, key[b + j + 1])) load8((const O*)a.dout + (int64_t)at[b + j] * a.ld + e, left, v[j]);
+    for (int j = 0; j < BATCH; ++j) load8((const O*)a.dout + (int64_t)at[min(b + j, last - 1)] * a.ld + e, left, v[j]);
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
-      if (b + j >= n) break;
-      const uint32_t k = key[b + j + 1];
-      if (k >= a.none) return;                             // and all behind it
-      const bool ends = key[b + j + 2] != k;
-      if (!wanted(a, k)) { from_before = !ends; continue; }
+      if (b + j >= last) break;
+      const uint32_t k = key[b + j];
+      if (k >= a.none) return;
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[i] += v[j][i];
-      if (!ends && b + j + 1 < n) continue;
-      if (ends && !from_before) {
-        float scale;
-        T* const row = row_of<T>(a, k, scale);
+      const bool ends = key[b + j + 1] != k;
+      if (!ends && b + j + 1 < last) continue;
+      if (wanted(a, k)) {
+        if (ends && !from_before) {
+          float scale;
+          T* const row = row_of<T>(a, k, scale);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] *= scale;
-        store8(row + e, left, sum);
-      } else {
-        store8(a.parts + ((int64_t)blockIdx.x * 2 + (from_before ? 0 : 1)) * a.D + e, left, sum);
+          for (int i = 0; i < 8; ++i) sum[i] *= scale;
+          store8(row + e, left, sum);
+        } else {
+          store8(a.parts + ((int64_t)piece * 2 + (from_before ? 0 : 1)) * a.D + e, left, sum);
+        }
       }
       from_before = false;
 #pragma unroll
@@ -267,42 +371,52 @@ template <typename T, typename O> __global__ __launch_bounds__(256) void sums_ke
   }
 }
 
-// Runs that start in piece blockIdx.x and go on: their partial sums, 256 columns a block, sixteen groups of threads in turn.
-template <typename T> __global__ __launch_bounds__(1024) void runs_kernel(SumsArgs a) {
-  __shared__ float part[16][256];
-  const int piece = blockIdx.x;
-  const int64_t next = (int64_t)(piece + 1) * a.piece;     // < tokens
-  const uint32_t k = a.key[next];
-  if (!wanted(a, k) || a.key[next - 1] != k || (piece > 0 && a.key[next - a.piece - 1] == k)) return;
-  int64_t last = next, step = 1;                           // the last token of the run
-  while (last + step < a.tokens && a.key[last + step] == k) { last += step; step *= 2; }
-  for (; step > 0; step /= 2)
-    if (last + step < a.tokens && a.key[last + step] == k) last += step;
-  const int n = (int)(last / a.piece) - piece + 1;
-  const int g = threadIdx.x >> 6, e = (int)blockIdx.y * 256 + (int)(threadIdx.x & 63) * 4;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int p = g; p < n; p += 16) {
-    const float* const from = a.parts + ((int64_t)(piece + p) * 2 + (p ? 0 : 1)) * a.D + e;
-    if (e + 4 <= a.D) {
-      const quad4 u = *(const quad4*)from;
+// Long runs, those over three pieces or more, as sums_kernel listed them: the parts of one, some columns a block, groups of threads in
+// turn.  Most have a few parts: eight groups for 512 columns; from kManyParts on 64 for 64, so that a token that takes most places is spread
+// over the chip (29 500 of 32 768 tokens, 3200 columns: 56 us by eight groups).
+template <typename T, bool TINY> __global__ __launch_bounds__(512) void runs_kernel(SumsArgs a) {
+  __shared__ float part[512 * 8];
+  const int few = (int)a.runs->count[0], many = (int)a.runs->count[1];
+  const int few_cols = (a.D + 511) / 512, many_cols = (a.D + 63) / 64;
+  const int64_t items = (int64_t)few * few_cols + (int64_t)many * many_cols;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const bool is_few = item < (int64_t)few * few_cols;
+    const int64_t i = is_few ? item : item - (int64_t)few * few_cols;
+    const int cols = is_few ? few_cols : many_cols, run = (int)(i / cols), slice = (int)(i - (int64_t)run * cols);
+    const Run r = is_few ? a.runs->list[run] : a.runs->list[a.most_runs - 1 - run];
+    const int lanes = is_few ? 64 : 8, G = 512 / lanes, lane = threadIdx.x & (lanes - 1), g = threadIdx.x / lanes;
+    const int c0 = slice * lanes * 8, at = c0 + lane * 8, e = TINY ? at : min(at, a.D - 8), left = TINY ? a.D - at : 8;      // see sums_kernel
+    float v[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] += u[i];
-    } else {
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if (at < a.D) {
+      constexpr int BATCH = 4;
+      for (int p = g; p < r.parts; p += G * BATCH) {
+        float u[BATCH][8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) if (e + i < a.D) v[i] += from[i];
+        for (int b = 0; b < BATCH; ++b) {
+          const int q = min(p + G * b, r.parts - 1);
+          load8(a.parts + ((int64_t)(r.piece + q) * 2 + (q ? 0 : 1)) * a.D + e, left, u[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += p + G * b < r.parts ? u[b][j] : 0.f;
+      }
+      // (the shifted window of a row's last threads writes the columns that they share alike)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) if (e + j - c0 >= 0 && j < left) part[g * lanes * 8 + e + j - c0] = v[j];
     }
+    __syncthreads();
+    const int c = c0 + (int)threadIdx.x;
+    if ((int)threadIdx.x < lanes * 8 && c < a.D) {
+      float sum = part[threadIdx.x], scale;
+      for (int j = 1; j < G; ++j) sum += part[j * lanes * 8 + threadIdx.x];
+      T* const row = row_of<T>(a, r.key, scale);
+      row[c] = (T)(sum * scale);
+    }
+    __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) part[g][(threadIdx.x & 63) * 4 + i] = v[i];
-  __syncthreads();
-  const int c = (int)blockIdx.y * 256 + (int)threadIdx.x;
-  if (threadIdx.x >= 256 || c >= a.D) return;
-  float sum = part[0][threadIdx.x], scale;
-#pragma unroll
-  for (int i = 1; i < 16; ++i) sum += part[i][threadIdx.x];
-  T* const row = row_of<T>(a, k, scale);
-  row[c] = (T)(sum * scale);
 }
 
 epd_status check_cfg(const char* who, const epd_embed_cfg* c) {
@@ -313,6 +427,7 @@ epd_status check_cfg(const char* who, const epd_embed_cfg* c) {
   if (c->vocab < 1 || c->vocab > kEmbedRows) return op_fail(EPD_ERR_UNSUPPORTED, "%s: vocab %d: 1 .. 2^30", who, c->vocab);
   if (c->hidden < 1 || c->hidden > kEmbedDim) return op_fail(EPD_ERR_UNSUPPORTED, "%s: hidden %d: 1 .. %d", who, c->hidden, kEmbedDim);
   if (c->max_tokens < 1 || c->max_tokens > kEmbedTokens) return op_fail(EPD_ERR_UNSUPPORTED, "%s: max_tokens %d: 1 .. 2^24", who, c->max_tokens);
+  if ((int64_t)c->max_tokens * c->hidden > kEmbedElements) return op_fail(EPD_ERR_UNSUPPORTED, "%s: max_tokens * hidden %lld: up to 2^38", who, (long long)c->max_tokens * c->hidden);
   if (!std::isfinite(c->scale)) return op_fail(EPD_ERR_INVALID_ARG, "%s: scale must be finite", who);
   return EPD_OK;
 }
@@ -325,13 +440,15 @@ epd_status check_call(const char* who, const epd_embed_cfg* c, int32_t num_rows,
   return EPD_OK;
 }
 
-struct EmbedLayout { size_t list, parts, total; };         // bytes: key and at, twice, and the partial sums
+struct EmbedLayout { size_t list, parts, runs, total; };   // bytes: key and at, twice, the partial sums, and the long runs
+int most_runs(int pieces) { return pieces / 2 + 1; }       // a long run covers the piece behind its first one
 EmbedLayout embed_layout(const epd_embed_cfg& c) {
   EmbedLayout L;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   L.list = up((size_t)c.max_tokens * 4);
   L.parts = 4 * L.list;
-  L.total = up(L.parts + (size_t)most_pieces(c.max_tokens) * 2 * c.hidden * 4);
+  L.runs = up(L.parts + (size_t)most_pieces(c.max_tokens) * 2 * c.hidden * 4);
+  L.total = up(L.runs + sizeof(Runs) + (size_t)most_runs(most_pieces(c.max_tokens)) * sizeof(Run));
   return L;
 }
 
@@ -393,6 +510,8 @@ epd_status epd_embed_backward(const epd_embed_cfg* cfg, const int32_t* ids, int3
   hipStream_t st = (hipStream_t)stream;
 
   SortArgs s{};
+  Runs* const runs = (Runs*)(ws + L.runs);
+  s.counts = runs->count;
   s.ids = ids; s.key = key; s.at = at; s.tokens = tokens; s.vocab = c.vocab; s.num_rows = num_rows;
   s.none = (uint32_t)c.vocab + (uint32_t)num_rows;
   int bits = 1;
@@ -401,15 +520,19 @@ epd_status epd_embed_backward(const epd_embed_cfg* cfg, const int32_t* ids, int3
   s.bits = std::max(6, (bits + s.passes - 1) / s.passes);
   s.sort_blocks = (tokens + kSortList - 1) / kSortList;
   auto clears = [&](int j, void* p, int64_t n) { if (p) { s.clear[j] = p; s.pieces[j] = n * es / 16; s.tail[j] = (int)(n * es % 16); } };
-  clears(0, dtable, (int64_t)c.vocab * c.hidden);
-  clears(1, drows, (int64_t)num_rows * c.hidden);
-  const int clear_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(1024, (s.pieces[0] + s.pieces[1]) / 8192));
+  // Which launch clears the gradients: all rows beside the sort, which leaves most of the chip idle, or the rows of no token beside the sums.
+  // The former writes rows of tokens twice.
+  const bool clear_all = (int64_t)tokens * c.hidden * es <= kClearAll;
+  if (clear_all) {
+    clears(0, dtable, (int64_t)c.vocab * c.hidden);
+    clears(1, drows, (int64_t)num_rows * c.hidden);
+  }
+  const int clear_blocks = !clear_all ? 0 : (int)std::max<int64_t>(1, std::min<int64_t>(1024, (s.pieces[0] + s.pieces[1]) / 8192));
   void* sargs[] = {(void*)&s};
   hipError_t e = hipLaunchKernel((const void*)sort_kernel, dim3(s.sort_blocks + clear_blocks), dim3(1024), sargs, 0, st);
   int64_t len = kSortList;
   for (; e == hipSuccess && len < tokens; len *= kMergeLists) {
-    MergeArgs m{key, at, key2, at2, tokens, (int)len, 1};
-    while ((1ll << m.steps) <= len) ++m.steps;
+    MergeArgs m{key, at, key2, at2, tokens, (int)len};
     void* margs[] = {(void*)&m};
     e = hipLaunchKernel((const void*)merge_kernel, dim3((tokens + 255) / 256), dim3(256), margs, 0, st);
     std::swap(key, key2);
@@ -418,12 +541,22 @@ epd_status epd_embed_backward(const epd_embed_cfg* cfg, const int32_t* ids, int3
   if (e == hipSuccess && tokens) {
     const int pieces = pieces_of(tokens);
     SumsArgs a{key, at, dout, (float*)(ws + L.parts), dtable, drows, ld_dout, tokens, c.hidden, c.vocab, piece_of(tokens), s.none, c.scale};
+    a.runs = runs; a.most_runs = most_runs(pieces);
+    a.slices = (c.hidden + 2047) / 2048;
+    a.sum_blocks = pieces * a.slices;
+    a.clear_rows = (int)std::min<int64_t>(64, std::max<int64_t>(1, 65536 / ((int64_t)c.hidden * es)));         // 64 KB a wave
+    a.clear_blocks = clear_all ? 0 : (int)std::min<int64_t>(kMaxGrid, ((int64_t)s.none + 4 * a.clear_rows - 1) / (4 * a.clear_rows));
     void* args[] = {(void*)&a};
     e = by_types(c, [&](auto t, auto o) {
-      return hipLaunchKernel((const void*)sums_kernel<decltype(t), decltype(o)>, dim3(pieces, (c.hidden + 2047) / 2048), dim3(256), args, 0, st);
+      typedef decltype(t) T;
+      typedef decltype(o) O;
+      return hipLaunchKernel(c.hidden < 8 ? (const void*)sums_kernel<T, O, true> : (const void*)sums_kernel<T, O, false>, dim3(a.sum_blocks + a.clear_blocks), dim3(256), args, 0, st);
     });
-    if (e == hipSuccess && pieces > 1)
-      e = hipLaunchKernel(es == 4 ? (const void*)runs_kernel<float> : (const void*)runs_kernel<__bf16>, dim3(pieces - 1, (c.hidden + 255) / 256), dim3(1024), args, 0, st);
+    if (e == hipSuccess && pieces > 2)
+      e = by_types(c, [&](auto t, auto) {
+        typedef decltype(t) T;
+        return hipLaunchKernel(c.hidden < 8 ? (const void*)runs_kernel<T, true> : (const void*)runs_kernel<T, false>, dim3((int)std::min<int64_t>(1024, (int64_t)a.most_runs * ((c.hidden + 63) / 64))), dim3(512), args, 0, st);
+      });
   }
   return e == hipSuccess ? EPD_OK : op_launch_failed(who, e);
 }

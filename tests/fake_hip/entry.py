@@ -104,7 +104,7 @@ def launches_stay_within_the_thread_limit(fake, lib):
     calls = [(quant, t, T, D) for t in ("bf16", "f32") for T in (most, most - 1, 1 << 24) for D in (1, 512, 2048, 4096, 65536)]
     calls += [(dequant, *c[1:]) for c in calls]
     calls += [(f, t, T, D) for f in (norm, norm_backward) for t in TYPES for T in (most, 1 << 24) for D in (1, 2048, 65536)]
-    calls += [(f, t, 1 << 24, V, D, R) for f in (embed, embed_backward) for t in TYPES for V in (1, 1 << 30) for D in (1, 512, 65536) for R in (0, 1 << 30)]
+    calls += [(f, t, min(1 << 24, (1 << 38) // D), V, D, R) for f in (embed, embed_backward) for t in TYPES for V in (1, 1 << 30) for D in (1, 512, 2049, 16384, 65536) for R in (0, 1 << 30)]
     for K in (16, 1024, 131056):
         for N in (8, 64, 72, 4096, 1 << 15, 1 << 20):
             if K * N < 1 << 32:

@@ -66,7 +66,7 @@ EMBED_BOTH = [
     (dict(struct_size=3), INVALID, "struct_size"), (dict(dtype=7), INVALID, "dtype"), (dict(out_dtype=-1), INVALID, "out_dtype"),
     (dict(dtype=B.EPD_F32, out_dtype=B.EPD_BF16), UNSUPPORTED, "fp32"), (dict(vocab=0), UNSUPPORTED, "vocab"), (dict(vocab=(1 << 30) + 1), UNSUPPORTED, "vocab"),
     (dict(hidden=0), UNSUPPORTED, "hidden"), (dict(hidden=65537), UNSUPPORTED, "hidden"), (dict(max_tokens=0), UNSUPPORTED, "max_tokens"),
-    (dict(max_tokens=(1 << 24) + 1), UNSUPPORTED, "max_tokens"), (dict(scale=float("nan")), INVALID, "scale"), (dict(scale=float("inf")), INVALID, "scale"),
+    (dict(max_tokens=(1 << 24) + 1), UNSUPPORTED, "max_tokens"), (dict(max_tokens=1 << 24, hidden=16385), UNSUPPORTED, "2^38"), (dict(scale=float("nan")), INVALID, "scale"), (dict(scale=float("inf")), INVALID, "scale"),
     (dict(tokens=-1), SHAPE, "tokens"), (dict(tokens=51), SHAPE, "max_tokens"), (dict(num_rows=-1), UNSUPPORTED, "num_rows"),
     (dict(num_rows=(1 << 30) + 1), UNSUPPORTED, "num_rows"), (dict(ids=None), INVALID, "ids"), (dict(ids=A[2] + 2), INVALID, "ids"),
     (dict(ld=23), SHAPE, "apart"), (dict(ld=-24), SHAPE, "apart"), (dict(ld=(1 << 40) + 1), SHAPE, "apart")]
@@ -82,7 +82,7 @@ def test_embed_refusals(kw, status, needle):
 
 @pytest.mark.parametrize("kw,status,needle", EMBED_BOTH + [
     (dict(dout=None), INVALID, "dout"), (dict(dtable=A[0] + 1), INVALID, "aligned"), (dict(drows=A[1] + 1), INVALID, "aligned"), (dict(ws=None), WORKSPACE, "workspace"),
-    (dict(ws=A[4] + 128), WORKSPACE, "256"), (dict(ws_bytes=4 * 256 + 4 * 2 * 24 * 4 - 1), WORKSPACE, "required")])
+    (dict(ws=A[4] + 128), WORKSPACE, "256"), (dict(ws_bytes=4 * 256 + 7 * 2 * 24 * 4 - 1), WORKSPACE, "required")])
 def test_embed_backward_refusals(kw, status, needle):
     got, msg = embed_backward(**kw)
     assert got == status and needle in msg, (got, msg)

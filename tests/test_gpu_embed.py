@@ -52,7 +52,7 @@ def check_backward(got, dout, ids, scale, V, R, dtype):
 
 @pytest.mark.parametrize("dtype,out", TYPES)
 @pytest.mark.parametrize("T,V,D,R", [(1, 1, 1, 0), (1, 7, 8, 0), (2, 3, 5, 2), (5, 100, 513, 0), (32, 1000, 3200, 0), (63, 64, 1024, 17), (129, 50, 2049, 64),
-                                     (1000, 300, 130, 400), (4099, 999, 40, 1000)])
+                                     (1000, 300, 130, 400), (4099, 999, 40, 1000), (300, 30, 5, 7)])
 def test_forward_and_gradients(dtype, out, T, V, D, R):
     gen = generator(T + V + D)
     ids = some_ids(gen, T, V, R)
@@ -79,16 +79,21 @@ def test_rows_of_many_tokens(dtype, out, T, D):
     check_forward(op.forward(table, ids, rows), table, rows, ids, op.cfg.scale, V, R)
 
 
-# lists of 8192 that are merged: two, the eighth full, one more than eight; tables of one to four digits of nine bits
-@pytest.mark.parametrize("T,V,D,hot", [(8192, 500, 8, 0.0), (8193, 40000, 8, 0.9), (16384, 131072, 16, 0.1), (16385, 131072, 8, 0.5), (65536, 70, 8, 0.2),
-                                       (65537, 262143, 8, 0.3), (150001, 1 << 20, 4, 0.99)])
+# lists of 4096 that are merged: one full, two, the eighth full, one more than eight, three rounds of merging; tables of one to four digits of nine bits
+@pytest.mark.parametrize("T,V,D,hot", [(4096, 300, 8, 0.0), (4097, 40000, 8, 0.9), (8192, 500, 8, 0.0), (8193, 40000, 8, 0.9), (32768, 1000, 8, 0.1), (32769, 1000, 8, 0.1), (262145, 3000, 4, 0.3), (16384, 131072, 16, 0.1), (16385, 131072, 8, 0.5), (65536, 70, 8, 0.2),
+                                       (65537, 262143, 8, 0.3), (150001, 1 << 20, 4, 0.99),
+                                       # rows of no token cleared beside the sums: few rows, many, one wave's last ones, and odd lengths
+                                       (8300, 300, 3200, 0.4), (10007, 5000, 2601, 0.1), (9001, 4099, 2804, 0.0), (400, 70, 65536, 0.3)])
 def test_gradients_of_many_tokens(T, V, D, hot):
     gen = generator(T)
     R = 100
     ids = some_ids(gen, T, V, R, hot)
     op = B.Embedding("bf16", V, D, out="f32", scale=0.5, max_tokens=T, training=True)
     dout = randn(gen, T, D)
-    check_backward(op.backward(ids, dout, num_rows=R), dout, ids, 0.5, V, R, "bf16")
+    got = op.backward(ids, dout, num_rows=R)
+    check_backward(got, dout, ids, 0.5, V, R, "bf16")
+    for name in got:
+        assert torch.equal(op.backward(ids, dout, num_rows=R, want=[name])[name], got[name])
 
 
 def test_every_digit_of_a_key():
