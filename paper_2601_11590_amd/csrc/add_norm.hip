@@ -37,11 +37,28 @@ __device__ __forceinline__ void store_q8(int8_t* p, int left, const float* v, fl
   }
 }
 
-// Sum or maximum over the row's TPR threads, in an order of its own whatever else the block does; every thread gets it.
-template <int TPR, class Op> __device__ __forceinline__ auto row_reduce(decltype(Op::of(0, 0)) v, void* lds, Op) {
-  typedef decltype(v) V;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = Op::of(v, (V)__shfl_xor(v, o));
+struct Sum { static __device__ __forceinline__ float of(float a, float b) { return a + b; } };
+struct Most { static __device__ __forceinline__ uint32_t of(uint32_t a, uint32_t b) { return a > b ? a : b; } };
+
+template <class Op, class V> __device__ __forceinline__ V with_lane(V v, uint32_t other) { return Op::of(v, __builtin_bit_cast(V, other)); }
+template <class Op, int CTRL, class V> __device__ __forceinline__ V with_dpp(V v) {
+  return with_lane<Op>(v, (uint32_t)__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+// Sum or maximum over the row's TPR threads, in an order of its own whatever else the block does; every thread gets it.  Lanes meet in
+// vector instructions, without LDS.
+template <class Op, int TPR, class V> __device__ __forceinline__ V row_reduce(V v, void* lds) {
+  v = with_dpp<Op, 0xB1>(v);                               // quad_perm 1,0,3,2
+  v = with_dpp<Op, 0x4E>(v);                               // quad_perm 2,3,0,1
+  v = with_dpp<Op, 0x141>(v);                              // row_half_mirror
+  if constexpr (TPR > 8) {
+    v = with_dpp<Op, 0x140>(v);                            // row_mirror
+    const uint32_t a = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    v = Op::of(__builtin_bit_cast(V, (uint32_t)r[0]), __builtin_bit_cast(V, (uint32_t)r[1]));
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    v = Op::of(__builtin_bit_cast(V, (uint32_t)q[0]), __builtin_bit_cast(V, (uint32_t)q[1]));
+  }
   if constexpr (TPR > 64) {                                // the block is one row
     V* const part = (V*)lds;
     __syncthreads();                                       // (of the reduction before)
@@ -53,9 +70,21 @@ template <int TPR, class Op> __device__ __forceinline__ auto row_reduce(decltype
   }
   return v;
 }
-struct Sum { static __device__ __forceinline__ float of(float a, float b) { return a + b; } };
-struct Most { static __device__ __forceinline__ uint32_t of(uint32_t a, uint32_t b) { return a > b ? a : b; } };
-
+// Two sums at once.
+template <int TPR> __device__ __forceinline__ void row_sums(float& a, float& b, float* lds) {
+  a = row_reduce<Sum, TPR < 64 ? TPR : 64>(a, nullptr);
+  b = row_reduce<Sum, TPR < 64 ? TPR : 64>(b, nullptr);
+  if constexpr (TPR > 64) {
+    float2* const part = (float2*)lds;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    float2 v = part[0];
+#pragma unroll
+    for (int i = 1; i < TPR / 64; ++i) { const float2 w = part[i]; v.x += w.x; v.y += w.y; }
+    a = v.x; b = v.y;
+  }
+}
 struct NormArgs {
   const void *x, *r, *gain;          // x or r may be nullptr, and any output
   void *sum, *y;
@@ -79,9 +108,9 @@ template <typename T, typename R, int TPR, int U, bool NORM>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a) {
   __shared__ uint32_t lds[TPR > 64 ? TPR / 64 : 1];
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-  static_assert(TPR == 64 || TPR >= 256, "a wave or a block per row");
+  static_assert(TPR == 8 || TPR == 64 || TPR >= 256, "eight lanes, a wave or a block per row");
   const int row = blockIdx.x * RPB + (int)threadIdx.x / TPR, at = (int)threadIdx.x % TPR;
-  if (row >= a.rows) return;                               // whole waves of a row each
+  if (row >= a.rows) return;                               // whole groups of lanes, which only meet each other
   float v[U][8];
   const T* const x = a.x ? (const T*)a.x + (int64_t)row * a.ld_x : nullptr;
 #pragma unroll
@@ -118,7 +147,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss = fmaf(v[u][i], v[u][i], ss);
-    ss = row_reduce<TPR>(ss, lds, Sum{});
+    ss = row_reduce<Sum, TPR>(ss, lds);
     const float rstd = 1.0f / sqrtf(fmaf(ss, a.inv_d, a.eps));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -145,7 +174,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int i = 0; i < 8; ++i) most = Most::of(most, __float_as_uint(v[u][i]) & 0x7fffffffu);
-  most = row_reduce<TPR>(most, lds, Most{});
+  most = row_reduce<Most, TPR>(most, lds);
   const bool finite = most < 0x7f800000u;
   const float m = fmaxf(__uint_as_float(most), kLeastMax), to_q = 127.0f / m;
   if (at == 0) a.scale[row] = finite ? m * (1.0f / 127.0f) : __uint_as_float(0x7fc00000u);
@@ -167,7 +196,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 template <typename T, typename R, int TPR, int U>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGradArgs a) {
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-  __shared__ float lds[RPB > 1 ? (RPB - 1) * U * TPR * 8 : 16];
+  __shared__ float lds[RPB > 1 ? (RPB - 1) * U * TPR * 8 : 2 * TPR / 64];
   const int group = (int)threadIdx.x / TPR, at = (int)threadIdx.x % TPR;
   const int64_t r0 = ((int64_t)blockIdx.x * RPB + group) * a.per;
   const int r1 = (int)min(r0 + a.per, (int64_t)a.rows);
@@ -177,16 +206,17 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGr
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[u][i] = 0.f;
   for (int64_t row = r0; row < r1; ++row) {
-    float s[U][8], d[U][8];
+    float s[U][8], d[U][8], o[U][8];
     float ss = 0.f, gn = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int e = (u * TPR + at) * 8, left = a.D - e;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[u][i] = d[u][i] = 0.f;
+      for (int i = 0; i < 8; ++i) s[u][i] = d[u][i] = o[u][i] = 0.f;
       if (left <= 0) continue;
       load8((const R*)a.s + row * a.ld_s + e, left, s[u]);
       load8((const T*)a.dy + row * a.ld_dy + e, left, d[u]);
+      if (a.ds) load8((const R*)a.ds + row * a.ld_ds + e, left, o[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -197,27 +227,23 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGr
 #pragma unroll
       for (int i = 0; i < 8; ++i) { ss = fmaf(s[u][i], s[u][i], ss); gn = fmaf(d[u][i] * g[i], s[u][i], gn); }
     }
-    ss = row_reduce<TPR>(ss, lds, Sum{});
-    gn = row_reduce<TPR>(gn, lds, Sum{});
+    row_sums<TPR>(ss, gn, lds);
     const float rstd = 1.0f / sqrtf(fmaf(ss, a.inv_d, a.eps));
     const float k = gn * rstd * a.inv_d;                   // mean(g n)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int e = (u * TPR + at) * 8, left = a.D - e;
       if (left <= 0) continue;
-      float g[8], o[8];
+      float g[8];
       load8((const T*)a.gain + e, left, g);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = 0.f;
-      if (a.ds) load8((const R*)a.ds + row * a.ld_ds + e, left, o);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float n = s[u][i] * rstd;
         sums[u][i] = fmaf(d[u][i], n, sums[u][i]);
-        o[i] = fmaf(rstd, fmaf(-n, k, d[u][i] * g[i]), o[i]);
+        o[u][i] = fmaf(rstd, fmaf(-n, k, d[u][i] * g[i]), o[u][i]);
       }
-      if (a.dx) store8((T*)a.dx + row * a.ld_dx + e, left, o);
-      if (a.dr) store8((R*)a.dr + row * a.ld_dr + e, left, o);
+      if (a.dx) store8((T*)a.dx + row * a.ld_dx + e, left, o[u]);
+      if (a.dr) store8((R*)a.dr + row * a.ld_dr + e, left, o[u]);
     }
   }
   if (!a.parts) return;
@@ -288,11 +314,14 @@ template <typename T> __global__ __launch_bounds__(256) void dequant_kernel(Dequ
 template <class F> hipError_t by_width(int D, F&& f) {
   using std::integral_constant;
 #define EPD_WIDTH(tpr, u) return f(integral_constant<int, tpr>{}, integral_constant<int, u>{})
+  if (D <= 64) EPD_WIDTH(8, 1);
   if (D <= 512) EPD_WIDTH(64, 1);
   if (D <= 1024) EPD_WIDTH(64, 2);
+  if (D <= 1536) EPD_WIDTH(64, 3);
   if (D <= 2048) EPD_WIDTH(64, 4);
   if (D <= 4096) EPD_WIDTH(256, 2);
   if (D <= 8192) EPD_WIDTH(256, 4);
+  if (D <= 16384) EPD_WIDTH(1024, 2);
   if (D <= 32768) EPD_WIDTH(1024, 4);
   EPD_WIDTH(1024, 8);
 #undef EPD_WIDTH
@@ -317,17 +346,22 @@ template <typename T, typename R, bool NORM> hipError_t launch_norm_rows(const N
   });
 }
 
-// Blocks of the backward pass: the chip filled, each group of threads with some rows, whose sums it keeps.
-constexpr int kGradBlocks = 1024;
-int grad_rows_per_block(int D) { return D <= 2048 ? 4 : 1; }
+// Blocks of the backward pass: the chip filled, each group of threads with two rows or more, whose sums it keeps.
+constexpr int kGradRows = 2;
+int grad_rows_per_block(int D) { return D <= 64 ? 32 : D <= 2048 ? 4 : 1; }
+int grad_most_blocks(int D) { return D > 8192 ? 512 : 1024; }
+int grad_rows(int rows, int D) {         // of a group
+  const int64_t groups = (int64_t)grad_most_blocks(D) * grad_rows_per_block(D);
+  return (int)std::max<int64_t>(kGradRows, (rows + groups - 1) / groups);
+}
 int grad_blocks(int rows, int D) {
-  const int rpb = grad_rows_per_block(D), per = std::max(4, (int)(((int64_t)rows + kGradBlocks * rpb - 1) / (kGradBlocks * rpb)));
-  return (int)(((int64_t)rows + per * rpb - 1) / (per * rpb));
+  const int64_t per = (int64_t)grad_rows(rows, D) * grad_rows_per_block(D);
+  return (int)((rows + per - 1) / per);
 }
 
 template <typename T, typename R> hipError_t launch_norm_grad(NormGradArgs a, void* dgain, hipStream_t s) {
-  const int rpb = grad_rows_per_block(a.D), blocks = grad_blocks(a.rows, a.D);
-  a.per = std::max(4, (int)(((int64_t)a.rows + kGradBlocks * rpb - 1) / (kGradBlocks * rpb)));
+  const int blocks = grad_blocks(a.rows, a.D);
+  a.per = grad_rows(a.rows, a.D);
   void* args[] = {(void*)&a};
   hipError_t e = by_width(a.D, [&](auto TPR, auto U) {
     constexpr int tpr = decltype(TPR)::value;
@@ -351,8 +385,8 @@ epd_status check_cfg(const char* who, const epd_add_norm_cfg* c) {
 }
 
 uint64_t workspace_bytes(const epd_add_norm_cfg& c) {
-  // (fewer tokens may take as many blocks: a block has at least four rows a group)
-  const int64_t rpb = grad_rows_per_block(c.hidden), blocks = std::min<int64_t>(kGradBlocks, (c.max_tokens + 4 * rpb - 1) / (4 * rpb));
+  // (fewer tokens may take as many blocks)
+  const int64_t per = kGradRows * grad_rows_per_block(c.hidden), blocks = std::min<int64_t>(grad_most_blocks(c.hidden), (c.max_tokens + per - 1) / per);
   return ((uint64_t)blocks * c.hidden * 4 + 255) / 256 * 256;
 }
 
