@@ -310,17 +310,20 @@ template <typename T> __global__ __launch_bounds__(256) void dequant_kernel(Dequ
   }
 }
 
-// f(threads per row, chunks per thread) as integral constants: the fewest threads that hold a row of D in four chunks each (eight beyond 32768)
-template <class F> hipError_t by_width(int D, F&& f) {
+// f(threads per row, chunks per thread) as integral constants.  Few chunks a thread keep more rows in flight: 32 768 x 3200 with its sum and
+// 8 bits 210 us by 512 threads of one chunk, 221 by 256 of two, 243 by a wave of seven; backward, 10 000 x 2048 42 us by 256 of one, 67 by a
+// wave of four; 6000 x 8192 bf16 forward 74 by 512 of two, 79 by 256 of four; but 6272 x 1024 backward 13.9 by a wave of two, 18.8 by 256 of
+// one.  Rows that are only rounded (NORM = false) have half the loads: 12 800 x 3200 24.3 us by 256 of two, 29.6 by 512 of one.
+template <bool NORM, class F> hipError_t by_width(int D, F&& f) {
   using std::integral_constant;
 #define EPD_WIDTH(tpr, u) return f(integral_constant<int, tpr>{}, integral_constant<int, u>{})
   if (D <= 64) EPD_WIDTH(8, 1);
   if (D <= 512) EPD_WIDTH(64, 1);
   if (D <= 1024) EPD_WIDTH(64, 2);
-  if (D <= 1536) EPD_WIDTH(64, 3);
-  if (D <= 2048) EPD_WIDTH(64, 4);
-  if (D <= 4096) EPD_WIDTH(256, 2);
-  if (D <= 8192) EPD_WIDTH(256, 4);
+  if (D <= 2048) EPD_WIDTH(256, 1);
+  if constexpr (NORM) { if (D <= 4096) EPD_WIDTH(512, 1); }
+  else if (D <= 4096) EPD_WIDTH(256, 2);
+  if (D <= 8192) EPD_WIDTH(512, 2);
   if (D <= 16384) EPD_WIDTH(1024, 2);
   if (D <= 32768) EPD_WIDTH(1024, 4);
   EPD_WIDTH(1024, 8);
@@ -328,7 +331,7 @@ template <class F> hipError_t by_width(int D, F&& f) {
 }
 
 template <typename T, typename R, bool NORM> hipError_t launch_norm_rows(const NormArgs& all, hipStream_t s) {
-  return by_width(all.D, [&](auto TPR, auto U) {
+  return by_width<NORM>(all.D, [&](auto TPR, auto U) {
     constexpr int tpr = decltype(TPR)::value, rpb = tpr < 256 ? 256 / tpr : 1;
     constexpr int64_t most = (int64_t)kMaxGrid * rpb / (tpr > 512 ? 2 : 1);      // rows of a launch
     for (int64_t r = 0; r < all.rows; r += most) {
@@ -346,13 +349,12 @@ template <typename T, typename R, bool NORM> hipError_t launch_norm_rows(const N
   });
 }
 
-// Blocks of the backward pass: the chip filled, each group of threads with two rows or more, whose sums it keeps.
-constexpr int kGradRows = 2;
-int grad_rows_per_block(int D) { return D <= 64 ? 32 : D <= 2048 ? 4 : 1; }
+// Blocks of the backward pass: the chip filled, then more rows for each group of threads, whose sums it keeps.
+int grad_rows_per_block(int D) { return D <= 64 ? 32 : D <= 1024 ? 4 : 1; }      // as by_width has it
 int grad_most_blocks(int D) { return D > 8192 ? 512 : 1024; }
 int grad_rows(int rows, int D) {         // of a group
   const int64_t groups = (int64_t)grad_most_blocks(D) * grad_rows_per_block(D);
-  return (int)std::max<int64_t>(kGradRows, (rows + groups - 1) / groups);
+  return (int)((rows + groups - 1) / groups);
 }
 int grad_blocks(int rows, int D) {
   const int64_t per = (int64_t)grad_rows(rows, D) * grad_rows_per_block(D);
@@ -363,7 +365,7 @@ template <typename T, typename R> hipError_t launch_norm_grad(NormGradArgs a, vo
   const int blocks = grad_blocks(a.rows, a.D);
   a.per = grad_rows(a.rows, a.D);
   void* args[] = {(void*)&a};
-  hipError_t e = by_width(a.D, [&](auto TPR, auto U) {
+  hipError_t e = by_width<true>(a.D, [&](auto TPR, auto U) {
     constexpr int tpr = decltype(TPR)::value;
     return hipLaunchKernel((const void*)norm_grad_kernel<T, R, tpr, decltype(U)::value>, dim3(blocks), dim3(tpr < 256 ? 256 : tpr), args, 0, s);
   });
@@ -386,7 +388,7 @@ epd_status check_cfg(const char* who, const epd_add_norm_cfg* c) {
 
 uint64_t workspace_bytes(const epd_add_norm_cfg& c) {
   // (fewer tokens may take as many blocks)
-  const int64_t per = kGradRows * grad_rows_per_block(c.hidden), blocks = std::min<int64_t>(grad_most_blocks(c.hidden), (c.max_tokens + per - 1) / per);
+  const int64_t per = grad_rows_per_block(c.hidden), blocks = std::min<int64_t>(grad_most_blocks(c.hidden), (c.max_tokens + per - 1) / per);
   return ((uint64_t)blocks * c.hidden * 4 + 255) / 256 * 256;
 }
 

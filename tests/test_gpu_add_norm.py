@@ -17,8 +17,8 @@ pytestmark = pytest.mark.gpu
 TYPES = [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")]
 EPS = 1e-6
 LEAST = 2.0 ** -100
-# every width of rows a wave or a block takes: one to four (eight) chunks of eight each, full, one less and one more
-SIZES = [(1, 1), (3, 7), (2, 8), (5, 511), (4, 512), (7, 513), (9, 1024), (3, 1100), (6, 2048), (5, 2049), (16, 3200), (2, 4096), (3, 4100), (2, 8192), (3, 8200), (2, 16384),
+# every width of rows that eight lanes, a wave or a block take in chunks of eight: full, one less and one more
+SIZES = [(1, 1), (3, 7), (2, 8), (70, 64), (33, 65), (5, 511), (4, 512), (7, 513), (9, 1024), (3, 1100), (6, 2048), (5, 2049), (16, 3200), (2, 4096), (3, 4100), (2, 8192), (3, 8200), (2, 16384), (3, 16385),
          (2, 32768), (3, 32769), (2, 65535), (1, 65536), (257, 1152), (1031, 72)]
 
 
