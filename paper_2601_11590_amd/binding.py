@@ -1003,7 +1003,9 @@ class Embedding(_Operator):
         prows = _dense(rows, "rows", (R, self.hidden), self.dtype, self._index) if R else None
         if out is None:
             out = torch.empty((T, self.hidden), dtype=self.out_dtype, device=self.device)
-        py, ld = _matrix(out, "out", T, self.hidden, self.out_dtype, self._index)
+            py, ld = out.data_ptr() or 256, self.hidden
+        else:
+            py, ld = _matrix(out, "out", T, self.hidden, self.out_dtype, self._index)
         _on(self._index, epd_embed, self.cfg, ptable, prows, R, pids, T, py, ld)
         return out
 
@@ -1036,7 +1038,7 @@ class AddNorm(_Operator):
         c = self.cfg = epd_add_norm_cfg()
         _sizes(c, dtype=_DTYPES[dtype], residual_dtype=_DTYPES[residual or dtype], hidden=hidden, max_tokens=max_tokens, eps=eps)
         self.hidden, self.dtype, self.residual_dtype, self.training = hidden, torch_dtype(dtype), torch_dtype(residual or dtype), training
-        self._types = {"x": self.dtype, "residual": self.residual_dtype, "sum": self.residual_dtype, "y": self.dtype, "q": torch.int8, "dy": self.dtype,
+        self._types = {"sum": self.residual_dtype, "y": self.dtype, "q": torch.int8, "dy": self.dtype,
                        "dsum": self.residual_dtype, "dx": self.dtype, "dresidual": self.residual_dtype}
         nbytes = epd_add_norm_workspace_bytes(c)
         self._own(nbytes if training or nbytes == 0 else None, device)
@@ -1064,22 +1066,33 @@ class AddNorm(_Operator):
                 out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
         """x, residual: [tokens, hidden], rows any stride apart; one of them may be None.  ``want``: any of "sum", "y" and "q", which comes
         with "scale" (``quant_rows``).  ``out`` may name tensors for the outputs; sum may be ``residual``, y may be ``x``."""
-        r = epd_add_norm_rows()
-        some = x if x is not None else residual
+        # (arguments are put together in one go: for 16 rows the call is a third of the host's time, its preparation another)
+        some, D, i = x if x is not None else residual, self.hidden, self._index
         if some is None:
             raise ValueError("neither x nor residual")
         T = self._tokens(some)
-        if x is not None:
-            self._put(r, "x", x, T)
-        if residual is not None:
-            self._put(r, "residual", residual, T)
-        made = self._outputs(r, want, out, T)
+        px, ld_x = (None, 0) if x is None else _matrix(x, "x", T, D, self.dtype, i)
+        pr, ld_r = (None, 0) if residual is None else _matrix(residual, "residual", T, D, self.residual_dtype, i)
+        made, at = {}, {}
+        for n in want:
+            if n not in ("sum", "y", "q"):
+                raise ValueError("%r is no output" % (n,))
+            t, kind = out.get(n) if out else None, self._types[n]
+            if t is None:
+                like = residual if residual is not None and self.residual_dtype == kind else x if x is not None and self.dtype == kind else None
+                made[n] = t = torch.empty((T, D), dtype=kind, device=self.device) if like is None else torch.empty_like(like)
+                at[n] = t.data_ptr() or 256, D
+            else:
+                made[n], at[n] = t, _matrix(t, n, T, D, kind, i)
+        ps = None
         if "q" in made:
-            s = out.get("scale") if out else None
-            made["scale"] = s = torch.empty(T, dtype=torch.float32, device=self.device) if s is None else s
-            r.scale = _dense(s, "scale", (T,), torch.float32, self._index)
-        pg = None if gain is None else _dense(gain, "gain", (self.hidden,), self.dtype, self._index)
-        _on(self._index, epd_add_norm, self.cfg, r, pg, T)
+            t = out.get("scale") if out else None
+            made["scale"] = t = torch.empty(T, dtype=torch.float32, device=self.device) if t is None else t
+            ps = _dense(t, "scale", (T,), torch.float32, i)
+        none = (None, 0)
+        (psum, ld_s), (py, ld_y), (pq, ld_q) = at.get("sum", none), at.get("y", none), at.get("q", none)
+        pg = None if gain is None else _dense(gain, "gain", (D,), self.dtype, i)
+        _on(i, epd_add_norm, self.cfg, epd_add_norm_rows(px, pr, psum, py, pq, ps, ld_x, ld_r, ld_s, ld_y, ld_q), pg, T)
         return made
 
     def backward(self, gain: torch.Tensor, sum: torch.Tensor, dy: torch.Tensor, dsum: Optional[torch.Tensor] = None, want: Optional[Sequence[str]] = None,
@@ -1091,6 +1104,8 @@ class AddNorm(_Operator):
             raise EpdError(EPD_ERR_INVALID_ARG, "the object was made without training")
         if want is None:
             want = ("dx", "gain") if self.dtype == self.residual_dtype else ("dx", "dresidual", "gain")
+        if any(n not in ("dx", "dresidual", "gain") for n in want):
+            raise ValueError("gradients are dx, dresidual and gain")
         g, T = epd_add_norm_grads(), self._tokens(sum)
         self._put(g, "sum", sum, T)
         self._put(g, "dy", dy, T)
@@ -1157,7 +1172,9 @@ class Int8Linear(_Operator):
         ps = _dense(x_scale, "x_scale", (T,), torch.float32, i)
         if out is None:
             out = torch.empty((T, N), dtype=self.out_dtype, device=self.device)
-        py, ld_y = _matrix(out, "out", T, N, self.out_dtype, i)
+            py, ld_y = out.data_ptr() or 256, N
+        else:
+            py, ld_y = _matrix(out, "out", T, N, self.out_dtype, i)
         self._with_workspace(epd_int8_linear, self.cfg, w, px, ld_x, ps, T, py, ld_y)
         return out
 
