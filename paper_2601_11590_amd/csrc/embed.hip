@@ -4,7 +4,7 @@
 //
 // Backward.  Text and visual rows are one range of keys, the table's rows and behind them those of V_m:
 //   grad[key] = sum of dout over the tokens of that key (* scale)
-// The tokens are sorted by key, which puts those of a row side by side; blocks then add runs of equal keys.  Nothing is added
+// The tokens are sorted by key, which puts those of a row side by side; blocks then add runs of equal keys (up to 128 tokens: few_kernel).  Nothing is added
 // atomically, so a gradient's bits depend on the ids alone.
 //   1. sort_kernel: up to 4096 tokens a block, sorted in LDS by their keys' digits, from the lowest up, keeping the order of equal ones;
 //      meanwhile the other blocks clear the gradients, which is most of what is written where the table is large
@@ -79,6 +79,11 @@ struct SortArgs {
   int tail[2];
 };
 
+__device__ __forceinline__ uint32_t key_of(int id, int vocab, int num_rows, uint32_t none) {
+  if (id >= 0) return id < vocab ? (uint32_t)id : none;
+  return id >= -num_rows ? (uint32_t)vocab + (uint32_t)(-1 - id) : none;
+}
+
 __global__ __launch_bounds__(1024) void sort_kernel(SortArgs a) {
   __shared__ uint32_t keys[2][kSortList];
   __shared__ uint16_t ats[2][kSortList];
@@ -100,12 +105,8 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs a) {
   const int rounds = (n + 1023) / 1024, base = wave * rounds * 64;       // a wave's elements: side by side, 64 a round
   for (int r = 0; r < rounds; ++r) {
     const int i = base + r * 64 + lane;
-    uint32_t k = a.none;                                   // elements past the last one stay behind it: equal keys keep their order
-    if (i < n) {
-      const int id = a.ids[first + i];
-      if (id >= 0) { if (id < a.vocab) k = (uint32_t)id; }
-      else if (id >= -a.num_rows) k = (uint32_t)a.vocab + (uint32_t)(-1 - id);
-    }
+    // elements past the last one stay behind it: equal keys keep their order
+    const uint32_t k = i < n ? key_of(a.ids[first + i], a.vocab, a.num_rows, a.none) : a.none;
     keys[0][i] = k;
     ats[0][i] = (uint16_t)i;
   }
@@ -251,6 +252,8 @@ struct SumsArgs {
   float scale;
   Runs* runs;
   int most_runs;                     // that the list holds
+  const int32_t* ids;                // few_kernel
+  int num_rows;
   int slices, sum_blocks, clear_blocks, clear_rows;        // sums_kernel: blocks per piece, of sums, and those that clear `clear_rows` rows a wave
 };
 
@@ -264,16 +267,16 @@ template <typename T> __device__ __forceinline__ T* row_of(const SumsArgs& a, ui
 __device__ __forceinline__ bool wanted(const SumsArgs& a, uint32_t key) { return key < (uint32_t)a.vocab ? a.table != nullptr : key < a.none && a.rows != nullptr; }
 
 // Rows of no token, by a wave, `clear_rows` (up to 64) at a time: its lanes look for as many rows among the sorted keys.
-template <typename T> __device__ __forceinline__ void clear_rows(const SumsArgs& a, int64_t wave) {
+template <typename T> __device__ __forceinline__ void clear_rows(const SumsArgs& a, const uint32_t* sorted, int64_t wave) {
   const int lane = threadIdx.x & 63;
   for (int64_t r0 = wave * a.clear_rows; r0 < (int64_t)a.none; r0 += 4ll * a.clear_blocks * a.clear_rows) {
     const uint32_t key = (uint32_t)min(r0 + lane, (int64_t)a.none);
     int lo = 0, hi = a.tokens;                             // the first token of this key or a later one
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (a.key[mid] < key) lo = mid + 1; else hi = mid;
+      if (sorted[mid] < key) lo = mid + 1; else hi = mid;
     }
-    uint64_t absent = __ballot(lane < a.clear_rows && key < a.none && wanted(a, key) && (lo >= a.tokens || a.key[min(lo, a.tokens - 1)] != key));
+    uint64_t absent = __ballot(lane < a.clear_rows && key < a.none && wanted(a, key) && (lo >= a.tokens || sorted[min(lo, a.tokens - 1)] != key));
     float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, scale;
     for (; absent; absent &= absent - 1) {
       T* const row = row_of<T>(a, (uint32_t)(r0 + __ffsll((unsigned long long)absent) - 1), scale);
@@ -282,17 +285,73 @@ template <typename T> __device__ __forceinline__ void clear_rows(const SumsArgs&
   }
 }
 
-// A block's runs are those that start in its piece.  One that ends in the next piece is finished here, beyond the piece's end, and
-// passed over there; one that goes on further is `long`: every block adds its own part, for runs_kernel.
+// The runs of sorted tokens [first, last), whose last one ends there or leaves a part: rows of the gradient, or partial sums.  e: the
+// thread's first column; all lanes of a wave come here, those past the row's end with it.  What decides about a token -- whether its run ends,
+// whether it counts -- is made for all of a batch at once by its lanes: read from LDS token by token it took longer than the rows
+// (230 rows of one token: 56 us).
 //   TINY: rows of fewer than eight elements.  Otherwise the last eight of a row stand in for the ones that would run past it, which two
 // threads then write alike, so that no load waits behind a branch (embed-grad of 32 768 x 3200 with branches: 190 us).
+template <typename T, typename O, bool TINY, int BATCH>
+__device__ __forceinline__ void add_runs(const SumsArgs& a, const uint32_t* key, const uint32_t* at, int first, int last, bool from_before, int piece, int e) {
+  const int lane = threadIdx.x & 63;
+  if (e - lane * 8 >= a.D || first >= last || (!a.table && key[last - 1] < (uint32_t)a.vocab) || (!a.rows && key[first] >= (uint32_t)a.vocab)) return;
+  const bool live = e < a.D;
+  const int left = TINY ? a.D : 8;
+  e = TINY ? 0 : min(e, a.D - 8);
+  float sum[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+  for (int b = first; b < last; b += BATCH) {
+    const uint32_t held = key[min(b + lane, last - 1)];
+    const uint32_t next = key[min(b + lane, last - 1) + 1];
+    const uint64_t ends = __ballot(held != next), counts = __ballot(held < a.none);        // (sorted: those that count stand first)
+    const uint32_t row_at = at[min(b + lane, last - 1)];
+    float v[BATCH][8];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const O* const from = (const O*)a.dout + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)row_at, j) * a.ld + e;
+      if constexpr (TINY) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = (float)from[min(i, left - 1)];
+      } else {
+        load8(from, 8, v[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      if (b + j >= last || !(counts >> j & 1)) break;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += v[j][i];
+      if (!(ends >> j & 1) && b + j + 1 < last) continue;
+      const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)held, j);
+      if (wanted(a, k) && live) {
+        if ((ends >> j & 1) && !from_before) {
+          float scale;
+          T* const row = row_of<T>(a, k, scale);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum[i] *= scale;
+          store8(row + e, left, sum);
+        } else {
+          store8(a.parts + ((int64_t)piece * 2 + (from_before ? 0 : 1)) * a.D + e, left, sum);
+        }
+      }
+      from_before = false;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    }
+    if (!(counts >> (BATCH - 1) & 1)) return;              // what is left has no row
+  }
+}
+
+// A block's runs are those that start in its piece.  One that ends in the next piece is finished here, beyond the piece's end, and
+// passed over there; one that goes on further is `long`: every block adds its own part, for runs_kernel.
 template <typename T, typename O, bool TINY> __global__ __launch_bounds__(256) void sums_kernel(SumsArgs a) {
   __shared__ uint32_t keys[3 * kPiece + 2], at[2 * kPiece];            // from the token ahead of the piece before on
   // blocks that clear stand evenly between the others, so that reads and writes go on together
   const int64_t all = gridDim.x;
   const int clear = (int)((int64_t)blockIdx.x * a.clear_blocks / all);
   if ((int)(((int64_t)blockIdx.x + 1) * a.clear_blocks / all) > clear) {
-    clear_rows<T>(a, (int64_t)clear * 4 + (threadIdx.x >> 6));
+    clear_rows<T>(a, a.key, (int64_t)clear * 4 + (threadIdx.x >> 6));
     return;
   }
   const int block = (int)blockIdx.x - clear, piece = block / a.slices, slice = block - piece * a.slices;
@@ -329,46 +388,52 @@ template <typename T, typename O, bool TINY> __global__ __launch_bounds__(256) v
       a.runs->list[many ? a.most_runs - 1 - i : i] = Run{k, piece, to - piece + 1, 0};
     }
   }
-  // (the ballots above need every lane)
-  if (first >= last || (!a.table && key[last - 1] < (uint32_t)a.vocab) || (!a.rows && key[first] >= (uint32_t)a.vocab)) return;
-  int e = (slice * 256 + (int)threadIdx.x) * 8;
-  if (e >= a.D) return;
-  const int left = TINY ? a.D : 8;
-  if constexpr (!TINY) e = min(e, a.D - 8);
-  float sum[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-  constexpr int BATCH = 8;
-  for (int b = first; b < last; b += BATCH) {
-    if (key[b] >= a.none) return;                          // and all behind it
-    float v[BATCH][8];
-#pragma unroll
-    for (int j = 0; j < BATCH; ++j) load8((const O*)a.dout + (int64_t)at[min(b + j, last - 1)] * a.ld + e, left, v[j]);
-#pragma unroll
-    for (int j = 0; j < BATCH; ++j) {
-      if (b + j >= last) break;
-      const uint32_t k = key[b + j];
-      if (k >= a.none) return;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += v[j][i];
-      const bool ends = key[b + j + 1] != k;
-      if (!ends && b + j + 1 < last) continue;
-      if (wanted(a, k)) {
-        if (ends && !from_before) {
-          float scale;
-          T* const row = row_of<T>(a, k, scale);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) sum[i] *= scale;
-          store8(row + e, left, sum);
-        } else {
-          store8(a.parts + ((int64_t)piece * 2 + (from_before ? 0 : 1)) * a.D + e, left, sum);
-        }
-      }
-      from_before = false;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-    }
+  add_runs<T, O, TINY, 8>(a, key, at, first, last, from_before, piece, (slice * 256 + (int)threadIdx.x) * 8);          // (the ballots above need every lane)
+}
+
+// Up to kFewTokens tokens: every block sorts them for itself, by how many go before each, so that one launch does for all (150 rows of 382
+// 9.6 us, by three launches 15.6).  Runs are added whole by the wave whose piece they start in, 2.8 us for 16 rows, which is why more tokens
+// take the other way: a token that takes most of 256 places, 43 us.
+constexpr int kFewTokens = 128;
+template <typename T, typename O, bool TINY> __global__ __launch_bounds__(256) void few_kernel(SumsArgs a) {
+  __shared__ __attribute__((aligned(16))) uint32_t given[kFewTokens], key[kFewTokens + 1], at[kFewTokens];
+  const int tid = threadIdx.x, lane = tid & 63;
+  uint32_t mine = 0xffffffffu;
+  if (tid < a.tokens) mine = key_of(a.ids[tid], a.vocab, a.num_rows, a.none);
+  if (tid < kFewTokens) given[tid] = mine;
+  key[a.tokens] = 0xffffffffu;
+  __syncthreads();
+  int place = 0;
+#pragma unroll 8
+  for (int i = 0; i < a.tokens; i += 4) {                  // (what stands past the last token goes before nothing)
+    const uint4 k = *(const uint4*)(given + i);
+    place += (k.x < mine || (k.x == mine && i < tid)) + (k.y < mine || (k.y == mine && i + 1 < tid)) + (k.z < mine || (k.z == mine && i + 2 < tid)) +
+             (k.w < mine || (k.w == mine && i + 3 < tid));
   }
+  if (tid < a.tokens) { key[place] = mine; at[place] = (uint32_t)tid; }
+  __syncthreads();
+  const int clear = (int)((int64_t)blockIdx.x * a.clear_blocks / gridDim.x);
+  if ((int)(((int64_t)blockIdx.x + 1) * a.clear_blocks / gridDim.x) > clear) {
+    clear_rows<T>(a, key, (int64_t)clear * 4 + (tid >> 6));
+    return;
+  }
+  // 512 columns of a piece a wave (2048 a block leave a token that takes most places to two units of the chip: 54 us for 230 rows of 3200)
+  const int item = ((int)blockIdx.x - clear) * 4 + (tid >> 6), piece = item / a.slices, slice = item - piece * a.slices;
+  if (piece * a.piece >= a.tokens) return;
+  auto end_of = [&](int p) {                               // of the run that holds sorted token p; every lane looks at one of 64 tokens
+    const uint32_t k = key[p];
+    for (;;) {
+      const uint64_t other = __ballot(key[min(p + lane, a.tokens)] != k);
+      if (other) return p + __ffsll((unsigned long long)other) - 1;
+      p += 64;
+    }
+  };
+  int first = piece * a.piece, last = min(first + a.piece, a.tokens);
+  const bool begun = first > 0 && key[first - 1] == key[first];
+  last = end_of(last - 1);
+  if (begun) first = end_of(first);
+  // (a run over the whole piece that started before leaves first = last)
+  add_runs<T, O, TINY, TINY ? 8 : 16>(a, key, at, first, last, false, piece, (slice * 64 + lane) * 8);
 }
 
 // Long runs, those over three pieces or more, as sums_kernel listed them: the parts of one, some columns a block, groups of threads in
@@ -509,55 +574,68 @@ epd_status epd_embed_backward(const epd_embed_cfg* cfg, const int32_t* ids, int3
   uint32_t *key = (uint32_t*)ws, *at = (uint32_t*)(ws + L.list), *key2 = (uint32_t*)(ws + 2 * L.list), *at2 = (uint32_t*)(ws + 3 * L.list);
   hipStream_t st = (hipStream_t)stream;
 
-  SortArgs s{};
+  const uint32_t none = (uint32_t)c.vocab + (uint32_t)num_rows;
+  const int pieces = tokens ? pieces_of(tokens) : 0;
   Runs* const runs = (Runs*)(ws + L.runs);
-  s.counts = runs->count;
-  s.ids = ids; s.key = key; s.at = at; s.tokens = tokens; s.vocab = c.vocab; s.num_rows = num_rows;
-  s.none = (uint32_t)c.vocab + (uint32_t)num_rows;
-  int bits = 1;
-  while ((uint64_t)s.none >> bits) ++bits;
-  s.passes = (bits + kMaxDigit - 1) / kMaxDigit;
-  s.bits = std::max(6, (bits + s.passes - 1) / s.passes);
-  s.sort_blocks = (tokens + kSortList - 1) / kSortList;
-  auto clears = [&](int j, void* p, int64_t n) { if (p) { s.clear[j] = p; s.pieces[j] = n * es / 16; s.tail[j] = (int)(n * es % 16); } };
+  SumsArgs a{key, at, dout, (float*)(ws + L.parts), dtable, drows, ld_dout, tokens, c.hidden, c.vocab, tokens ? piece_of(tokens) : 0, none, c.scale};
+  a.runs = runs; a.most_runs = most_runs(pieces);
+  a.ids = ids; a.num_rows = num_rows;
+  a.slices = (c.hidden + 2047) / 2048;
+  a.sum_blocks = pieces * a.slices;
+  // rows a wave clears: 64 KB, fewer while that leaves waves of the chip idle
+  a.clear_rows = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 65536 / ((int64_t)c.hidden * es)), none / 1024));
+  a.clear_blocks = (int)std::min<int64_t>(kMaxGrid, ((int64_t)none + 4 * a.clear_rows - 1) / (4 * a.clear_rows));
+  void* args[] = {(void*)&a};
+  if (tokens && tokens <= kFewTokens) {
+    a.slices = (c.hidden + 511) / 512;
+    a.sum_blocks = (pieces * a.slices + 3) / 4;
+    const hipError_t e = by_types(c, [&](auto t, auto o) {
+      typedef decltype(t) T;
+      typedef decltype(o) O;
+      return hipLaunchKernel(c.hidden < 8 ? (const void*)few_kernel<T, O, true> : (const void*)few_kernel<T, O, false>, dim3(a.sum_blocks + a.clear_blocks), dim3(256), args, 0, st);
+    });
+    return e == hipSuccess ? EPD_OK : op_launch_failed(who, e);
+  }
   // Which launch clears the gradients: all rows beside the sort, which leaves most of the chip idle, or the rows of no token beside the sums.
   // The former writes rows of tokens twice.
   const bool clear_all = (int64_t)tokens * c.hidden * es <= kClearAll;
+  SortArgs s{};
+  s.counts = runs->count;
+  s.ids = ids; s.key = key; s.at = at; s.tokens = tokens; s.vocab = c.vocab; s.num_rows = num_rows; s.none = none;
+  int bits = 1;
+  while ((uint64_t)none >> bits) ++bits;
+  s.passes = (bits + kMaxDigit - 1) / kMaxDigit;
+  s.bits = std::max(6, (bits + s.passes - 1) / s.passes);
+  s.sort_blocks = (tokens + kSortList - 1) / kSortList;
   if (clear_all) {
+    auto clears = [&](int j, void* p, int64_t n) { if (p) { s.clear[j] = p; s.pieces[j] = n * es / 16; s.tail[j] = (int)(n * es % 16); } };
     clears(0, dtable, (int64_t)c.vocab * c.hidden);
     clears(1, drows, (int64_t)num_rows * c.hidden);
+    a.clear_blocks = 0;
   }
   const int clear_blocks = !clear_all ? 0 : (int)std::max<int64_t>(1, std::min<int64_t>(1024, (s.pieces[0] + s.pieces[1]) / 8192));
   void* sargs[] = {(void*)&s};
   hipError_t e = hipLaunchKernel((const void*)sort_kernel, dim3(s.sort_blocks + clear_blocks), dim3(1024), sargs, 0, st);
-  int64_t len = kSortList;
-  for (; e == hipSuccess && len < tokens; len *= kMergeLists) {
+  for (int64_t len = kSortList; e == hipSuccess && len < tokens; len *= kMergeLists) {
     MergeArgs m{key, at, key2, at2, tokens, (int)len};
     void* margs[] = {(void*)&m};
     e = hipLaunchKernel((const void*)merge_kernel, dim3((tokens + 255) / 256), dim3(256), margs, 0, st);
     std::swap(key, key2);
     std::swap(at, at2);
   }
-  if (e == hipSuccess && tokens) {
-    const int pieces = pieces_of(tokens);
-    SumsArgs a{key, at, dout, (float*)(ws + L.parts), dtable, drows, ld_dout, tokens, c.hidden, c.vocab, piece_of(tokens), s.none, c.scale};
-    a.runs = runs; a.most_runs = most_runs(pieces);
-    a.slices = (c.hidden + 2047) / 2048;
-    a.sum_blocks = pieces * a.slices;
-    a.clear_rows = (int)std::min<int64_t>(64, std::max<int64_t>(1, 65536 / ((int64_t)c.hidden * es)));         // 64 KB a wave
-    a.clear_blocks = clear_all ? 0 : (int)std::min<int64_t>(kMaxGrid, ((int64_t)s.none + 4 * a.clear_rows - 1) / (4 * a.clear_rows));
-    void* args[] = {(void*)&a};
+  a.key = key; a.at = at;
+  if (e == hipSuccess && tokens)
     e = by_types(c, [&](auto t, auto o) {
       typedef decltype(t) T;
       typedef decltype(o) O;
       return hipLaunchKernel(c.hidden < 8 ? (const void*)sums_kernel<T, O, true> : (const void*)sums_kernel<T, O, false>, dim3(a.sum_blocks + a.clear_blocks), dim3(256), args, 0, st);
     });
-    if (e == hipSuccess && pieces > 2)
-      e = by_types(c, [&](auto t, auto) {
-        typedef decltype(t) T;
-        return hipLaunchKernel(c.hidden < 8 ? (const void*)runs_kernel<T, true> : (const void*)runs_kernel<T, false>, dim3((int)std::min<int64_t>(1024, (int64_t)a.most_runs * ((c.hidden + 63) / 64))), dim3(512), args, 0, st);
-      });
-  }
+  if (e == hipSuccess && pieces > 2)
+    e = by_types(c, [&](auto t, auto) {
+      typedef decltype(t) T;
+      return hipLaunchKernel(c.hidden < 8 ? (const void*)runs_kernel<T, true> : (const void*)runs_kernel<T, false>,
+                             dim3((int)std::min<int64_t>(1024, (int64_t)a.most_runs * ((c.hidden + 63) / 64))), dim3(512), args, 0, st);
+    });
   return e == hipSuccess ? EPD_OK : op_launch_failed(who, e);
 }
 

@@ -126,7 +126,7 @@ def work_grows_with_the_launch(fake, lib):
 
 # ------------------------------------------------------------------ what the sizes of the GPU tests reach
 
-NAMES = r"_GLOBAL__N_1\d+((?:embed|sort|merge|sums|runs|norm|norm_grad|gain|dequant|int8_\w+?)_kernel)"
+NAMES = r"_GLOBAL__N_1\d+((?:embed|sort|merge|sums|runs|few|norm|norm_grad|gain|dequant|int8_\w+?)_kernel)"
 
 
 def kernels(fake):

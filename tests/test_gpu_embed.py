@@ -51,7 +51,7 @@ def check_backward(got, dout, ids, scale, V, R, dtype):
 
 
 @pytest.mark.parametrize("dtype,out", TYPES)
-@pytest.mark.parametrize("T,V,D,R", [(1, 1, 1, 0), (1, 7, 8, 0), (2, 3, 5, 2), (5, 100, 513, 0), (32, 1000, 3200, 0), (63, 64, 1024, 17), (129, 50, 2049, 64),
+@pytest.mark.parametrize("T,V,D,R", [(1, 1, 1, 0), (1, 7, 8, 0), (2, 3, 5, 2), (5, 100, 513, 0), (32, 1000, 3200, 0), (63, 64, 1024, 17), (128, 50, 2049, 64), (129, 50, 2049, 64),
                                      (1000, 300, 130, 400), (4099, 999, 40, 1000), (300, 30, 5, 7)])
 def test_forward_and_gradients(dtype, out, T, V, D, R):
     gen = generator(T + V + D)
