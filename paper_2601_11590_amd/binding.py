@@ -966,11 +966,16 @@ class _Operator:
             self._stream = torch.cuda.current_stream(self.device).cuda_stream       # on which the workspace may be handed on
 
     def _with_workspace(self, call, *args) -> None:
-        def on(*a):
-            if a[-1] != self._stream:         # the allocator may not hand the workspace on before this stream is through
-                self.workspace.record_stream(torch.cuda.current_stream(self.device))
-            call(*a[:-1], self._base, self.workspace_bytes, a[-1])
-        _on(self._index, on, *args)
+        i = self._index                       # (as _on, without a function made for every call)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        stream = raw(i) if raw is not None else torch.cuda.current_stream(i).cuda_stream
+        if stream != self._stream:            # the allocator may not hand the workspace on before this stream is through
+            self.workspace.record_stream(torch.cuda.current_stream(self.device))
+        if torch.cuda.current_device() == i:
+            call(*args, self._base, self.workspace_bytes, stream)
+        else:
+            with torch.cuda.device(i):
+                call(*args, self._base, self.workspace_bytes, stream)
 
 
 class Embedding(_Operator):
@@ -1043,24 +1048,23 @@ class AddNorm(_Operator):
         nbytes = epd_add_norm_workspace_bytes(c)
         self._own(nbytes if training or nbytes == 0 else None, device)
 
-    def _put(self, to, name: str, t: torch.Tensor, tokens: Optional[int]) -> None:
-        p, ld = _matrix(t, name, tokens, self.hidden, self._types[name], self._index)
-        setattr(to, name, p)
-        setattr(to, "ld_" + name, ld)
-
     def _tokens(self, t: torch.Tensor) -> int:
         T = t.shape[0]
         if T > self.cfg.max_tokens:
             raise EpdError(EPD_ERR_SHAPE, "%d rows: 0 .. max_tokens %d" % (T, self.cfg.max_tokens))
         return T
 
-    def _outputs(self, to, want, out, T: int) -> Dict[str, torch.Tensor]:
-        made = {}
-        for n in want:
-            t = out.get(n) if out else None
-            made[n] = t = torch.empty((T, self.hidden), dtype=self._types[n], device=self.device) if t is None else t
-            self._put(to, n, t, T)
-        return made
+    def _output(self, out, name: str, T: int, like: Sequence[Optional[torch.Tensor]]):
+        """The caller's tensor of that name, or a new one, its address and what its rows are apart."""
+        t, kind = out.get(name) if out else None, self._types[name]
+        if t is not None:
+            return (t, *_matrix(t, name, T, self.hidden, kind, self._index))
+        for l in like:
+            if l is not None and l.dtype == kind:
+                t = torch.empty_like(l)       # (half the time of torch.empty; its rows are contiguous where those of l are)
+                return t, t.data_ptr() or 256, self.hidden
+        t = torch.empty((T, self.hidden), dtype=kind, device=self.device)
+        return t, t.data_ptr() or 256, self.hidden
 
     def forward(self, gain: Optional[torch.Tensor], x: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, want: Sequence[str] = ("sum", "y"),
                 out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
@@ -1077,13 +1081,7 @@ class AddNorm(_Operator):
         for n in want:
             if n not in ("sum", "y", "q"):
                 raise ValueError("%r is no output" % (n,))
-            t, kind = out.get(n) if out else None, self._types[n]
-            if t is None:
-                like = residual if residual is not None and self.residual_dtype == kind else x if x is not None and self.dtype == kind else None
-                made[n] = t = torch.empty((T, D), dtype=kind, device=self.device) if like is None else torch.empty_like(like)
-                at[n] = t.data_ptr() or 256, D
-            else:
-                made[n], at[n] = t, _matrix(t, n, T, D, kind, i)
+            made[n], *at[n] = self._output(out, n, T, (residual, x))
         ps = None
         if "q" in made:
             t = out.get("scale") if out else None
@@ -1106,17 +1104,22 @@ class AddNorm(_Operator):
             want = ("dx", "gain") if self.dtype == self.residual_dtype else ("dx", "dresidual", "gain")
         if any(n not in ("dx", "dresidual", "gain") for n in want):
             raise ValueError("gradients are dx, dresidual and gain")
-        g, T = epd_add_norm_grads(), self._tokens(sum)
-        self._put(g, "sum", sum, T)
-        self._put(g, "dy", dy, T)
-        if dsum is not None:
-            self._put(g, "dsum", dsum, T)
-        made = self._outputs(g, [n for n in want if n != "gain"], out, T)
+        T, D, i = self._tokens(sum), self.hidden, self._index
+        ps, ld_s = _matrix(sum, "sum", T, D, self.residual_dtype, i)
+        pdy, ld_dy = _matrix(dy, "dy", T, D, self.dtype, i)
+        pds, ld_ds = (None, 0) if dsum is None else _matrix(dsum, "dsum", T, D, self.residual_dtype, i)
+        made, none = {}, (None, 0)
+        dx, dr, pgain = none, none, None
+        if "dx" in want:
+            made["dx"], *dx = self._output(out, "dx", T, (dy,))
+        if "dresidual" in want:
+            made["dresidual"], *dr = self._output(out, "dresidual", T, (sum,))
         if "gain" in want:
             t = out.get("gain") if out else None
-            made["gain"] = t = torch.empty(self.hidden, dtype=self.dtype, device=self.device) if t is None else t
-            g.gain = _dense(t, "gain", (self.hidden,), self.dtype, self._index)
-        self._with_workspace(epd_add_norm_backward, self.cfg, g, _dense(gain, "gain", (self.hidden,), self.dtype, self._index), T)
+            made["gain"] = t = torch.empty_like(gain) if t is None else t
+            pgain = _dense(t, "gain", (D,), self.dtype, i)
+        g = epd_add_norm_grads(ps, pdy, pds, dx[0], dr[0], pgain, ld_s, ld_dy, ld_ds, dx[1], dr[1])
+        self._with_workspace(epd_add_norm_backward, self.cfg, g, _dense(gain, "gain", (D,), self.dtype, i), T)
         return made
 
 
