@@ -227,6 +227,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a) {
 
 // ------------------------------------------------------------------------------ sums of runs
 constexpr int64_t kClearAll = 48 << 20;              // bytes of the tokens' rows up to which all rows are cleared first
+constexpr int64_t kClearBesideSort = 96 << 20;       // bytes
 constexpr int kPiece = 32, kLeastPiece = 8, kFewPieces = 1024;      // tokens of a piece, fewer while that gives no more pieces than this
 int piece_of(int tokens) {
   int piece = kLeastPiece;
@@ -254,6 +255,7 @@ struct SumsArgs {
   int most_runs;                     // that the list holds
   const int32_t* ids;                // few_kernel
   int num_rows;
+  int cut, skip;                     // rows [cut, cut + skip) are clear already
   int slices, sum_blocks, clear_blocks, clear_rows;        // sums_kernel: blocks per piece, of sums, and those that clear `clear_rows` rows a wave
 };
 
@@ -269,8 +271,9 @@ __device__ __forceinline__ bool wanted(const SumsArgs& a, uint32_t key) { return
 // Rows of no token, by a wave, `clear_rows` (up to 64) at a time: its lanes look for as many rows among the sorted keys.
 template <typename T> __device__ __forceinline__ void clear_rows(const SumsArgs& a, const uint32_t* sorted, int64_t wave) {
   const int lane = threadIdx.x & 63;
-  for (int64_t r0 = wave * a.clear_rows; r0 < (int64_t)a.none; r0 += 4ll * a.clear_blocks * a.clear_rows) {
-    const uint32_t key = (uint32_t)min(r0 + lane, (int64_t)a.none);
+  for (int64_t r0 = wave * a.clear_rows; r0 < (int64_t)a.none - a.skip; r0 += 4ll * a.clear_blocks * a.clear_rows) {
+    const int64_t r = r0 + lane;                           // without the rows [cut, cut + skip)
+    const uint32_t key = (uint32_t)min(r < a.cut ? r : r + a.skip, (int64_t)a.none);
     int lo = 0, hi = a.tokens;                             // the first token of this key or a later one
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
@@ -279,7 +282,7 @@ template <typename T> __device__ __forceinline__ void clear_rows(const SumsArgs&
     uint64_t absent = __ballot(lane < a.clear_rows && key < a.none && wanted(a, key) && (lo >= a.tokens || sorted[min(lo, a.tokens - 1)] != key));
     float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, scale;
     for (; absent; absent &= absent - 1) {
-      T* const row = row_of<T>(a, (uint32_t)(r0 + __ffsll((unsigned long long)absent) - 1), scale);
+      T* const row = row_of<T>(a, (uint32_t)__builtin_amdgcn_readlane((int)key, __ffsll((unsigned long long)absent) - 1), scale);
       for (int e = lane * 8; e < a.D; e += 512) store8(row + e, a.D - e, zero);
     }
   }
@@ -596,8 +599,9 @@ epd_status epd_embed_backward(const epd_embed_cfg* cfg, const int32_t* ids, int3
     });
     return e == hipSuccess ? EPD_OK : op_launch_failed(who, e);
   }
-  // Which launch clears the gradients: all rows beside the sort, which leaves most of the chip idle, or the rows of no token beside the sums.
-  // The former writes rows of tokens twice.
+  // Which launch clears the gradients: rows beside the sort, which leaves most of the chip idle, or the rows of no token beside the sums.
+  // The former writes rows of tokens twice.  All rows where the tokens' are few; otherwise as many of the table's last rows as the sort
+  // hides (32 768 tokens, 131 072 x 3200: 298 us without these, 288 with).
   const bool clear_all = (int64_t)tokens * c.hidden * es <= kClearAll;
   SortArgs s{};
   s.counts = runs->count;
@@ -607,13 +611,17 @@ epd_status epd_embed_backward(const epd_embed_cfg* cfg, const int32_t* ids, int3
   s.passes = (bits + kMaxDigit - 1) / kMaxDigit;
   s.bits = std::max(6, (bits + s.passes - 1) / s.passes);
   s.sort_blocks = (tokens + kSortList - 1) / kSortList;
+  auto clears = [&](int j, void* p, int64_t n) { if (p) { s.clear[j] = p; s.pieces[j] = n * es / 16; s.tail[j] = (int)(n * es % 16); } };
   if (clear_all) {
-    auto clears = [&](int j, void* p, int64_t n) { if (p) { s.clear[j] = p; s.pieces[j] = n * es / 16; s.tail[j] = (int)(n * es % 16); } };
     clears(0, dtable, (int64_t)c.vocab * c.hidden);
     clears(1, drows, (int64_t)num_rows * c.hidden);
     a.clear_blocks = 0;
+  } else if (dtable) {
+    a.skip = (int)std::min<int64_t>(c.vocab, kClearBesideSort / ((int64_t)c.hidden * es));
+    a.cut = c.vocab - a.skip;
+    clears(0, (char*)dtable + (int64_t)a.cut * c.hidden * es, (int64_t)a.skip * c.hidden);
   }
-  const int clear_blocks = !clear_all ? 0 : (int)std::max<int64_t>(1, std::min<int64_t>(1024, (s.pieces[0] + s.pieces[1]) / 8192));
+  const int clear_blocks = !s.pieces[0] && !s.pieces[1] && !s.tail[0] && !s.tail[1] ? 0 : (int)std::max<int64_t>(1, std::min<int64_t>(1024, (s.pieces[0] + s.pieces[1]) / 8192));
   void* sargs[] = {(void*)&s};
   hipError_t e = hipLaunchKernel((const void*)sort_kernel, dim3(s.sort_blocks + clear_blocks), dim3(1024), sargs, 0, st);
   for (int64_t len = kSortList; e == hipSuccess && len < tokens; len *= kMergeLists) {
