@@ -313,13 +313,15 @@ template <typename T> __global__ __launch_bounds__(256) void dequant_kernel(Dequ
 // f(threads per row, chunks per thread) as integral constants.  Few chunks a thread keep more rows in flight: 32 768 x 3200 with its sum and
 // 8 bits 210 us by 512 threads of one chunk, 221 by 256 of two, 243 by a wave of seven; backward, 10 000 x 2048 42 us by 256 of one, 67 by a
 // wave of four; 6000 x 8192 bf16 forward 74 by 512 of two, 79 by 256 of four; but 6272 x 1024 backward 13.9 by a wave of two, 18.8 by 256 of
-// one.  Rows that are only rounded (NORM = false) have half the loads: 12 800 x 3200 24.3 us by 256 of two, 29.6 by 512 of one.
+// one.  Rows that are only rounded (NORM = false) have half the loads: 12 800 x 3200 24.3 us by 256 of two, 29.6 by 512 of one, 32 768 x 1152 28.1 by a wave of
+// three, 33.0 by 256 of one.  (Fewer blocks that load the next row ahead are no faster: 24.8 and 32.1.)
 template <bool NORM, class F> hipError_t by_width(int D, F&& f) {
   using std::integral_constant;
 #define EPD_WIDTH(tpr, u) return f(integral_constant<int, tpr>{}, integral_constant<int, u>{})
   if (D <= 64) EPD_WIDTH(8, 1);
   if (D <= 512) EPD_WIDTH(64, 1);
   if (D <= 1024) EPD_WIDTH(64, 2);
+  if constexpr (!NORM) { if (D <= 1536) EPD_WIDTH(64, 3); }
   if (D <= 2048) EPD_WIDTH(256, 1);
   if constexpr (NORM) { if (D <= 4096) EPD_WIDTH(512, 1); }
   else if (D <= 4096) EPD_WIDTH(256, 2);
