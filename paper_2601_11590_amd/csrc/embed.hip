@@ -124,16 +124,19 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs a) {
     for (int r = 0; r < kSortList / 1024; ++r) {
       if (r >= rounds) break;
       const uint32_t d = keys[from][base + r * 64 + lane] >> shift & (digits - 1);
-      uint64_t same = ~0ull;
-      for (int b = 0; b < a.bits; ++b) {
+      uint32_t lo = ~0u, hi = ~0u;                         // lanes of the same digit
+#pragma unroll
+      for (int b = 0; b < kMaxDigit; ++b) {                // (bits that no digit has change nothing)
         const uint64_t set = __ballot(d >> b & 1);
-        same &= d >> b & 1 ? set : ~set;
+        const uint32_t mask = (uint32_t)((int)(d << (31 - b)) >> 31);
+        lo &= ~((uint32_t)set ^ mask);
+        hi &= ~((uint32_t)(set >> 32) ^ mask);
       }
-      const uint32_t before = mine[d];
+      const uint32_t before = mine[d], ahead = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0u));
       asm volatile("" ::: "memory");
       digit[r] = d;
-      place[r] = before + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-      if (__ffsll((unsigned long long)same) - 1 == lane) mine[d] = before + (uint32_t)__popcll(same);
+      place[r] = before + ahead;
+      if (ahead == 0) mine[d] = before + (uint32_t)(__popc(lo) + __popc(hi));
       asm volatile("" ::: "memory");
     }
     __syncthreads();

@@ -260,14 +260,15 @@ __global__ __launch_bounds__(64 * NW) void int8_few_kernel(FewArgs a) {
 // Which calls these kernels take, the others' being the GEMM's.  Weights not in any cache, us (K x N):
 //   17 tokens  3200 x 12 800 11.1 (GEMM 11.0), 3200 x 9600 9.0 (10.5), 12 800 x 3200 10.0 (11.8)
 //   32 tokens  3200 x 12 800 11.9 (11.2), 3200 x 9600 9.1 (10.4), 12 800 x 3200 13.1 (13.0), 1024 x 4096 4.1 (5.9)
-//   64 tokens  3200 x 9600 14.3 (10.5), 12 800 x 3200 18.0 (13.8), 4096 x 1024 6.0 (7.7), 1152 x 4304 4.9 (6.7)
-constexpr int64_t kFewWeights = 1 << 24;
-bool takes_few(int T, int K, int N) { return T <= 32 || (T <= 64 && (int64_t)K * N <= kFewWeights); }
+//   64 tokens  1152 x 4304 4.9 (6.7), 4096 x 1024 6.0 (7.7), 4096 x 4096 8.2 (9.5), 3200 x 6400 8.3 (10.2), 1024 x 8192 5.2 (6.3), 6144 x 2048 8.2 (9.6);
+//              but 3200 x 9600 14.3 (10.5), 1152 x 16 384 9.0 (7.0), 12 800 x 3200 18.0 (13.8)
+bool takes_few(int T, int K, int N) { return T <= 32 || (T <= 64 && N <= 8192 && K <= 8192); }
 
 // One token: rows of up to 4096 bytes two a wave, longer ones a block each (3200 x 12 800 8.3 us, 8.8 with a block each; 12 800 x 3200 8.4 and
 // 7.8).  More: waves and stages are the fastest of ten choices at the sizes above, within 10 %: two waves of four stages where there are many
-// blocks (16 tokens through 3200 x 12 800 9.1 us, with four waves 10.0), four otherwise (through 12 800 x 3200 10.2, with two 12).  Reading
-// the weights as non-temporal is no faster at any of them (16 tokens through 3200 x 12 800: 9.9).
+// blocks (16 tokens through 3200 x 12 800 9.1 us, with four waves 10.0), four otherwise (through 12 800 x 3200 10.2, with two 12); the rings
+// of 64 tokens and four waves fill a unit's LDS, so beyond a block per unit two waves it is (2048 x 6144 6.5, with four 8.4; 2048 x 4096 5.7 and 5.2).
+// Reading the weights as non-temporal is no faster at any of them (16 tokens through 3200 x 12 800: 9.9).
 hipError_t launch_few(const GemmArgs& g, hipStream_t s) {
   FewArgs a{g.A, g.W, g.row_scales, g.col_scales, g.col_bias, g.out, g.lda * 2, g.ldo, g.M, g.N, g.K * 2, g.out_f32};
   void* args[] = {(void*)&a};
@@ -280,7 +281,7 @@ hipError_t launch_few(const GemmArgs& g, hipStream_t s) {
   if (a.T <= 16 && a.N > 8192) { f = (const void*)int8_few_kernel<1, 2, 4>; nw = 2; }
   else if (a.T <= 16) f = (const void*)int8_few_kernel<1, 4, 4>;
   else if (a.T <= 32) f = (const void*)int8_few_kernel<2, 4, 3>;
-  else if (a.K < 2048) { f = (const void*)int8_few_kernel<4, 2, 3>; nw = 2; }
+  else if (a.N > 4096) { f = (const void*)int8_few_kernel<4, 2, 3>; nw = 2; }
   else f = (const void*)int8_few_kernel<4, 4, 3>;
   return hipLaunchKernel(f, dim3((a.N + 15) / 16), dim3(64 * nw), args, 0, s);
 }

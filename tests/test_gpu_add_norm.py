@@ -149,6 +149,36 @@ def test_quant_of_odd_values():
     assert torch.isnan(o["y"][0, 3]) and torch.isnan(o["scale"][0]) and (o["q"][0] == 0).all() and (o["q"][1] == 127).all()
 
 
+def test_a_row_that_is_not_finite_stays_alone():
+    T, D = 40, 3200
+    x, r, gain, gen = inputs(T, D, "bf16", "f32", 5)
+    op = B.AddNorm("bf16", D, residual="f32", max_tokens=T, training=True)
+    want, wq = op.forward(gain, x, r, want=("sum", "y", "q")), B.quant_rows(x)
+    dy = randn(gen, T, D, dtype=torch.bfloat16)
+    wdx = op.backward(gain, want["sum"], dy)["dx"]
+    x[7, 3000], x[9, 0], x[30, 17] = float("nan"), float("inf"), float("-inf")
+    got, gq = op.forward(gain, x, r, want=("sum", "y", "q")), B.quant_rows(x)
+    bad = torch.zeros(T, dtype=torch.bool, device=DEV)
+    bad[[7, 9, 30]] = True
+    for n in ("sum", "y", "q", "scale"):
+        assert torch.equal(got[n][~bad], want[n][~bad]), n
+    assert torch.isnan(got["scale"][bad]).all() and (got["q"][bad] == 0).all() and torch.isnan(got["y"][7]).all()
+    for a, b in zip(gq, wq):
+        assert torch.equal(a[~bad], b[~bad])
+    assert torch.isnan(gq[1][bad]).all() and torch.isnan(B.dequant_rows(*gq)[bad]).all()
+    back = op.backward(gain, got["sum"], dy)
+    assert torch.equal(back["dx"][~bad], wdx[~bad]) and torch.isnan(back["dx"][bad].float()).any(dim=1).all()
+
+
+def test_a_sum_alone_needs_no_gain():
+    x, r, _, _ = inputs(5, 100, "bf16", "f32", 6)
+    op = B.AddNorm("bf16", 100, residual="f32", max_tokens=5)
+    assert torch.equal(op.forward(None, x, r, want=("sum",))["sum"], x.float() + r)
+    for want in ((), ("dx",), ("sum", "scale")):
+        with pytest.raises((ValueError, B.EpdError)):
+            op.forward(None, x, r, want=want)
+
+
 def test_zero_rows():
     op = B.AddNorm("bf16", 40, max_tokens=3, training=True)
     z, gain = torch.zeros(3, 40, dtype=torch.bfloat16, device=DEV), torch.ones(40, dtype=torch.bfloat16, device=DEV)

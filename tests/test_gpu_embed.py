@@ -96,6 +96,17 @@ def test_gradients_of_many_tokens(T, V, D, hot):
         assert torch.equal(op.backward(ids, dout, num_rows=R, want=[name])[name], got[name])
 
 
+def test_one_object_and_calls_of_every_size():
+    """Sizes on both sides of every border -- one launch or several, tokens of a piece, rounds of the sort, lists that are merged -- through one
+    object, whose workspace holds what the calls before left; rows of dout apart."""
+    V, D, R, most = 40, 9, 11, 33000
+    op = B.Embedding("bf16", V, D, out="f32", scale=0.25, max_tokens=most, training=True)
+    for T in (33000, 1, 7, 8, 9, 16, 17, 24, 25, 127, 128, 129, 136, 137, 1023, 1024, 1025, 2049, 4095, 4096, 4097, 8191, 8192, 8193, 16384, 16385, 32768, 32769, 2):
+        gen = generator(T)
+        ids, dout = some_ids(gen, T, V, R, hot=0.3), Gapped(T, D, torch.float32, gap=3, offset=1, values=randn(gen, T, D))
+        check_backward(op.backward(ids, dout.view, num_rows=R), dout.view, ids, 0.25, V, R, "bf16")
+
+
 def test_every_digit_of_a_key():
     # the most visual rows that fit beside a small table: keys of three and four digits, in turn from both ends
     for R in (1 << 18, (1 << 27) + 5):

@@ -4,7 +4,7 @@ the next norm; and the backward pass of what is trained in fp32."""
 import pytest
 import torch
 
-from entry_util import DEV, generator, randn
+from entry_util import DEV, generator, randn, replays
 from paper_2601_11590_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -64,3 +64,40 @@ def test_training_step_of_embedding_and_norm():
     for got, w in zip((e["table"], e["rows"], g["gain"], g["dx"]), want):
         # fp32 throughout: dx within 200 half steps of terms that are a few times its size, sums of up to 200 of them
         assert (got.double() - w).norm() <= 1e-5 * w.norm()
+
+
+def test_a_row_that_is_not_finite_comes_out_as_nan_alone():
+    gen, D, N, T = generator(2), 640, 264, 70
+    x, gain = randn(gen, T, D, dtype=torch.bfloat16), torch.ones(D, dtype=torch.bfloat16, device=DEV)
+    w = dict(zip(("w", "scale"), B.quant_rows(randn(gen, N, D))))
+    norm, linear = B.AddNorm("bf16", D, max_tokens=T), B.Int8Linear(D, N, max_tokens=T)
+
+    def stage():
+        o = norm.forward(gain, x, want=("q",))
+        return linear.forward(w, o["q"], o["scale"])
+
+    want = stage()
+    x[33, 600] = float("inf")
+    got = stage()
+    others = torch.arange(T, device=DEV) != 33
+    assert torch.isnan(got[33]).all() and torch.equal(got[others], want[others])
+
+
+def test_operators_captured_together():
+    """A prompt's way through the operators as one graph, replayed on other prompts."""
+    gen, V, D, N, R, T = generator(3), 300, 512, 512, 40, 150
+    table, visual, gain = randn(gen, V, D, dtype=torch.bfloat16), randn(gen, R, D, dtype=torch.bfloat16), torch.ones(D, dtype=torch.bfloat16, device=DEV)
+    w = dict(zip(("w", "scale"), B.quant_rows(randn(gen, N, D))))
+    ids = torch.randint(-R, V, (T,), generator=gen, device=DEV).to(torch.int32)
+    embed, norm = B.Embedding("bf16", V, D, out="f32", max_tokens=T, training=True), B.AddNorm("bf16", D, residual="f32", max_tokens=T, training=True)
+    linear = B.Int8Linear(D, N, max_tokens=T)
+
+    def call():
+        s = embed.forward(table, ids, visual)
+        o = norm.forward(gain, residual=s, want=("q",))
+        y = linear.forward(w, o["q"], o["scale"])
+        o = norm.forward(gain, y, s)
+        g = norm.backward(gain, o["sum"], o["y"], dsum=o["sum"])
+        return [y, *o.values(), *g.values(), *embed.backward(ids, g["dresidual"], num_rows=R).values()]
+
+    replays(call, lambda v: v, lambda i: ids.copy_(torch.randint(-R - 3, V + 3, (T,), generator=generator(50 + i), device=DEV).to(torch.int32)))

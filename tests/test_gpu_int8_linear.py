@@ -30,7 +30,7 @@ SIZES = [(1, 16, 8), (1, 3200, 136), (1, 2064, 4096), (1, 1040, 72), (2, 32, 16)
          (513, 528, 776), (640, 16, 640), (1000, 80, 1000), (2049, 336, 264)]
 
 # a size for every tile, whole, cut behind its whole rounds, and in parts (test_entry_host_logic.py counts them)
-PLANS = [(1, 5008, 8), (2, 16, 8328), (65, 6272, 3736), (1340, 896, 14648), (4256, 8416, 72), (5697, 14816, 392), (6160, 544, 4208), (10362, 7360, 72),
+PLANS = [(1, 5008, 8), (2, 16, 8328), (35, 16, 5160), (61, 1040, 8192), (64, 8192, 264), (64, 8208, 264), (65, 6272, 3736), (1340, 896, 14648), (4256, 8416, 72), (5697, 14816, 392), (6160, 544, 4208), (10362, 7360, 72),
          (16779, 5200, 80), (18230, 8336, 136), (19241, 144, 680), (25656, 16, 648), (28671, 96, 432), (32410, 3952, 648), (32554, 992, 160), (33870, 7072, 168),
          (36136, 16, 424), (38188, 16, 8), (44024, 3008, 312), (45731, 1840, 88)]
 
