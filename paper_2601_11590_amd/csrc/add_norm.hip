@@ -6,7 +6,8 @@
 // s is not rounded before y is made of it.  Backward, at the s that was kept: n = s * rstd, g = dy * gain,
 //   dx = ds + rstd * (g - n * mean(g n)),   dgain = sum over rows of dy * n
 // rstd is made again: its sum passes over the row beside that of g n.
-// Bound: HBM, each row is read once, held in registers as fp32 between its sums and its results, and written once.
+// Bound: HBM, each row is read once, held in registers as fp32 between its sums and its results, and written once (backward, beyond 16 384
+// columns: read twice, once out of a cache).  32 768 x 3200 with its sum and 8 bits 5.4 TB/s, backward 30 000 x 1024 4.8.
 //
 #include "op_error.h"
 #include "rows.h"
@@ -205,45 +206,76 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGr
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[u][i] = 0.f;
+  // AHEAD: the next row's loads go out before this row's sums (bf16, 30 000 x 1024 51 us, without 68; 10 000 x 2048 36 and 43; 16 384 x 3200 106
+  // and 134), where registers allow: 6000 x 8000 in two chunks of 512 threads 98, without 89.
+  // AGAIN: rows of four chunks a thread and more are read again for the results, out of the caches, as they would not stay in registers (3000 x
+  // 30 000 205 us, spilled 318; 1500 x 65 536 with an fp32 residual 422 and 1136).
+  constexpr bool AHEAD = U == 1 || (U == 2 && TPR < 512), AGAIN = U >= 4;
+  struct Raw {
+    typename raw8_of<R>::type s, o;
+    typename raw8_of<T>::type d;
+  } next[AHEAD ? U : 1];
+  auto fetch = [&](int64_t row, int u, Raw& to) {
+    const int e = (u * TPR + at) * 8, left = a.D - e;
+    if (left <= 0) return;
+    load_raw8((const R*)a.s + row * a.ld_s + e, left, to.s);
+    load_raw8((const T*)a.dy + row * a.ld_dy + e, left, to.d);
+    if (a.ds) load_raw8((const R*)a.ds + row * a.ld_ds + e, left, to.o);
+  };
+  if constexpr (AHEAD) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) if (r0 < r1) fetch(r0, u, next[u]);
+  }
   for (int64_t row = r0; row < r1; ++row) {
-    float s[U][8], d[U][8], o[U][8];
+    float s[AGAIN ? 1 : U][8], d[AGAIN ? 1 : U][8], o[AGAIN ? 1 : U][8];
     float ss = 0.f, gn = 0.f;
+    auto held = [&](int u) {                               // chunk u as floats
+      const int k = AGAIN ? 0 : u;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int e = (u * TPR + at) * 8, left = a.D - e;
+      for (int i = 0; i < 8; ++i) s[k][i] = d[k][i] = o[k][i] = 0.f;
+      if (a.D <= (u * TPR + at) * 8) return;
+      Raw now;
+      if constexpr (AHEAD) now = next[u]; else fetch(row, u, now);
+      from_raw8(now.s, s[k]);
+      from_raw8(now.d, d[k]);
+      if (a.ds) from_raw8(now.o, o[k]);
+    };
+    if constexpr (!AGAIN) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[u][i] = d[u][i] = o[u][i] = 0.f;
-      if (left <= 0) continue;
-      load8((const R*)a.s + row * a.ld_s + e, left, s[u]);
-      load8((const T*)a.dy + row * a.ld_dy + e, left, d[u]);
-      if (a.ds) load8((const R*)a.ds + row * a.ld_ds + e, left, o[u]);
+      for (int u = 0; u < U; ++u) held(u);
+    }
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) if (row + 1 < r1) fetch(row + 1, u, next[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int e = (u * TPR + at) * 8, left = a.D - e;
+      const int e = (u * TPR + at) * 8, left = a.D - e, k = AGAIN ? 0 : u;
+      if constexpr (AGAIN) held(u);
       if (left <= 0) continue;
       float g[8];
       load8((const T*)a.gain + e, left, g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { ss = fmaf(s[u][i], s[u][i], ss); gn = fmaf(d[u][i] * g[i], s[u][i], gn); }
+      for (int i = 0; i < 8; ++i) { ss = fmaf(s[k][i], s[k][i], ss); gn = fmaf(d[k][i] * g[i], s[k][i], gn); }
     }
     row_sums<TPR>(ss, gn, lds);
     const float rstd = 1.0f / sqrtf(fmaf(ss, a.inv_d, a.eps));
-    const float k = gn * rstd * a.inv_d;                   // mean(g n)
+    const float mean = gn * rstd * a.inv_d;                // of g n
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int e = (u * TPR + at) * 8, left = a.D - e;
+      const int e = (u * TPR + at) * 8, left = a.D - e, k = AGAIN ? 0 : u;
+      if constexpr (AGAIN) held(u);
       if (left <= 0) continue;
       float g[8];
       load8((const T*)a.gain + e, left, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float n = s[u][i] * rstd;
-        sums[u][i] = fmaf(d[u][i], n, sums[u][i]);
-        o[u][i] = fmaf(rstd, fmaf(-n, k, d[u][i] * g[i]), o[u][i]);
+        const float n = s[k][i] * rstd;
+        sums[u][i] = fmaf(d[k][i], n, sums[u][i]);
+        o[k][i] = fmaf(rstd, fmaf(-n, mean, d[k][i] * g[i]), o[k][i]);
       }
-      if (a.dx) store8((T*)a.dx + row * a.ld_dx + e, left, o[u]);
-      if (a.dr) store8((R*)a.dr + row * a.ld_dr + e, left, o[u]);
+      if (a.dx) store8((T*)a.dx + row * a.ld_dx + e, left, o[k]);
+      if (a.dr) store8((R*)a.dr + row * a.ld_dr + e, left, o[k]);
     }
   }
   if (!a.parts) return;
@@ -269,18 +301,21 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGr
   }
 }
 
-// gain's gradient: the sums of the blocks, 16 columns a block of 64 groups, in fixed orders.
+// gain's gradient: the sums of the blocks, 32 columns (whole lines of memory) a block of 32 groups, in fixed orders: 512 blocks of 8000 columns
+// 5.0 us, by 16 columns 9.0; 784 of 1024 4.0 either way, the time to launch and read once.
 struct GainArgs { const float* parts; void* out; int n, D; };
+constexpr int kGainCols = 32;
 template <typename T> __global__ __launch_bounds__(1024) void gain_kernel(GainArgs a) {
-  __shared__ float part[64][16];
-  const int l = threadIdx.x & 15, c = blockIdx.x * 16 + l, g = threadIdx.x >> 4;
+  constexpr int G = 1024 / kGainCols;
+  __shared__ float part[G][kGainCols];
+  const int l = threadIdx.x % kGainCols, c = blockIdx.x * kGainCols + l, g = threadIdx.x / kGainCols;
   float v = 0.f;
   if (c < a.D) {
 #pragma unroll 4
-    for (int p = g; p < a.n; p += 64) v += a.parts[(int64_t)p * a.D + c];
+    for (int p = g; p < a.n; p += G) v += a.parts[(int64_t)p * a.D + c];
   }
   part[g][l] = v;
-  for (int n = 32; n > 0; n >>= 1) {
+  for (int n = G / 2; n > 0; n >>= 1) {
     __syncthreads();
     if (g < n) part[g][l] += part[g + n][l];
   }
@@ -311,10 +346,11 @@ template <typename T> __global__ __launch_bounds__(256) void dequant_kernel(Dequ
 }
 
 // f(threads per row, chunks per thread) as integral constants.  Few chunks a thread keep more rows in flight: 32 768 x 3200 with its sum and
-// 8 bits 210 us by 512 threads of one chunk, 221 by 256 of two, 243 by a wave of seven; backward, 10 000 x 2048 42 us by 256 of one, 67 by a
-// wave of four; 6000 x 8192 bf16 forward 74 by 512 of two, 79 by 256 of four; but 6272 x 1024 backward 13.9 by a wave of two, 18.8 by 256 of
-// one.  Rows that are only rounded (NORM = false) have half the loads: 12 800 x 3200 24.3 us by 256 of two, 29.6 by 512 of one, 32 768 x 1152 28.1 by a wave of
-// three, 33.0 by 256 of one.  (Fewer blocks that load the next row ahead are no faster: 24.8 and 32.1.)
+// 8 bits 210 us by 512 threads of one chunk, 221 by 256 of two, 243 by a wave of seven; 6000 x 8192 bf16 forward 74 by 512 of two, 79 by 256 of
+// four; backward (measured without loads ahead) 10 000 x 2048 42 us by 256 of one, 67 by a wave of four, but 6272 x 1024 13.9 by a wave of two, 18.8
+// by 256 of one; with them 6000 x 8000 89 by 512 of two, 96 by 1024 of one.  Rows that are only rounded (NORM = false) have half the loads: 12 800 x
+// 3200 24.3 us by 256 of two, 29.6 by 512 of one, 32 768 x 1152 28.1 by a wave of three, 33.0 by 256 of one.  (Fewer blocks that load the next
+// row ahead are no faster: 24.8 and 32.1.)
 template <bool NORM, class F> hipError_t by_width(int D, F&& f) {
   using std::integral_constant;
 #define EPD_WIDTH(tpr, u) return f(integral_constant<int, tpr>{}, integral_constant<int, u>{})
@@ -351,9 +387,11 @@ template <typename T, typename R, bool NORM> hipError_t launch_norm_rows(const N
   });
 }
 
-// Blocks of the backward pass: the chip filled, then more rows for each group of threads, whose sums it keeps.
+// Blocks of the backward pass: the chip filled, then more rows for each group of threads, whose sums it keeps.  As many as stay resident (16 384 x
+// 3200 with 512 blocks 102 us and 4.8 for gain's kernel, with 1024 106 and 6.2; 20 000 x 400 with 1024 26.8, with 512 32.2; 1500 x 65 536, whose
+// blocks fill a unit each, with 256 422 and 28, with 512 436 and 53).
 int grad_rows_per_block(int D) { return D <= 64 ? 32 : D <= 1024 ? 4 : 1; }      // as by_width has it
-int grad_most_blocks(int D) { return D > 8192 ? 512 : 1024; }
+int grad_most_blocks(int D) { return D > 8192 ? 256 : D > 2048 ? 512 : 1024; }
 int grad_rows(int rows, int D) {         // of a group
   const int64_t groups = (int64_t)grad_most_blocks(D) * grad_rows_per_block(D);
   return (int)((rows + groups - 1) / groups);
@@ -374,7 +412,7 @@ template <typename T, typename R> hipError_t launch_norm_grad(NormGradArgs a, vo
   if (e != hipSuccess || !dgain) return e;
   GainArgs g{a.parts, dgain, blocks, a.D};
   void* gargs[] = {(void*)&g};
-  return hipLaunchKernel((const void*)gain_kernel<T>, dim3((a.D + 15) / 16), dim3(1024), gargs, 0, s);
+  return hipLaunchKernel((const void*)gain_kernel<T>, dim3((a.D + kGainCols - 1) / kGainCols), dim3(1024), gargs, 0, s);
 }
 
 epd_status check_cfg(const char* who, const epd_add_norm_cfg* c) {
@@ -453,7 +491,7 @@ epd_status epd_add_norm_backward(const epd_add_norm_cfg* cfg, const epd_add_norm
     if (!g.gain) return EPD_OK;
     GainArgs a{(const float*)workspace, g.gain, 0, D};
     void* args[] = {(void*)&a};
-    e = hipLaunchKernel(es == 4 ? (const void*)gain_kernel<float> : (const void*)gain_kernel<__bf16>, dim3((D + 15) / 16), dim3(1024), args, 0, (hipStream_t)stream);
+    e = hipLaunchKernel(es == 4 ? (const void*)gain_kernel<float> : (const void*)gain_kernel<__bf16>, dim3((D + kGainCols - 1) / kGainCols), dim3(1024), args, 0, (hipStream_t)stream);
     return e == hipSuccess ? EPD_OK : op_launch_failed(who, e);
   }
   if (epd_status s = check_rows(who, "sum", g.sum, g.ld_sum, tokens, D, rs)) return s;

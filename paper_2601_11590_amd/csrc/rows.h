@@ -54,6 +54,37 @@ __device__ __forceinline__ void store8(float* p, int left, const float* v) {
     for (int i = 0; i < 8; ++i) if (i < left) p[i] = v[i];
   }
 }
+
+// The same in two steps, for loads ahead of their use: eight elements as they lie in memory, and what they stand for.
+struct Raw8bf { bf16v8 v; };
+struct Raw8f { quad4 a, b; };
+template <typename T> struct raw8_of;
+template <> struct raw8_of<__bf16> { typedef Raw8bf type; };
+template <> struct raw8_of<float> { typedef Raw8f type; };
+__device__ __forceinline__ void load_raw8(const __bf16* p, int left, Raw8bf& r) {
+  if (left >= 8) {
+    r.v = __builtin_bit_cast(bf16v8, *(const quad2*)p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = i < left ? p[i] : (__bf16)0.f;
+  }
+}
+__device__ __forceinline__ void load_raw8(const float* p, int left, Raw8f& r) {
+  if (left >= 8) {
+    r.a = *(const quad4*)p; r.b = *(const quad4*)(p + 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { r.a[i] = i < left ? p[i] : 0.f; r.b[i] = 4 + i < left ? p[4 + i] : 0.f; }
+  }
+}
+__device__ __forceinline__ void from_raw8(const Raw8bf& r, float* v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)r.v[i];
+}
+__device__ __forceinline__ void from_raw8(const Raw8f& r, float* v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[i] = r.a[i]; v[4 + i] = r.b[i]; }
+}
 constexpr int64_t kMaxStride = 1ll << 40;
 
 inline bool known_dtype(int dtype) { return dtype == EPD_F32 || dtype == EPD_BF16; }

@@ -87,6 +87,27 @@ def test_backward(dtype, residual, T, D):
             assert torch.equal(op.backward(gain, s, dy, dsum=ds if with_ds else None, want=[name])[name], got[name])
 
 
+@pytest.mark.parametrize("dtype,residual", TYPES)
+@pytest.mark.parametrize("T,D", [(2100, 1100), (1100, 2049), (1030, 8192), (530, 16384), (530, 16392), (261, 65536)])
+def test_several_rows_a_block_and_in_place(dtype, residual, T, D):
+    """Loads of the next row ahead of its turn, and wide rows that are read twice, where the results take the inputs' places."""
+    s, ds, gain, gen = inputs(T, D, residual, residual, 2)
+    gain = gain.to(KINDS[dtype])
+    dy = randn(gen, T, D, dtype=KINDS[dtype])
+    op = B.AddNorm(dtype, D, residual=residual, eps=EPS, max_tokens=T, training=True)
+    got = op.backward(gain, s, dy, dsum=ds, want=("dx", "dresidual", "gain"))
+    h = s.double()
+    rstd = 1 / (h.square().mean(dim=1, keepdim=True) + op.cfg.eps).sqrt()
+    n, g = h * rstd, dy.double() * gain.double()
+    within(got["gain"], (dy.double() * n).sum(dim=0), (60 + T) * U32 * (dy.double() * n).abs().sum(dim=0) + unit(KINDS[dtype]) * (dy.double() * n).sum(dim=0).abs())
+    dx = ds.double() + rstd * (g - n * (g * n).mean(dim=1, keepdim=True))
+    off = 200 * U32 * (ds.double().abs() + rstd * (g.abs() + n.abs() * (g * n).abs().mean(dim=1, keepdim=True)))
+    for k, kind in (("dx", dtype), ("dresidual", residual)):
+        within(got[k], dx, off + unit(KINDS[kind]) * (dx.abs() + off))
+    here = op.backward(gain, s, dy, dsum=ds, want=("dx", "dresidual", "gain"), out={"dx": dy, "dresidual": ds})
+    assert here["dx"] is dy and here["dresidual"] is ds and all(torch.equal(here[k], got[k]) for k in got)
+
+
 def test_gradients_against_differences():
     T, D = 6, 200
     x, r, gain, gen = inputs(T, D, "f32", "f32", 2)
