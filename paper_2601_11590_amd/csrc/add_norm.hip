@@ -322,8 +322,8 @@ template <typename T> __global__ __launch_bounds__(1024) void gain_kernel(GainAr
   if (g == 0 && c < a.D) ((T*)a.out)[c] = (T)part[0][l];
 }
 
-// values = q * scale
-struct DequantArgs { const int8_t* q; const float* scale; void* out; int64_t ld_q, ld_out; int rows, D; };
+// values = q * scale.  Bound: HBM; 32 768 x 3200 into bf16 58 us, 5.4 TB/s; 12 800 x 3200 19.7 (20.8 without writing through).
+struct DequantArgs { const int8_t* q; const float* scale; void* out; int64_t ld_q, ld_out; int rows, D; bool through; };
 template <typename T> __global__ __launch_bounds__(256) void dequant_kernel(DequantArgs a) {
   const int chunks = (a.D + 7) / 8;
   const int64_t all = (int64_t)a.rows * chunks;
@@ -341,7 +341,7 @@ template <typename T> __global__ __launch_bounds__(256) void dequant_kernel(Dequ
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = j < left ? (float)q[j] * s : 0.f;
     }
-    store8((T*)a.out + row * a.ld_out + e, left, v);
+    store8((T*)a.out + row * a.ld_out + e, left, v, a.through);
   }
 }
 
@@ -533,7 +533,7 @@ epd_status epd_dequant_rows(const void* q, int64_t ld_q, const float* scale, int
   if (epd_status s = check_rows(who, "q", q, ld_q, rows, cols, 1)) return s;
   if (epd_status s = check_rows(who, "out", out, ld_out, rows, cols, dtype == EPD_F32 ? 4 : 2)) return s;
   if (!scale || (uintptr_t)scale % 4) return op_fail(EPD_ERR_INVALID_ARG, "%s: scale is NULL or not aligned", who);
-  DequantArgs a{(const int8_t*)q, scale, out, ld_q, ld_out, rows, cols};
+  DequantArgs a{(const int8_t*)q, scale, out, ld_q, ld_out, rows, cols, writes_through(out, ld_out, dtype == EPD_F32 ? 4 : 2)};
   const int64_t threads = (int64_t)rows * ((cols + 7) / 8);
   void* args[] = {(void*)&a};
   const hipError_t e = hipLaunchKernel(dtype == EPD_F32 ? (const void*)dequant_kernel<float> : (const void*)dequant_kernel<__bf16>,

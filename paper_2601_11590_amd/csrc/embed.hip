@@ -32,9 +32,10 @@ struct EmbedArgs {
   int64_t ld_out;
   int tokens, D, vocab, num_rows;
   float scale;
+  bool through;                      // see writes_through
 };
 
-// A wave takes U * 512 elements of a token's row.
+// A wave takes U * 512 elements of a token's row.  16 384 rows of 3584, bf16: 47.2 us, 5.0 TB/s (48.6 ... 49.3 without writing through).
 template <typename T, typename O, int U> __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -59,7 +60,7 @@ template <typename T, typename O, int U> __global__ __launch_bounds__(256) void 
     if (left <= 0) continue;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[u][i] *= scale;
-    store8(out + e, left, v[u]);
+    store8(out + e, left, v[u], a.through);
   }
 }
 
@@ -95,7 +96,11 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs a) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       quad2* const to = (quad2*)a.clear[j];
-      for (int64_t i = t0; i < a.pieces[j]; i += n) to[i] = quad2{0u, 0u, 0u, 0u};
+      if ((uintptr_t)to % 16 == 0) {                       // (65 MB beside 2049 tokens 10.0 us, not written through 11.3 ... 12.8)
+        for (int64_t i = t0; i < a.pieces[j]; i += n) store16_through(to + i, quad2{0u, 0u, 0u, 0u});
+      } else {
+        for (int64_t i = t0; i < a.pieces[j]; i += n) to[i] = quad2{0u, 0u, 0u, 0u};
+      }
       if (t0 < a.tail[j]) ((uint8_t*)(to + a.pieces[j]))[t0] = 0;
     }
     return;
@@ -550,7 +555,7 @@ epd_status epd_embed(const epd_embed_cfg* cfg, const void* table, const void* ro
   if (((uintptr_t)table | (num_rows ? (uintptr_t)rows : 0)) % es) return op_fail(EPD_ERR_INVALID_ARG, "%s: table or rows are not aligned to their elements", who);
   if (tokens == 0) return EPD_OK;
   if (epd_status s = check_rows(who, "out", out, ld_out, tokens, c.hidden, c.out_dtype == EPD_F32 ? 4 : 2)) return s;
-  EmbedArgs a{table, rows, ids, out, ld_out, tokens, c.hidden, c.vocab, num_rows, c.scale};
+  EmbedArgs a{table, rows, ids, out, ld_out, tokens, c.hidden, c.vocab, num_rows, c.scale, writes_through(out, ld_out, c.out_dtype == EPD_F32 ? 4 : 2)};
   void* args[] = {(void*)&a};
   // few tokens: a row over as many waves as it has pieces of 512 (32 rows of 3200: 7 waves each, not 2)
   const bool few = (int64_t)tokens * ((c.hidden + 2047) / 2048) < 4096;
