@@ -1059,11 +1059,8 @@ class AddNorm(_Operator):
         t, kind = out.get(name) if out else None, self._types[name]
         if t is not None:
             return (t, *_matrix(t, name, T, self.hidden, kind, self._index))
-        for l in like:
-            if l is not None and l.dtype == kind:
-                t = torch.empty_like(l)       # (half the time of torch.empty; its rows are contiguous where those of l are)
-                return t, t.data_ptr() or 256, self.hidden
-        t = torch.empty((T, self.hidden), dtype=kind, device=self.device)
+        like = like[0] if like[0] is not None else like[-1]
+        t = torch.empty_like(like, dtype=kind)      # (two thirds of the time of torch.empty; its rows lie side by side where those of `like` are contiguous)
         return t, t.data_ptr() or 256, self.hidden
 
     def forward(self, gain: Optional[torch.Tensor], x: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, want: Sequence[str] = ("sum", "y"),
@@ -1129,8 +1126,11 @@ def quant_rows(x: torch.Tensor, out: Optional[torch.Tensor] = None):
     if index < 0 or len(shape) != 2 or x.dtype not in _CODES or shape[0] >= 1 << 31 or shape[1] >= 1 << 31:
         raise ValueError("x must be a device matrix of float32 or bfloat16")
     px, ld_x = _matrix(x, "x", shape[0], shape[1], x.dtype, index)
-    q = torch.empty(shape, dtype=torch.int8, device=x.device) if out is None else out
-    pq, ld_q = _matrix(q, "out", shape[0], shape[1], torch.int8, index)
+    if out is None:
+        q = torch.empty_like(x, dtype=torch.int8)       # (rows side by side; see AddNorm._output)
+        pq, ld_q = q.data_ptr() or 256, shape[1]
+    else:
+        q, (pq, ld_q) = out, _matrix(out, "out", shape[0], shape[1], torch.int8, index)
     scale = torch.empty(shape[0], dtype=torch.float32, device=x.device)
     _on(index, epd_quant_rows, _CODES[x.dtype], px, ld_x, shape[0], shape[1], pq, ld_q, scale.data_ptr() or 256)
     return q, scale
@@ -1144,8 +1144,10 @@ def dequant_rows(q: torch.Tensor, scale: torch.Tensor, dtype: str = "bf16", out:
     pq, ld_q = _matrix(q, "q", shape[0], shape[1], torch.int8, index)
     ps = _dense(scale, "scale", (shape[0],), torch.float32, index)
     if out is None:
-        out = torch.empty(shape, dtype=kind, device=q.device)
-    po, ld_o = _matrix(out, "out", shape[0], shape[1], kind, index)
+        out = torch.empty_like(q, dtype=kind)
+        po, ld_o = out.data_ptr() or 256, shape[1]
+    else:
+        po, ld_o = _matrix(out, "out", shape[0], shape[1], kind, index)
     _on(index, epd_dequant_rows, pq, ld_q, ps, shape[0], shape[1], _DTYPES[dtype], po, ld_o)
     return out
 

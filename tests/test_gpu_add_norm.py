@@ -147,6 +147,19 @@ def test_quant_and_back(dtype, T, D):
         assert torch.equal(v, (q.float() * scale[:, None]).to(KINDS[out]))
 
 
+def test_quant_of_rows_apart_makes_dense_outputs():
+    gen = generator(31)
+    base = randn(gen, 12, 40)
+    for x in (base[:, 3:20], base[::2, :1], base[5:6], base[5:6, 7:8], base.t()[:1, :1], base[4:5, :9].expand(1, 9)):
+        q, scale = B.quant_rows(x)
+        wq, ws = B.quant_rows(x.contiguous().clone(memory_format=torch.contiguous_format))
+        assert q.is_contiguous() and q.dtype == torch.int8 and q.shape == x.shape and torch.equal(q, wq) and torch.equal(scale, ws)
+        wide = torch.full((x.shape[0], x.shape[1] + 3), 99, dtype=torch.int8, device=DEV)
+        wide[:, 1:-2] = q
+        back = B.dequant_rows(wide[:, 1:-2], scale, "f32")
+        assert back.is_contiguous() and torch.equal(back, q.float() * scale[:, None])
+
+
 def test_quant_of_odd_values():
     inf, nan = float("inf"), float("nan")
     rows = [[0.0, -0.0, 0.0], [1e-38, -1e-38, 0.0], [3e38, -3e38, 1.0], [1.0, inf, 2.0], [1.0, -inf, nan], [nan, 1.0, 2.0], [127.0, 0.5, 1.5], [-127.0, 2.5, -0.5], [1.0, 1.0, 1.0]]
