@@ -449,7 +449,8 @@ epd_status epd_add_norm(const epd_add_norm_cfg* cfg, const epd_add_norm_rows* ro
 uint64_t epd_add_norm_workspace_bytes(const epd_add_norm_cfg* cfg);
 
 /* Gradients of sum(y * dy) + sum(s * dsum) by x (and the residual) and by gain, at `sum`.  The workspace is not looked at where the
- * gradient of gain is not wanted; tokens = 0 clears it. */
+ * gradient of gain is not wanted; tokens = 0 clears it.  A row whose mean squares are beyond fp32 has dx = dsum, or NaN where the sum of
+ * its gradients is beyond fp32 too. */
 epd_status epd_add_norm_backward(const epd_add_norm_cfg* cfg, const epd_add_norm_grads* grads, const void* gain, int32_t tokens,
                                  void* workspace, uint64_t workspace_bytes, void* stream);
 

@@ -5,12 +5,13 @@
 // Backward.  Text and visual rows are one range of keys, the table's rows and behind them those of V_m:
 //   grad[key] = sum of dout over the tokens of that key (* scale)
 // The tokens are sorted by key, which puts those of a row side by side; blocks then add runs of equal keys (up to 128 tokens: few_kernel).  Nothing is added
-// atomically, so a gradient's bits depend on the ids alone.
+// atomically (an atomic counter only gives long runs their places in a list), so a gradient's bits depend on ids and values alone.
 //   1. sort_kernel: up to 4096 tokens a block, sorted in LDS by their keys' digits, from the lowest up, keeping the order of equal ones;
-//      meanwhile the other blocks clear the gradients, which is most of what is written where the table is large
+//      meanwhile other blocks clear the gradients, or as much of them as the sort hides (4096 keys of 18 bits 11 us; 65 MB beside 2049 tokens 10)
 //   2. merge_kernel (more than 4096 tokens): eight sorted lists into one at a time: an element's place is its own plus the numbers of
 //      smaller ones in the other lists
-//   3. sums_kernel: pieces of 8 to 32 sorted tokens; runs within a piece and the next are written, longer ones left as partial sums
+//   3. sums_kernel: pieces of 8 to 32 sorted tokens; runs within a piece and the next are written, longer ones left as partial sums; where the
+//      tokens' rows are many, its other blocks clear the rest of the rows of no token (32 768 fp32 rows of 3200 into 131 072 in bf16: 257 us, 4.5 TB/s)
 //   4. runs_kernel: those, so that a token that takes every other place costs no more than others
 #include "op_error.h"
 #include "rows.h"
@@ -301,7 +302,7 @@ template <typename T> __device__ __forceinline__ void clear_rows(const SumsArgs&
 // whether it counts -- is made for all of a batch at once by its lanes: read from LDS token by token it took longer than the rows
 // (230 rows of one token: 56 us).
 //   TINY: rows of fewer than eight elements.  Otherwise the last eight of a row stand in for the ones that would run past it, which two
-// threads then write alike, so that no load waits behind a branch (embed-grad of 32 768 x 3200 with branches: 190 us).
+// threads then write alike, so that no load waits behind a branch: a batch's loads go out together.
 template <typename T, typename O, bool TINY, int BATCH>
 __device__ __forceinline__ void add_runs(const SumsArgs& a, const uint32_t* key, const uint32_t* at, int first, int last, bool from_before, int piece, int e) {
   const int lane = threadIdx.x & 63;
@@ -402,8 +403,8 @@ template <typename T, typename O, bool TINY> __global__ __launch_bounds__(256) v
   add_runs<T, O, TINY, 8>(a, key, at, first, last, from_before, piece, (slice * 256 + (int)threadIdx.x) * 8);          // (the ballots above need every lane)
 }
 
-// Up to kFewTokens tokens: every block sorts them for itself, by how many go before each, so that one launch does for all (150 rows of 382
-// 9.6 us, by three launches 15.6).  Runs are added whole by the wave whose piece they start in, 2.8 us for 16 rows, which is why more tokens
+// Up to kFewTokens tokens: every block sorts them for itself, by how many go before each, so that one launch does for all (100 rows of 382
+// 8.2 us, by three launches 15).  Runs are added whole by the wave whose piece they start in, 2.8 us for 16 rows, which is why more tokens
 // take the other way: a token that takes most of 256 places, 43 us.
 constexpr int kFewTokens = 128;
 template <typename T, typename O, bool TINY> __global__ __launch_bounds__(256) void few_kernel(SumsArgs a) {

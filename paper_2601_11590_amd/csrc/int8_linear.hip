@@ -13,6 +13,8 @@ namespace epd {
 
 namespace {
 
+// Bound: large products by the matrix cores and the clock that the power limit leaves them (32 768 x 3200 x 12 800: 1060 us, 2.53 POP/s); those of few
+// rounds by the last, which is not full, and the epilogue, which nothing hides (7057 x 1152 x 4304: 42 us; its operations at that rate 28).
 template <class T, int OUT>
 __global__ __launch_bounds__(T::NT, T::MINBLK) void int8_gemm_kernel(GemmArgs g) {
   // stages, scales of the rows, scales and bias of the columns
@@ -32,7 +34,8 @@ template <class T> hipError_t launch_whole(const GemmArgs& g, hipStream_t s) {
   return hipLaunchKernel(g.out_f32 ? (const void*)int8_gemm_kernel<T, OUT_F32> : (const void*)int8_gemm_kernel<T, OUT_BF16>, dim3(tiles_m * tiles_n), dim3(T::NT), args, 0, s);
 }
 
-// K in parts of k_part (pairs of values, a multiple of 64), each a block's own: int32 sums [part][M][N] for scale_kernel.
+// K in parts of k_part (pairs of values, a multiple of 64), each a block's own: int32 sums [part][M][N] for int8_scale_kernel.  Few rows leave most
+// of the chip idle: 200 x 12 800 x 3200 19.1 + 4.0 us, whole 32.0; 1000 rows 47.3 + 6.3, whole 67.4.
 struct SplitArgs { GemmArgs g; int k_part; };
 template <class T> __global__ __launch_bounds__(T::NT, T::MINBLK) void int8_split_kernel(SplitArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS_BYTES + T::BM * 4 + T::BN * 8];
@@ -49,7 +52,7 @@ template <class T> __global__ __launch_bounds__(T::NT, T::MINBLK) void int8_spli
   gemm_tile<T, EPI_INT8_SUMS, OUT_F32, false, false, T::PINGPONG, T::PINGPONG>(g, tm * T::BM, tn * T::BN, lds);
 }
 
-// y = sum of the parts * scales + bias, eight columns a thread.
+// y = sum of the parts * scales + bias, eight columns a thread.  Bound: latency, a launch and a read of what the last kernel wrote.
 struct ScaleArgs { const int* in; const float *row_scales, *col_scales, *col_bias; void* out; int parts, M, N, ldo; };
 constexpr int kSplits = 8, kPartK = 256;                          // parts at most, and the shortest one in pairs
 constexpr int64_t kSplitSums = 1 << 24;                           // sums of all parts at most: 64 MB
@@ -111,7 +114,7 @@ __device__ __forceinline__ void store_one(const FewArgs& a, int t, int n, int su
 }
 
 // One token: R rows of W a wave, or a block with K of its four waves in turn, 16 bytes a lane and access straight to registers, four
-// products an instruction.
+// products an instruction.  Bound: HBM, the weights: 3200 x 12 800 8.3 us, 4.9 TB/s.
 template <int SPLIT, int R, int U>
 __global__ __launch_bounds__(256) void int8_one_kernel(FewArgs a) {
   __shared__ int part[4][R];
@@ -158,7 +161,7 @@ __global__ __launch_bounds__(256) void int8_one_kernel(FewArgs a) {
 
 // Up to 16 NB tokens: a block makes 16 rows of W for all of them; its waves take K in turn, 128 at a time, each with a ring of S stages of
 // its own in LDS, which direct loads of 8 rows x 128 bytes fill and nobody else reads, so no wave waits for another until their sums meet.
-// Bound: HBM, every weight is read once.
+// Bound: HBM, every weight is read once: 16 tokens through 3200 x 12 800 9.1 ... 9.7 us, 4.2 ... 4.5 TB/s.
 #define EPD_DSR(d, a, o) "ds_read_b128 %" #d ", %" #a " offset:%" #o "\n\t"
 template <int N> __device__ __forceinline__ void read_stage(bf16x8* f, uint32_t a0, uint32_t a1) {      // one asm block with its wait, as read_frags
   static_assert(N == 1 || N == 2 || N == 4, "blocks");
