@@ -874,7 +874,15 @@ class GatedMLP:
         return out
 
 
+def _beyond_int32(who: str) -> None:
+    raise ValueError("%s: sizes must be int32" % who)
+
+
+# What these entries take as int32 is looked at here, or-ed together, as ctypes would cut it to its lower 32 bits: a number beyond takes all of it
+# out of -2^31 ... 2^31 - 1, or stands beside a negative one, which the library refuses.
 def epd_embed(cfg: epd_embed_cfg, table: int, rows: Optional[int], num_rows: int, ids: int, tokens: int, out: int, ld_out: int, stream: int) -> None:
+    if not -1 << 31 <= num_rows | tokens < 1 << 31:
+        _beyond_int32("epd_embed")
     _op_check(lib.epd_embed(cfg, table, rows, num_rows, ids, tokens, out, ld_out, stream))
 
 
@@ -884,10 +892,14 @@ def epd_embed_workspace_bytes(cfg: epd_embed_cfg) -> int:
 
 def epd_embed_backward(cfg: epd_embed_cfg, ids: int, tokens: int, dout: int, ld_dout: int, num_rows: int, dtable: Optional[int], drows: Optional[int],
                        workspace: int, workspace_bytes: int, stream: int) -> None:
+    if not -1 << 31 <= num_rows | tokens < 1 << 31:
+        _beyond_int32("epd_embed_backward")
     _op_check(lib.epd_embed_backward(cfg, ids, tokens, dout, ld_dout, num_rows, dtable, drows, workspace, workspace_bytes, stream))
 
 
 def epd_add_norm(cfg: epd_add_norm_cfg, rows: epd_add_norm_rows, gain: Optional[int], tokens: int, stream: int) -> None:
+    if not -1 << 31 <= tokens < 1 << 31:
+        _beyond_int32("epd_add_norm")
     _op_check(lib.epd_add_norm(cfg, rows, gain, tokens, stream))
 
 
@@ -896,14 +908,20 @@ def epd_add_norm_workspace_bytes(cfg: epd_add_norm_cfg) -> int:
 
 
 def epd_add_norm_backward(cfg: epd_add_norm_cfg, grads: epd_add_norm_grads, gain: int, tokens: int, workspace: Optional[int], workspace_bytes: int, stream: int) -> None:
+    if not -1 << 31 <= tokens < 1 << 31:
+        _beyond_int32("epd_add_norm_backward")
     _op_check(lib.epd_add_norm_backward(cfg, grads, gain, tokens, workspace, workspace_bytes, stream))
 
 
 def epd_quant_rows(dtype: int, x: int, ld_x: int, rows: int, cols: int, q: int, ld_q: int, scale: int, stream: int) -> None:
+    if not -1 << 31 <= dtype | rows | cols < 1 << 31:
+        _beyond_int32("epd_quant_rows")
     _op_check(lib.epd_quant_rows(dtype, x, ld_x, rows, cols, q, ld_q, scale, stream))
 
 
 def epd_dequant_rows(q: int, ld_q: int, scale: int, rows: int, cols: int, dtype: int, out: int, ld_out: int, stream: int) -> None:
+    if not -1 << 31 <= dtype | rows | cols < 1 << 31:
+        _beyond_int32("epd_dequant_rows")
     _op_check(lib.epd_dequant_rows(q, ld_q, scale, rows, cols, dtype, out, ld_out, stream))
 
 
@@ -913,6 +931,8 @@ def epd_int8_linear_workspace_bytes(cfg: epd_int8_linear_cfg) -> int:
 
 def epd_int8_linear(cfg: epd_int8_linear_cfg, weights: epd_int8_linear_weights, x: int, ld_x: int, x_scale: int, tokens: int, y: int, ld_y: int,
                     workspace: int, workspace_bytes: int, stream: int) -> None:
+    if not -1 << 31 <= tokens < 1 << 31:
+        _beyond_int32("epd_int8_linear")
     _op_check(lib.epd_int8_linear(cfg, weights, x, ld_x, x_scale, tokens, y, ld_y, workspace, workspace_bytes, stream))
 
 
