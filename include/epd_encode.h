@@ -413,8 +413,8 @@ epd_status epd_embed_backward(const epd_embed_cfg* cfg, const int32_t* ids, int3
                               void* dtable, void* drows, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* The residual's addition and RMS norm:  s = x + residual,  y = s / sqrt(mean(s^2) + eps) * gain, in fp32; s is rounded where it is
- * kept (sum) and not before y is made of it.  q: y in 8 bits, as epd_quant_rows makes them of y before any rounding.  Mean squares
- * beyond fp32 give zeros. */
+ * kept (sum) and not before y is made of it.  q: y in 8 bits, as epd_quant_rows makes them of y before any rounding.  Rows of finite s
+ * may be of any size, as their squares need not fit fp32; where 1 / sqrt(mean(s^2) + eps) itself does not, fp32's largest number stands for it. */
 typedef struct {
   uint32_t struct_size;   /* sizeof(epd_add_norm_cfg)                                                */
   int32_t dtype;          /* epd_dtype of x, gain, y and their gradients                             */
@@ -449,8 +449,8 @@ epd_status epd_add_norm(const epd_add_norm_cfg* cfg, const epd_add_norm_rows* ro
 uint64_t epd_add_norm_workspace_bytes(const epd_add_norm_cfg* cfg);
 
 /* Gradients of sum(y * dy) + sum(s * dsum) by x (and the residual) and by gain, at `sum`.  The workspace is not looked at where the
- * gradient of gain is not wanted; tokens = 0 clears it.  A row whose mean squares are beyond fp32 has dx = dsum, or NaN where the sum of
- * its gradients is beyond fp32 too. */
+ * gradient of gain is not wanted; tokens = 0 clears it.  Rows may be of any size as above, but one whose sum of
+ * dy * gain * s is beyond fp32 has a dx that is not finite. */
 epd_status epd_add_norm_backward(const epd_add_norm_cfg* cfg, const epd_add_norm_grads* grads, const void* gain, int32_t tokens,
                                  void* workspace, uint64_t workspace_bytes, void* stream);
 

@@ -86,6 +86,21 @@ template <int TPR> __device__ __forceinline__ void row_sums(float& a, float& b, 
     a = v.x; b = v.y;
   }
 }
+
+// Mean squares that fp32 does not hold: a sum beyond it, or, where eps does not hide it, so small a mean that squares lost bits.  Those rows' sums are
+// made again of their values times 2^shift, and eps times its square: once where they are large, twice where they are smallest.  The other rows' bits
+// stay as without this, and their times within 2 % (32 768 x 3200 with its sum and 8 bits 197 us either way, 10 000 x 2048 28.4 and 29.0).  Every
+// thread of a row has the same mean, bit by bit, so all go the same way; rows of zeros or with a NaN or an infinity end as they would have.
+constexpr float kLeastMean = 7.888609052210118e-31f;      // 2^-100: what is below the last bit of a square, 2^-150, is 2^-50 of it
+constexpr int kScalings = 2;
+__device__ __forceinline__ bool fp32_holds(float mean) { return mean >= kLeastMean && mean < __builtin_inff(); }
+__device__ __forceinline__ int scale_step(float mean) { return mean < 1.f ? 64 : -80; }
+// 1 / sqrt(mean) of the row itself, given the mean of the scaled values; beyond fp32 its largest number.
+__device__ __forceinline__ float row_rstd(float mean, int shift) {
+  const float rstd = 1.0f / sqrtf(mean);
+  return shift && mean > 0.f ? fminf(ldexpf(rstd, shift), 3.402823466e38f) : rstd;
+}
+
 struct NormArgs {
   const void *x, *r, *gain;          // x or r may be nullptr, and any output
   void *sum, *y;
@@ -149,7 +164,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss = fmaf(v[u][i], v[u][i], ss);
     ss = row_reduce<Sum, TPR>(ss, lds);
-    const float rstd = 1.0f / sqrtf(fmaf(ss, a.inv_d, a.eps));
+    float mean = fmaf(ss, a.inv_d, a.eps);
+    int shift = 0;
+    for (int j = 0; j < kScalings && __builtin_expect(!fp32_holds(mean), 0); ++j) {
+      shift += scale_step(mean);
+      ss = 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { const float w = ldexpf(v[u][i], shift); ss = fmaf(w, w, ss); }
+      mean = fmaf(row_reduce<Sum, TPR>(ss, lds), a.inv_d, ldexpf(a.eps, 2 * shift));
+    }
+    const float rstd = row_rstd(mean, shift);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int e = (u * TPR + at) * 8, left = a.D - e;
@@ -259,8 +285,26 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGr
       for (int i = 0; i < 8; ++i) { ss = fmaf(s[k][i], s[k][i], ss); gn = fmaf(d[k][i] * g[i], s[k][i], gn); }
     }
     row_sums<TPR>(ss, gn, lds);
-    const float rstd = 1.0f / sqrtf(fmaf(ss, a.inv_d, a.eps));
-    const float mean = gn * rstd * a.inv_d;                // of g n
+    float var = fmaf(ss, a.inv_d, a.eps);
+    int shift = 0;
+    for (int j = 0; j < kScalings && __builtin_expect(!fp32_holds(var), 0); ++j) {
+      shift += scale_step(var);
+      ss = gn = 0.f;
+#pragma unroll(AGAIN ? 1 : U)
+      for (int u = 0; u < U; ++u) {
+        const int e = (u * TPR + at) * 8, left = a.D - e, k = AGAIN ? 0 : u;
+        if constexpr (AGAIN) held(u);
+        if (left <= 0) continue;
+        float g[8];
+        load8((const T*)a.gain + e, left, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { const float v = ldexpf(s[k][i], shift); ss = fmaf(v, v, ss); gn = fmaf(d[k][i] * g[i], v, gn); }
+      }
+      row_sums<TPR>(ss, gn, lds);
+      var = fmaf(ss, a.inv_d, ldexpf(a.eps, 2 * shift));
+    }
+    const float rstd = row_rstd(var, shift);
+    const float mean = gn * (1.0f / sqrtf(var)) * a.inv_d; // of g n
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int e = (u * TPR + at) * 8, left = a.D - e, k = AGAIN ? 0 : u;
