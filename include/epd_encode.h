@@ -484,8 +484,8 @@ typedef struct {        /* device, dense                                        
 uint64_t epd_int8_linear_workspace_bytes(const epd_int8_linear_cfg* cfg);
 
 /* x device int8 [tokens, K], 16-byte aligned, rows ld_x apart: a multiple of 16, K .. 2^22 - 16; x_scale device [tokens]; y device [tokens, N], 16-byte
- * aligned, rows ld_y elements apart: a multiple of 8, N .. 2^22 - 8 (the ld of a single row is not looked at).  tokens = 0 launches nothing.
- * Nothing in the workspace is kept from one call to the next. */
+ * aligned, rows ld_y elements apart: a multiple of 8, N .. 2^22 - 8 in bf16, N .. 2^21 - 8 in fp32 (the ld of a single row is not looked at).
+ * tokens = 0 launches nothing.  Nothing in the workspace is kept from one call to the next. */
 epd_status epd_int8_linear(const epd_int8_linear_cfg* cfg, const epd_int8_linear_weights* weights, const void* x, int64_t ld_x, const float* x_scale,
                            int32_t tokens, void* y, int64_t ld_y, void* workspace, uint64_t workspace_bytes, void* stream);
 

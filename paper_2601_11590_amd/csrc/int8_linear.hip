@@ -433,8 +433,8 @@ epd_status epd_int8_linear(const epd_int8_linear_cfg* cfg, const epd_int8_linear
   if (tokens == 1) { ld_x = K; ld_y = N; }
   // (rows of a wave's tile stay below 2^31 bytes)
   const int64_t most_y = c.out_dtype == EPD_F32 ? kMaxTokens / 2 : kMaxTokens;
-  if (ld_x < K || ld_x >= kMaxTokens || ld_x % 16) return op_fail(EPD_ERR_SHAPE, "%s: rows of x are %lld apart: a multiple of 16, in_features %d .. 2^22", who, (long long)ld_x, K);
-  if (ld_y < N || ld_y >= most_y || ld_y % 8) return op_fail(EPD_ERR_SHAPE, "%s: rows of y are %lld apart: a multiple of 8, out_features %d .. %lld", who, (long long)ld_y, N, (long long)most_y);
+  if (ld_x < K || ld_x >= kMaxTokens || ld_x % 16) return op_fail(EPD_ERR_SHAPE, "%s: rows of x are %lld apart: a multiple of 16, in_features %d .. 2^22 - 16", who, (long long)ld_x, K);
+  if (ld_y < N || ld_y >= most_y || ld_y % 8) return op_fail(EPD_ERR_SHAPE, "%s: rows of y are %lld apart: a multiple of 8, out_features %d .. %lld", who, (long long)ld_y, N, (long long)most_y - 8);
   if (((uintptr_t)x | (uintptr_t)y) % 16) return op_fail(EPD_ERR_UNSUPPORTED, "%s: x and y must be aligned to 16 bytes", who);
   if ((uintptr_t)x_scale % 4) return op_fail(EPD_ERR_INVALID_ARG, "%s: x_scale is not aligned", who);
   GemmArgs g{};
