@@ -7,7 +7,7 @@
 //   dx = ds + rstd * (g - n * mean(g n)),   dgain = sum over rows of dy * n
 // rstd is made again: its sum passes over the row beside that of g n.
 // Bound: HBM, each row is read once, held in registers as fp32 between its sums and its results, and written once (backward, beyond 16 384
-// columns: read twice, once out of a cache).  32 768 x 3200 with its sum and 8 bits 5.4 TB/s, backward 30 000 x 1024 4.8.
+// columns: read twice, once out of a cache).  32 768 x 3200 with its sum and 8 bits 5.7 TB/s, backward 30 000 x 1024 4.8.
 //
 #include "op_error.h"
 #include "rows.h"
@@ -234,8 +234,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGr
     for (int i = 0; i < 8; ++i) sums[u][i] = 0.f;
   // AHEAD: the next row's loads go out before this row's sums (bf16, 30 000 x 1024 51 us, without 68; 10 000 x 2048 36 and 43; 16 384 x 3200 106
   // and 134), where registers allow: 6000 x 8000 in two chunks of 512 threads 98, without 89.
-  // AGAIN: rows of four chunks a thread and more are read again for the results, out of the caches, as they would not stay in registers (3000 x
-  // 30 000 205 us, spilled 318; 1500 x 65 536 with an fp32 residual 422 and 1136).
+  // AGAIN: rows of four chunks a thread and more are read again for the results, out of the caches, as floats of all would not stay in registers (3000
+  // x 30 000 201 us, spilled 318; 1500 x 65 536 with an fp32 residual 425 and 1136).  Of eight chunks a thread 12 to 18 registers still spill.
   constexpr bool AHEAD = U == 1 || (U == 2 && TPR < 512), AGAIN = U >= 4;
   struct Raw {
     typename raw8_of<R>::type s, o;
@@ -366,7 +366,7 @@ template <typename T> __global__ __launch_bounds__(1024) void gain_kernel(GainAr
   if (g == 0 && c < a.D) ((T*)a.out)[c] = (T)part[0][l];
 }
 
-// values = q * scale.  Bound: HBM; 32 768 x 3200 into bf16 58 us, 5.4 TB/s; 12 800 x 3200 19.7 (20.8 without writing through).
+// values = q * scale.  Bound: HBM; 32 768 x 3200 into bf16 53 us, 6.0 TB/s; 12 800 x 3200 19.2 (20.8 without writing through).
 struct DequantArgs { const int8_t* q; const float* scale; void* out; int64_t ld_q, ld_out; int rows, D; bool through; };
 template <typename T> __global__ __launch_bounds__(256) void dequant_kernel(DequantArgs a) {
   const int chunks = (a.D + 7) / 8;

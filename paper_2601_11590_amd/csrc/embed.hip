@@ -24,7 +24,7 @@ namespace epd {
 namespace {
 
 constexpr int kEmbedDim = 65536, kEmbedRows = 1 << 30, kEmbedTokens = 1 << 24;
-constexpr int64_t kEmbedElements = 1ll << 38;              // of all tokens: a launch has fewer than 2^32 threads
+constexpr int64_t kEmbedElements = 1ll << 38;              // of all tokens: a launch has fewer than 2^32 threads along each axis of its grid
 
 struct EmbedArgs {
   const void *table, *rows;

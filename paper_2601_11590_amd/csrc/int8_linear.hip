@@ -13,8 +13,9 @@ namespace epd {
 
 namespace {
 
-// Bound: large products by the matrix cores and the clock that the power limit leaves them (32 768 x 3200 x 12 800: 1060 us, 2.53 POP/s); those of few
-// rounds by the last, which is not full, and the epilogue, which nothing hides (7057 x 1152 x 4304: 42 us; its operations at that rate 28).
+// Bound: large products by the matrix cores and the clock that the power limit leaves them (32 768 x 3200 x 12 800: 1074 us, 2.5 POP/s at 1394 W of the
+// board's 1400; on zeros 831 us at 1070 W); those of few rounds by the last, which is not full, and the epilogue, which nothing hides (7057 x 1152 x
+// 4304: 42.5 us; its operations at that rate 28).
 template <class T, int OUT>
 __global__ __launch_bounds__(T::NT, T::MINBLK) void int8_gemm_kernel(GemmArgs g) {
   // stages, scales of the rows, scales and bias of the columns
@@ -35,7 +36,8 @@ template <class T> hipError_t launch_whole(const GemmArgs& g, hipStream_t s) {
 }
 
 // K in parts of k_part (pairs of values, a multiple of 64), each a block's own: int32 sums [part][M][N] for int8_scale_kernel.  Few rows leave most
-// of the chip idle: 200 x 12 800 x 3200 19.1 + 4.0 us, whole 32.0; 1000 rows 47.3 + 6.3, whole 67.4.
+// of the chip idle: 200 x 12 800 x 3200 19.1 + 4.0 us, whole 32.0; 1000 rows 47.3 + 6.3, whole 67.4.  (Weights of three products in turn, which the
+// chip's last cache holds; out of HBM 25 and 57 together.)
 struct SplitArgs { GemmArgs g; int k_part; };
 template <class T> __global__ __launch_bounds__(T::NT, T::MINBLK) void int8_split_kernel(SplitArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS_BYTES + T::BM * 4 + T::BN * 8];
@@ -114,7 +116,7 @@ __device__ __forceinline__ void store_one(const FewArgs& a, int t, int n, int su
 }
 
 // One token: R rows of W a wave, or a block with K of its four waves in turn, 16 bytes a lane and access straight to registers, four
-// products an instruction.  Bound: HBM, the weights: 3200 x 12 800 8.3 us, 4.9 TB/s.
+// products an instruction.  Bound: the weights' way to the chip: 3200 x 12 800 8.3 us, 4.9 TB/s, out of its last cache, 9.3 us, 4.4 TB/s, out of HBM.
 template <int SPLIT, int R, int U>
 __global__ __launch_bounds__(256) void int8_one_kernel(FewArgs a) {
   __shared__ int part[4][R];
@@ -161,7 +163,7 @@ __global__ __launch_bounds__(256) void int8_one_kernel(FewArgs a) {
 
 // Up to 16 NB tokens: a block makes 16 rows of W for all of them; its waves take K in turn, 128 at a time, each with a ring of S stages of
 // its own in LDS, which direct loads of 8 rows x 128 bytes fill and nobody else reads, so no wave waits for another until their sums meet.
-// Bound: HBM, every weight is read once: 16 tokens through 3200 x 12 800 9.1 ... 9.7 us, 4.2 ... 4.5 TB/s.
+// Bound: the weights' way to the chip, each read once: 16 tokens through 3200 x 12 800 9.1 ... 9.7 us, 4.2 ... 4.5 TB/s, out of its last cache, 10.9 out of HBM.
 #define EPD_DSR(d, a, o) "ds_read_b128 %" #d ", %" #a " offset:%" #o "\n\t"
 template <int N> __device__ __forceinline__ void read_stage(bf16x8* f, uint32_t a0, uint32_t a1) {      // one asm block with its wait, as read_frags
   static_assert(N == 1 || N == 2 || N == 4, "blocks");
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(64 * NW) void int8_few_kernel(FewArgs a) {
   }
 }
 
-// Which calls these kernels take, the others' being the GEMM's.  Weights not in any cache, us (K x N):
+// Which calls these kernels take, the others' being the GEMM's.  Weights not in L2, us (K x N):
 //   17 tokens  3200 x 12 800 11.1 (GEMM 11.0), 3200 x 9600 9.0 (10.5), 12 800 x 3200 10.0 (11.8)
 //   32 tokens  3200 x 12 800 11.9 (11.2), 3200 x 9600 9.1 (10.4), 12 800 x 3200 13.1 (13.0), 1024 x 4096 4.1 (5.9)
 //   64 tokens  1152 x 4304 4.9 (6.7), 4096 x 1024 6.0 (7.7), 4096 x 4096 8.2 (9.5), 3200 x 6400 8.3 (10.2), 1024 x 8192 5.2 (6.3), 6144 x 2048 8.2 (9.6);
@@ -311,8 +313,8 @@ hipError_t launch_split(const GemmArgs& g, int tile, int parts, int k_part, void
 }
 
 // Time of a launch in us: per round of blocks alpha * K / 2048 + beta (bf16 or fp32 out; the last round, of a share f of the blocks, last0 +
-// last1 * f of that), and `launch`.  Fitted to 194 shapes in every tile (17 ... 32 768 tokens, K 32 ... 12 800, N 16 ... 12 800, weights not in any
-// cache): 5 ... 10 % off in the mean.  Over these shapes, whole and in parts, what it ranks first is 1.3 % slower than the fastest in the mean, 19 % at
+// last1 * f of that), and `launch`.  Fitted to 194 shapes in every tile (17 ... 32 768 tokens, K 32 ... 12 800, N 16 ... 12 800, weights not in L2):
+// 5 ... 10 % off in the mean.  Over these shapes, whole and in parts, what it ranks first is 1.3 % slower than the fastest in the mean, 19 % at
 // most (568 tokens, 12 800 x 3200: 48.8 us, 41.1), and within 3 % in 166.
 struct Int8Tile { int cfg, bm, bn, blocks; double last0, last1, launch, alpha, beta[2]; bool parts; };
 constexpr Int8Tile kInt8Tiles[] = {
